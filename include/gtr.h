@@ -402,6 +402,157 @@ gtr_status gtr_heads_merge(const void* src, void* dst, int32_t B, int32_t H, int
 gtr_status gtr_add(const void* a, const void* b, void* y, int64_t n, gtr_dtype dtype, hipStream_t stream);
 
 /*
+ * Training a block's channel mixer: layer normalisation and the gated
+ * feed-forward, each with its backward pass. Statuses, streams and checks as
+ * for every call above: every check runs before any launch, nothing is
+ * allocated, results are the same on every run (no sum depends on the order in
+ * which work-groups run), and the calls may be recorded into a HIP graph.
+ *
+ * gtr_layernorm_fwd: for every row m of d channels, in float32,
+ *   mean = sum_j x_j / d, rstd = (sum_j (x_j - mean)^2 / d + eps)^(-1/2),
+ *   y_j = (x_j - mean) rstd w_j + b_j.
+ * x, y : [M, d] dtype (GTR_F32, GTR_F16 or GTR_BF16); y may be x (in place)
+ * w, b : [d] float32; NULL stands for ones / zeros
+ * mean, rstd : [M] float32, the statistics for gtr_layernorm_bwd, or NULL
+ * Any width 1 <= d <= 16384 and 1 <= M < 2^31; no alignment beyond an
+ * element's. 0 <= eps < 1e30 (a row of equal values with eps 0 gives NaN).
+ */
+typedef struct {
+  const void* x;
+  const float* w;
+  const float* b;
+  void* y;
+  float* mean;
+  float* rstd;
+  gtr_dtype dtype;
+  int32_t d;
+  int64_t M;
+  float eps;
+} gtr_layernorm_fwd_args;
+
+gtr_status gtr_layernorm_fwd(const gtr_layernorm_fwd_args* args, hipStream_t stream);
+
+/*
+ * gtr_layernorm_bwd: the gradients of gtr_layernorm_fwd. With
+ * h = (x - mean) rstd and t = dy w:
+ *   dx_j = rstd (t_j - sum_i t_i / d - h_j sum_i t_i h_i / d) (+ dres_j)
+ *   dw_j = sum over the rows of dy_j h_j,  db_j = sum over the rows of dy_j
+ * dy, x, dres, dx : [M, d] dtype. dres (a gradient that reaches x another way,
+ *          a residual's) may be NULL. dx may be NULL (not wanted) or be dy, x or
+ *          dres itself.
+ * mean, rstd : [M] float32 as gtr_layernorm_fwd left them; w as there
+ * dw, db : [d] float32, or NULL where not wanted; accumulate 1: added to what
+ *          they hold
+ * workspace : for dw and db: 256-byte aligned, at least
+ *          gtr_layernorm_bwd_workspace_size(args) bytes, no initialisation
+ *          needed; calls that overlap in time must not share one.
+ * Sizes and types as for gtr_layernorm_fwd.
+ */
+typedef struct {
+  const void* dy;
+  const void* x;
+  const float* mean;
+  const float* rstd;
+  const float* w;
+  const void* dres;
+  void* dx;
+  float* dw;
+  float* db;
+  gtr_dtype dtype;
+  int32_t d;
+  int64_t M;
+  int32_t accumulate;
+  void* workspace;
+  size_t workspace_bytes;
+} gtr_layernorm_bwd_args;
+
+/* 0 if the sizes or the type are invalid; pointers are ignored (host only). */
+size_t gtr_layernorm_bwd_workspace_size(const gtr_layernorm_bwd_args* args);
+gtr_status gtr_layernorm_bwd(const gtr_layernorm_bwd_args* args, hipStream_t stream);
+
+/* The activation of the gated feed-forward: SiLU(g) = g / (1 + exp(-g)), or
+ * GELU(g) = g P(g), P the normal distribution function (the exact form). */
+typedef enum { GTR_ACT_SILU = 0, GTR_ACT_GELU = 1 } gtr_act;
+
+/*
+ * gtr_ffn_fwd: the gated feed-forward, token by token (the channel mixer of
+ * gtr_spatial_swiglu without its convolution):
+ *   g = x W_gate^T, v = x W_value^T, y = (act(g) * v) W_out^T (+ residual)
+ * x, y     : [M, d] dtype (GTR_F16 or GTR_BF16)
+ * w_gate, w_value : [hidden, d], w_out : [d, hidden] dtype (output features first)
+ * residual : [M, d] dtype or NULL; may be y (in place)
+ * gate, value : [M, hidden] dtype, receive g and v for gtr_ffn_bwd; either may
+ *            be NULL
+ * M >= 1 (one token upwards); d and hidden multiples of 8; every pointer
+ * 16-byte aligned; an output overlaps nothing else.
+ * Both projections, the activation and their product are one launch. The
+ * products accumulate in float32; act(g) v is formed in float32 and rounded to
+ * dtype for the output product (in fp16 it must stay in range).
+ * workspace : 256-byte aligned, at least gtr_ffn_fwd_workspace_size(args) bytes
+ *            (M * hidden * 2 and the partial sums of products cut along K), no
+ *            initialisation needed; calls that overlap in time must not share one.
+ */
+typedef struct {
+  const void* x;
+  const void* w_gate;
+  const void* w_value;
+  const void* w_out;
+  const void* residual;
+  void* y;
+  void* gate;
+  void* value;
+  gtr_dtype dtype;
+  gtr_act act;
+  int64_t M;
+  int32_t d, hidden;
+  void* workspace;
+  size_t workspace_bytes;
+} gtr_ffn_fwd_args;
+
+size_t gtr_ffn_fwd_workspace_size(const gtr_ffn_fwd_args* args);
+gtr_status gtr_ffn_fwd(const gtr_ffn_fwd_args* args, hipStream_t stream);
+
+/*
+ * gtr_ffn_bwd: the gradients of gtr_ffn_fwd (of its residual: dy itself).
+ *   dh = dy W_out, dg = dh v act'(g), dv = dh act(g)
+ *   dx = dg W_gate + dv W_value
+ *   dW_gate = dg^T x, dW_value = dv^T x, dW_out = dy^T (act(g) v)
+ * dy, x, dx : [M, d] dtype; weights, gate and value as in gtr_ffn_fwd
+ * dw_gate, dw_value : [hidden, d], dw_out : [d, hidden] dw_dtype (dtype or
+ *          GTR_F32). accumulate 1: added to what they hold.
+ * dx and each dw may be NULL where not wanted, not all of them.
+ * dg, dv and act(g) v are formed in float32 and rounded to dtype for the
+ * products that take them (in fp16 they must stay in range). No output may
+ * overlap anything else. Sizes, alignment and the workspace
+ * (gtr_ffn_bwd_workspace_size, about three times M * hidden * 2 bytes) as for
+ * gtr_ffn_fwd; which outputs are wanted changes its size.
+ */
+typedef struct {
+  const void* dy;
+  const void* x;
+  const void* w_gate;
+  const void* w_value;
+  const void* w_out;
+  const void* gate;
+  const void* value;
+  void* dx;
+  void* dw_gate;
+  void* dw_value;
+  void* dw_out;
+  gtr_dtype dtype;
+  gtr_dtype dw_dtype;
+  gtr_act act;
+  int32_t accumulate;
+  int64_t M;
+  int32_t d, hidden;
+  void* workspace;
+  size_t workspace_bytes;
+} gtr_ffn_bwd_args;
+
+size_t gtr_ffn_bwd_workspace_size(const gtr_ffn_bwd_args* args);
+gtr_status gtr_ffn_bwd(const gtr_ffn_bwd_args* args, hipStream_t stream);
+
+/*
  * gtr_gla_fwd_noalloc - gtr_gla_fwd for callers that cannot allocate device
  * memory (code under HIP graph capture, serving loops, harnesses that forbid
  * hipMalloc). Same arguments, results and schedules as gtr_gla_fwd, except

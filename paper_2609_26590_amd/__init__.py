@@ -15,6 +15,10 @@ Entry points (same names as the C ABI in ``include/gtr.h``):
   :func:`gtr_gla_workspace_fault`, :func:`gtr_status_string`.
 * :func:`gtr_spatial_swiglu` - the Spatial SwiGLU channel mixer (Sec. 3.1),
   with :func:`gtr_spatial_swiglu_workspace_size` in the C ABI.
+* :func:`gtr_layernorm_fwd`, :func:`gtr_layernorm_bwd` - layer normalisation
+  for training, with the gradients of input, weight and bias.
+* :func:`gtr_ffn_fwd`, :func:`gtr_ffn_bwd` - the gated feed-forward
+  ``[act(x W_gate^T) * (x W_value^T)] W_out^T`` and its gradients.
 
 :class:`Workspace` keeps a caller-owned, zero-initialised workspace buffer.
 """
@@ -32,6 +36,7 @@ LIB_PATH = os.path.join(_PKG, "libgtr.so")
 F32, F16, BF16 = 0, 1, 2
 SCANS = {"row": 0, "col": 1, "row_rev": 2, "col_rev": 3}
 PATHS = {"auto": 0, "fused": 1, "staged": 2, "inline": 3}
+ACTS = {"silu": 0, "gelu": 1}
 STATUS = {0: "GTR_OK", 1: "GTR_ERR_NULL", 2: "GTR_ERR_SHAPE", 3: "GTR_ERR_UNSUPPORTED",
           4: "GTR_ERR_ALIAS", 5: "GTR_ERR_WORKSPACE", 6: "GTR_ERR_HIP", 7: "GTR_ERR_SCRATCH"}
 
@@ -40,7 +45,9 @@ _DT_BACK = {F32: torch.float32, F16: torch.float16, BF16: torch.bfloat16}
 
 EXPORTS = ("gtr_scan_permute", "gtr_gla_workspace_size", "gtr_gla_workspace_init", "gtr_gla_fwd", "gtr_gla_fwd_noalloc",
            "gtr_gla_schedule", "gtr_gla_value_parts", "gtr_gla_segment_chunks", "gtr_gla_workspace_fault", "gtr_status_string", "gtr_spatial_swiglu_workspace_size",
-           "gtr_spatial_swiglu", "gtr_gemm", "gtr_layernorm", "gtr_heads_split", "gtr_heads_merge", "gtr_add")
+           "gtr_spatial_swiglu", "gtr_gemm", "gtr_layernorm", "gtr_heads_split", "gtr_heads_merge", "gtr_add",
+           "gtr_layernorm_fwd", "gtr_layernorm_bwd_workspace_size", "gtr_layernorm_bwd", "gtr_ffn_fwd_workspace_size",
+           "gtr_ffn_fwd", "gtr_ffn_bwd_workspace_size", "gtr_ffn_bwd")
 
 
 class GtrError(RuntimeError):
@@ -87,6 +94,47 @@ class GemmArgs(ctypes.Structure):
         ("M", ctypes.c_int64), ("N", ctypes.c_int32), ("K", ctypes.c_int32),
         ("a_tokens", ctypes.c_int64), ("c_tokens", ctypes.c_int64), ("c_heads", ctypes.c_int32),
         ("c_head_dim", ctypes.c_int32), ("row_norm_eps", ctypes.c_float), ("row_norm", ctypes.c_int32),
+    ]
+
+
+class LayernormFwdArgs(ctypes.Structure):
+    """Mirror of ``gtr_layernorm_fwd_args`` (include/gtr.h)."""
+    _fields_ = [
+        ("x", ctypes.c_void_p), ("w", ctypes.c_void_p), ("b", ctypes.c_void_p), ("y", ctypes.c_void_p),
+        ("mean", ctypes.c_void_p), ("rstd", ctypes.c_void_p), ("dtype", ctypes.c_int), ("d", ctypes.c_int32),
+        ("M", ctypes.c_int64), ("eps", ctypes.c_float),
+    ]
+
+
+class LayernormBwdArgs(ctypes.Structure):
+    """Mirror of ``gtr_layernorm_bwd_args`` (include/gtr.h)."""
+    _fields_ = [
+        ("dy", ctypes.c_void_p), ("x", ctypes.c_void_p), ("mean", ctypes.c_void_p), ("rstd", ctypes.c_void_p),
+        ("w", ctypes.c_void_p), ("dres", ctypes.c_void_p), ("dx", ctypes.c_void_p), ("dw", ctypes.c_void_p),
+        ("db", ctypes.c_void_p), ("dtype", ctypes.c_int), ("d", ctypes.c_int32), ("M", ctypes.c_int64),
+        ("accumulate", ctypes.c_int32), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class FfnFwdArgs(ctypes.Structure):
+    """Mirror of ``gtr_ffn_fwd_args`` (include/gtr.h)."""
+    _fields_ = [
+        ("x", ctypes.c_void_p), ("w_gate", ctypes.c_void_p), ("w_value", ctypes.c_void_p), ("w_out", ctypes.c_void_p),
+        ("residual", ctypes.c_void_p), ("y", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("value", ctypes.c_void_p),
+        ("dtype", ctypes.c_int), ("act", ctypes.c_int), ("M", ctypes.c_int64), ("d", ctypes.c_int32),
+        ("hidden", ctypes.c_int32), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class FfnBwdArgs(ctypes.Structure):
+    """Mirror of ``gtr_ffn_bwd_args`` (include/gtr.h)."""
+    _fields_ = [
+        ("dy", ctypes.c_void_p), ("x", ctypes.c_void_p), ("w_gate", ctypes.c_void_p), ("w_value", ctypes.c_void_p),
+        ("w_out", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("value", ctypes.c_void_p), ("dx", ctypes.c_void_p),
+        ("dw_gate", ctypes.c_void_p), ("dw_value", ctypes.c_void_p), ("dw_out", ctypes.c_void_p),
+        ("dtype", ctypes.c_int), ("dw_dtype", ctypes.c_int), ("act", ctypes.c_int), ("accumulate", ctypes.c_int32),
+        ("M", ctypes.c_int64), ("d", ctypes.c_int32), ("hidden", ctypes.c_int32), ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
     ]
 
 
@@ -138,6 +186,13 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.gtr_heads_merge.restype = ctypes.c_int
     lib.gtr_add.argtypes = [P, P, P, I64, ctypes.c_int, P]
     lib.gtr_add.restype = ctypes.c_int
+    for name, args in (("gtr_layernorm_fwd", LayernormFwdArgs), ("gtr_layernorm_bwd", LayernormBwdArgs),
+                       ("gtr_ffn_fwd", FfnFwdArgs), ("gtr_ffn_bwd", FfnBwdArgs)):
+        getattr(lib, name).argtypes = [ctypes.POINTER(args), P]
+        getattr(lib, name).restype = ctypes.c_int
+        if args is not LayernormFwdArgs:
+            getattr(lib, name + "_workspace_size").argtypes = [ctypes.POINTER(args)]
+            getattr(lib, name + "_workspace_size").restype = ctypes.c_size_t
     _lib = lib
     return lib
 
@@ -539,3 +594,191 @@ def gtr_add(a: torch.Tensor, b: torch.Tensor, *, out: Optional[torch.Tensor] = N
     if st:
         raise GtrError("gtr_add", st)
     return y
+
+
+# ---------------------------------------------------------------------------
+# training a channel mixer: gtr_layernorm_fwd / gtr_layernorm_bwd, gtr_ffn_fwd / gtr_ffn_bwd
+# ---------------------------------------------------------------------------
+def _on_stream(stream, tensors, body):
+    """body() with the tensors' device and ``stream`` (default: that device's current stream) current, so that what it
+    allocates belongs to the stream that uses it. Tensors used on a stream that is not their own are kept from being
+    handed out again before that stream is done with them."""
+    dev = tensors[0].device
+    if dev.type != "cuda":
+        raise ValueError("tensors must be on the GPU")
+    if stream is None:
+        if dev.index == torch._C._cuda_getDevice():
+            return body()
+        with torch.cuda.device(dev):
+            return body()
+    if stream.device != dev:
+        raise ValueError(f"stream is on {stream.device}, the tensors on {dev}")
+    if int(stream.cuda_stream) != torch._C._cuda_getCurrentRawStream(dev.index):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+    with torch.cuda.stream(stream):
+        return body()
+
+
+def _launch(fn: str, args, dev: torch.device, workspace: Optional["Workspace"], sized: bool = True) -> None:
+    """One call on the current stream. Without a ``workspace`` the scratch memory is the caching allocator's: it belongs
+    to this stream (and, in a graph capture, to the graph), so that no two calls in flight share it."""
+    lib = load()
+    if sized:
+        need = int(getattr(lib, fn + "_workspace_size")(ctypes.byref(args)))
+        if need:
+            if workspace is None:
+                buf = torch.empty(need, dtype=torch.uint8, device=dev)
+            else:
+                buf = workspace.get(need, torch.cuda.current_stream(dev))
+            args.workspace, args.workspace_bytes = buf.data_ptr(), buf.numel()
+    st = getattr(lib, fn)(ctypes.byref(args), torch._C._cuda_getCurrentRawStream(dev.index))
+    if st:
+        raise GtrError(fn, st)
+
+
+def gtr_layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+                      eps: float = 1e-6, out: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
+                      rstd: Optional[torch.Tensor] = None, stream=None):
+    """Layer normalisation over the last dimension of x (float32, fp16 or bf16; any width up to 16384) that keeps the
+    rows' statistics. weight, bias [d] float32. ``out`` may be x. Returns ``(y, mean, rstd)``, the statistics float32 of
+    shape x.shape[:-1]."""
+    def body():
+        d, rows = x.shape[-1], x.shape[:-1]
+        y = torch.empty_like(x) if out is None else out
+        mu = torch.empty(rows, dtype=torch.float32, device=x.device) if mean is None else mean
+        rs = torch.empty(rows, dtype=torch.float32, device=x.device) if rstd is None else rstd
+        _check("out", y, x.shape, (x.dtype,), x.device)
+        _check("weight", weight, (d,), (torch.float32,), x.device)
+        _check("bias", bias, (d,), (torch.float32,), x.device)
+        _check("mean", mu, rows, (torch.float32,), x.device)
+        _check("rstd", rs, rows, (torch.float32,), x.device)
+        a = LayernormFwdArgs(_ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mu), _ptr(rs), _DT[x.dtype], d,
+                             x.numel() // d if d else 0, float(eps))
+        _launch("gtr_layernorm_fwd", a, x.device, None, sized=False)
+        return y, mu, rs
+
+    _rows("x", x)
+    return _on_stream(stream, (x, weight, bias, out, mean, rstd), body)
+
+
+def gtr_layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                      weight: Optional[torch.Tensor] = None, *, dres: Optional[torch.Tensor] = None,
+                      want_dx: bool = True, want_dw: bool = True, out: Optional[torch.Tensor] = None,
+                      dw: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None, accumulate: bool = False,
+                      workspace: Optional["Workspace"] = None, stream=None):
+    """Gradients of :func:`gtr_layernorm_fwd`: ``(dx, dw, db)``, dx in x's type, dw and db [d] float32 summed over the
+    rows. ``dres`` (x's shape and type, a residual path's gradient) is added to dx. ``out`` (for dx) may be dy, x or
+    dres. ``accumulate``: dw and db are added to what the given ``dw`` and ``db`` hold. What is not wanted is None."""
+    def body():
+        d, dev = x.shape[-1], x.device
+        for name, t in (("dy", dy), ("dres", dres), ("out", out)):
+            _check(name, t, x.shape, (x.dtype,), dev)
+        for name, t in (("mean", mean), ("rstd", rstd)):
+            _check(name, t, x.shape[:-1], (torch.float32,), dev)
+        for name, t in (("weight", weight), ("dw", dw), ("db", db)):
+            _check(name, t, (d,), (torch.float32,), dev)
+        dx = None if not want_dx else torch.empty_like(x) if out is None else out
+        w_ = None if not want_dw else torch.empty(d, dtype=torch.float32, device=dev) if dw is None else dw
+        b_ = None if not want_dw else torch.empty(d, dtype=torch.float32, device=dev) if db is None else db
+        a = LayernormBwdArgs(_ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(dres), _ptr(dx), _ptr(w_),
+                             _ptr(b_), _DT[x.dtype], d, x.numel() // d if d else 0, int(bool(accumulate)))
+        _launch("gtr_layernorm_bwd", a, dev, workspace, sized=want_dw)
+        return dx, w_, b_
+
+    _rows("x", x)
+    if accumulate and want_dw and (dw is None or db is None):
+        raise ValueError("accumulate needs dw and db")
+    return _on_stream(stream, (x, dy, mean, rstd, weight, dres, out, dw, db), body)
+
+
+def _rows(name: str, t: torch.Tensor) -> None:
+    _dev_contig(name, t)
+    if t.dim() < 1 or t.dtype not in _DT:
+        raise ValueError(f"{name} must be [..., d] of float32, float16 or bfloat16")
+
+
+def _ffn_weights(x, w_gate, w_value, w_out) -> tuple:
+    if x.dtype == torch.float32:
+        raise ValueError("x must be float16 or bfloat16")
+    d, hidden = x.shape[-1], w_gate.shape[0]
+    _check("w_gate", w_gate, (hidden, d), (x.dtype,), x.device)
+    _check("w_value", w_value, (hidden, d), (x.dtype,), x.device)
+    _check("w_out", w_out, (d, hidden), (x.dtype,), x.device)
+    return d, hidden, x.numel() // d if d else 0
+
+
+def _act(act: str) -> int:
+    if act not in ACTS:
+        raise ValueError(f"act must be one of {sorted(ACTS)}")
+    return ACTS[act]
+
+
+def gtr_ffn_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor, w_out: torch.Tensor, *,
+                act: str = "silu", residual: Optional[torch.Tensor] = None, save: bool = False,
+                out: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                value: Optional[torch.Tensor] = None, workspace: Optional["Workspace"] = None, stream=None):
+    """Gated feed-forward y = [act(x W_gate^T) * (x W_value^T)] W_out^T (+ residual), one token upwards.
+
+    x [..., d] (fp16 or bf16), w_gate and w_value [hidden, d], w_out [d, hidden] (same type; d and hidden multiples of
+    8), ``residual`` of x's shape and type (may be ``out``). ``act``: "silu" or "gelu". Returns ``(y, gate, value)``:
+    the two projections [..., hidden] for :func:`gtr_ffn_bwd` with ``save`` (or where given), else None."""
+    def body():
+        d, hidden, M = _ffn_weights(x, w_gate, w_value, w_out)
+        dev, kept = x.device, (*x.shape[:-1], hidden)
+        y = torch.empty_like(x) if out is None else out
+        g = torch.empty(kept, dtype=x.dtype, device=dev) if gate is None and save else gate
+        v = torch.empty(kept, dtype=x.dtype, device=dev) if value is None and save else value
+        _check("out", y, x.shape, (x.dtype,), dev)
+        _check("residual", residual, x.shape, (x.dtype,), dev)
+        _check("gate", g, kept, (x.dtype,), dev)
+        _check("value", v, kept, (x.dtype,), dev)
+        a = FfnFwdArgs(_ptr(x), _ptr(w_gate), _ptr(w_value), _ptr(w_out), _ptr(residual), _ptr(y), _ptr(g), _ptr(v),
+                       _DT[x.dtype], kind, M, d, hidden)
+        _launch("gtr_ffn_fwd", a, dev, workspace)
+        return y, g, v
+
+    _rows("x", x)
+    kind = _act(act)
+    return _on_stream(stream, (x, w_gate, w_value, w_out, residual, out, gate, value), body)
+
+
+def gtr_ffn_bwd(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor, w_out: torch.Tensor,
+                gate: torch.Tensor, value: torch.Tensor, *, act: str = "silu", want_dx: bool = True,
+                want_dw: bool = True, dw_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                dw_gate: Optional[torch.Tensor] = None, dw_value: Optional[torch.Tensor] = None,
+                dw_out: Optional[torch.Tensor] = None, accumulate: bool = False,
+                workspace: Optional["Workspace"] = None, stream=None):
+    """Gradients of :func:`gtr_ffn_fwd`: ``(dx, dw_gate, dw_value, dw_out)``, from the projections it kept.
+
+    The weights' gradients are in ``dw_dtype`` (x's type, the default, or float32) or in that of the tensors given;
+    ``accumulate`` adds to what those hold. The residual's gradient is dy itself. What is not wanted is None."""
+    def body():
+        d, hidden, M = _ffn_weights(x, w_gate, w_value, w_out)
+        dev, kept = x.device, (*x.shape[:-1], hidden)
+        _check("dy", dy, x.shape, (x.dtype,), dev)
+        _check("out", out, x.shape, (x.dtype,), dev)
+        _check("gate", gate, kept, (x.dtype,), dev)
+        _check("value", value, kept, (x.dtype,), dev)
+        dx = None if not want_dx else torch.empty_like(x) if out is None else out
+        given = next((t.dtype for t in (dw_gate, dw_value, dw_out) if t is not None), x.dtype)
+        dt = given if dw_dtype is None else dw_dtype
+        if dt not in (x.dtype, torch.float32):
+            raise ValueError("dw_dtype must be x's type or float32")
+        dws = []
+        for name, t, shape in (("dw_gate", dw_gate, (hidden, d)), ("dw_value", dw_value, (hidden, d)),
+                               ("dw_out", dw_out, (d, hidden))):
+            _check(name, t, shape, (dt,), dev)
+            dws.append(None if not want_dw else torch.empty(shape, dtype=dt, device=dev) if t is None else t)
+        a = FfnBwdArgs(_ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_value), _ptr(w_out), _ptr(gate), _ptr(value), _ptr(dx),
+                       _ptr(dws[0]), _ptr(dws[1]), _ptr(dws[2]), _DT[x.dtype], _DT[dt], kind, int(bool(accumulate)), M, d,
+                       hidden)
+        _launch("gtr_ffn_bwd", a, dev, workspace)
+        return (dx, *dws)
+
+    _rows("x", x)
+    kind = _act(act)
+    if accumulate and want_dw and (dw_gate is None or dw_value is None or dw_out is None):
+        raise ValueError("accumulate needs dw_gate, dw_value and dw_out")
+    return _on_stream(stream, (x, dy, w_gate, w_value, w_out, gate, value, out, dw_gate, dw_value, dw_out), body)

@@ -1,0 +1,337 @@
+// The gated feed-forward y = [act(x W_g^T) * (x W_v^T)] W_o^T (+ residual) and its
+// backward pass, as products (ffn_gemm.h):
+//
+//   forward:   h = act(x W_g^T) * (x W_v^T)     one launch: both projections, the activation and the product
+//              y = h W_o^T (+ residual)
+//   backward:  dh = dy W_o, dg = dh v act'(g), dv = dh act(g), h = act(g) v   one launch
+//              dW_g = dg^T x, dW_v = dv^T x, dW_o = dy^T h                    one launch
+//              dx = dg W_g + dv W_v                                           one launch, one sum over both
+//
+// A product whose tiles do not fill the chip is cut along K; the partial sums are
+// added in a fixed order by a second launch.
+#include <hip/hip_runtime.h>
+
+#include "ffn_gemm.h"
+#include "gtr.h"
+#include "gtr_device.h"
+#include "gtr_internal.h"
+
+namespace gtr {
+
+constexpr int kFfnCus = 256;
+constexpr int64_t kFfnMaxWidth = 1 << 20;
+
+// Tiles a product can run in: 256 x 256 with one work-group of 8 waves per CU,
+// 128 x 128 with two of 4 waves, 64 x 64 with four of 4 waves.
+struct FfnTiles {
+  int bm, bn, per_cu;
+  float step, fixed;  // us of a 64-deep step with the CU full, of the rest of a tile
+};
+constexpr FfnTiles kFfnTiles[] = {{256, 256, 1, 1.2f, 6.f}, {128, 128, 2, 0.8f, 4.f}, {64, 64, 4, 0.55f, 3.f}};
+
+struct FfnPlan {
+  int tile, ksplit;
+  int64_t tiles;
+};
+
+// The tile size and the number of K slices with the least estimated time.
+// elems: elements of C.
+static FfnPlan ffn_plan(const FfnProd* p, int nprod, int epi) {
+  FfnPlan best = {0, 1, 0};
+  float least = 0.f;
+  for (int c = 0; c < 3; ++c) {
+    const FfnTiles& t = kFfnTiles[c];
+    const int bn = epi == kFfnGate ? t.bn / 2 : t.bn;
+    int64_t tiles = 0, elems = 0;
+    int steps = 0;
+    for (int i = 0; i < nprod; ++i) {
+      tiles += (int64_t)((p[i].M + t.bm - 1) / t.bm) * ((p[i].N + bn - 1) / bn);
+      elems += (int64_t)p[i].M * p[i].N;
+      const int s = (p[i].K + 63) / 64 * p[i].nseg;
+      steps = s > steps ? s : steps;
+    }
+    const int slots = kFfnCus * t.per_cu;
+    int most = 1;
+    if (epi == kFfnStore) most = steps / 4 < 32 ? steps / 4 : 32;
+    for (int ks = 1; ks <= (most < 1 ? 1 : most); ++ks) {
+      const int per = (steps + ks - 1) / ks;
+      if (ks > 1 && (steps + per - 1) / per != ks) continue;  // a slice would be empty
+      const int64_t rounds = (tiles * ks + slots - 1) / slots;
+      float us = (float)rounds * (per * t.step + t.fixed);
+      if (ks > 1) us += 4.f + (float)elems * (ks + 1) * 4.f / 3e6f;
+      if (least == 0.f || us < least) {
+        least = us;
+        best = {c, ks, tiles};
+      }
+    }
+  }
+  return best;
+}
+
+template <int DT, int TA, int TB, int EPI>
+static void ffn_launch_tile(const FfnGemm& g, int tile, unsigned grid, hipStream_t stream) {
+  constexpr int WM = EPI == kFfnGate ? 4 : 2, WN = EPI == kFfnGate ? 1 : 2;  // (64 x 64: both projections of a column in a wave)
+  if (tile == 0)
+    hipLaunchKernelGGL((ffn_gemm_kernel<DT, TA, TB, EPI, 256, 256, 2, 4>), dim3(grid), dim3(512), 0, stream, g);
+  else if (tile == 1)
+    hipLaunchKernelGGL((ffn_gemm_kernel<DT, TA, TB, EPI, 128, 128, 2, 2>), dim3(grid), dim3(256), 0, stream, g);
+  else
+    hipLaunchKernelGGL((ffn_gemm_kernel<DT, TA, TB, EPI, 64, 64, WM, WN>), dim3(grid), dim3(256), 0, stream, g);
+}
+
+// Fills in the tile counts and runs a launch of products. The plan's ksplit > 1 needs g.part.
+template <int TA, int TB, int EPI>
+static gtr_status ffn_run(FfnGemm& g, int dt, const FfnPlan& plan, hipStream_t stream) {
+  const FfnTiles& t = kFfnTiles[plan.tile];
+  const int bn = EPI == kFfnGate ? t.bn / 2 : t.bn;
+  int64_t off = 0;
+  for (int i = 0; i < g.nprod; ++i) {
+    g.p[i].gx = (g.p[i].M + t.bm - 1) / t.bm;
+    g.p[i].gy = (g.p[i].N + bn - 1) / bn;
+    g.p[i].part_off = off;
+    off += (int64_t)g.p[i].M * g.p[i].N;
+  }
+  g.ksplit = plan.ksplit;
+  g.part_slice = off;
+  const unsigned grid = (unsigned)(plan.tiles * plan.ksplit);
+  if (dt == GTR_F16)
+    ffn_launch_tile<GTR_F16, TA, TB, EPI>(g, plan.tile, grid, stream);
+  else
+    ffn_launch_tile<GTR_BF16, TA, TB, EPI>(g, plan.tile, grid, stream);
+  if (hipGetLastError() != hipSuccess) return GTR_ERR_HIP;
+  if (plan.ksplit > 1) {
+    const unsigned blocks = (unsigned)((off / 8 + 255) / 256);
+    if (dt == GTR_F16)
+      hipLaunchKernelGGL(ffn_reduce_kernel<GTR_F16>, dim3(blocks), dim3(256), 0, stream, g);
+    else
+      hipLaunchKernelGGL(ffn_reduce_kernel<GTR_BF16>, dim3(blocks), dim3(256), 0, stream, g);
+    if (hipGetLastError() != hipSuccess) return GTR_ERR_HIP;
+  }
+  return GTR_OK;
+}
+
+static FfnProd ffn_prod(const void* a, const void* b, void* c, int64_t lda, int64_t ldb, int64_t M, int64_t N, int64_t K) {
+  FfnProd p = {};
+  p.a[0] = p.a[1] = static_cast<const char*>(a);
+  p.b[0] = p.b[1] = static_cast<const char*>(b);
+  p.c = static_cast<char*>(c);
+  p.lda = lda;
+  p.ldb = ldb;
+  p.ldc = N;
+  p.M = (int)M;
+  p.N = (int)N;
+  p.K = (int)K;
+  p.nseg = 1;
+  return p;
+}
+
+struct FfnRange {
+  const void* p;
+  size_t n;
+};
+static bool ffn_overlap(const FfnRange& a, const FfnRange& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && x < y + b.n && y < x + a.n;
+}
+static bool ffn_misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+static size_t ffn_align(size_t n) { return (n + 255) & ~(size_t)255; }
+
+static gtr_status ffn_sizes(int64_t M, int32_t d, int32_t hidden, int dt, int act) {
+  if (M <= 0 || d <= 0 || hidden <= 0) return GTR_ERR_SHAPE;
+  if (d % 8 || hidden % 8 || d > kFfnMaxWidth || hidden > kFfnMaxWidth || (dt != GTR_F16 && dt != GTR_BF16) ||
+      (act != GTR_ACT_SILU && act != GTR_ACT_GELU))
+    return GTR_ERR_UNSUPPORTED;
+  // rows and work-groups count in 32 bits
+  const int64_t w = d > hidden ? d : hidden;
+  if (M > ((int64_t)1 << 30) || M * w > ((int64_t)1 << 38)) return GTR_ERR_SHAPE;
+  return GTR_OK;
+}
+
+// ---------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------
+struct FfnFwdPlan {
+  FfnProd up, down;
+  FfnPlan pu, pd;
+  size_t h_bytes, total;
+};
+
+static void ffn_fwd_plan(const gtr_ffn_fwd_args* a, FfnFwdPlan* f) {
+  f->up = ffn_prod(a->x, a->w_gate, nullptr, a->d, a->d, a->M, a->hidden, a->d);
+  f->up.b[1] = static_cast<const char*>(a->w_value);
+  f->down = ffn_prod(nullptr, a->w_out, a->y, a->hidden, a->hidden, a->M, a->d, a->hidden);
+  f->down.res = static_cast<const char*>(a->residual);
+  f->pu = ffn_plan(&f->up, 1, kFfnGate);
+  f->pd = ffn_plan(&f->down, 1, kFfnStore);
+  f->h_bytes = ffn_align((size_t)a->M * a->hidden * 2);
+  f->total = f->h_bytes + (f->pd.ksplit > 1 ? ffn_align((size_t)f->pd.ksplit * a->M * a->d * 4) : 0);
+}
+
+static gtr_status ffn_fwd_check(const gtr_ffn_fwd_args* a, const FfnFwdPlan& f) {
+  if (!a->x || !a->w_gate || !a->w_value || !a->w_out || !a->y) return GTR_ERR_NULL;
+  for (const void* p : {a->x, a->w_gate, a->w_value, a->w_out, a->residual, (const void*)a->y, (const void*)a->gate,
+                        (const void*)a->value})
+    if (ffn_misaligned(p)) return GTR_ERR_UNSUPPORTED;
+  if (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 255u) || a->workspace_bytes < f.total)
+    return GTR_ERR_WORKSPACE;
+  const size_t rows = (size_t)a->M * a->d * 2, kept = (size_t)a->M * a->hidden * 2, w = (size_t)a->d * a->hidden * 2;
+  const FfnRange ins[] = {{a->x, rows}, {a->w_gate, w}, {a->w_value, w}, {a->w_out, w}, {a->residual, rows}};
+  const FfnRange outs[] = {{a->y, rows}, {a->gate, kept}, {a->value, kept}, {a->workspace, f.total}};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < 5; ++j)
+      if (ffn_overlap(outs[i], ins[j]) && !(i == 0 && j == 4 && a->y == a->residual)) return GTR_ERR_ALIAS;
+    for (int j = 0; j < i; ++j)
+      if (ffn_overlap(outs[i], outs[j])) return GTR_ERR_ALIAS;
+  }
+  return GTR_OK;
+}
+
+// ---------------------------------------------------------------------------
+// backward
+// ---------------------------------------------------------------------------
+struct FfnBwdPlan {
+  FfnProd dh, dx, dw[3];
+  int ndw;
+  FfnPlan ph, px, pw;
+  size_t kept, dg_off, dv_off, h_off, part_off, total;
+};
+
+static void ffn_bwd_plan(const gtr_ffn_bwd_args* a, FfnBwdPlan* f) {
+  const int64_t M = a->M, d = a->d, h = a->hidden;
+  f->kept = ffn_align((size_t)M * h * 2);
+  f->dg_off = 0;
+  f->dv_off = f->kept;
+  f->h_off = 2 * f->kept;
+  f->part_off = (a->dw_out ? 3 : 2) * f->kept;
+  char* ws = static_cast<char*>(a->workspace);
+  char *dg = ws + f->dg_off, *dv = ws + f->dv_off, *hh = ws + f->h_off;
+  f->dh = ffn_prod(a->dy, a->w_out, a->dw_out ? hh : nullptr, d, h, M, h, d);
+  f->dx = ffn_prod(dg, a->w_gate, a->dx, h, d, M, d, h);
+  f->dx.a[1] = dv;
+  f->dx.b[1] = static_cast<const char*>(a->w_value);
+  f->dx.nseg = 2;
+  f->ndw = 0;
+  if (a->dw_gate) f->dw[f->ndw++] = ffn_prod(dg, a->x, a->dw_gate, h, d, h, d, M);
+  if (a->dw_value) f->dw[f->ndw++] = ffn_prod(dv, a->x, a->dw_value, h, d, h, d, M);
+  if (a->dw_out) f->dw[f->ndw++] = ffn_prod(a->dy, hh, a->dw_out, d, h, d, h, M);
+  for (int i = 0; i < f->ndw; ++i) f->dw[i].res = a->accumulate ? f->dw[i].c : nullptr;
+  f->ph = ffn_plan(&f->dh, 1, kFfnGateGrad);
+  f->px = ffn_plan(&f->dx, 1, kFfnStore);
+  f->pw = ffn_plan(f->dw, f->ndw, kFfnStore);
+  size_t part = 0;
+  if (a->dx && f->px.ksplit > 1) part = (size_t)f->px.ksplit * M * d * 4;
+  if (f->ndw && f->pw.ksplit > 1) {
+    const size_t n = (size_t)f->pw.ksplit * f->ndw * d * h * 4;
+    part = n > part ? n : part;
+  }
+  f->total = f->part_off + ffn_align(part);
+}
+
+static gtr_status ffn_bwd_check(const gtr_ffn_bwd_args* a, const FfnBwdPlan& f) {
+  if (!a->dy || !a->x || !a->w_gate || !a->w_value || !a->w_out || !a->gate || !a->value ||
+      (!a->dx && !a->dw_gate && !a->dw_value && !a->dw_out))
+    return GTR_ERR_NULL;
+  for (const void* p : {a->dy, a->x, a->w_gate, a->w_value, a->w_out, a->gate, a->value, (const void*)a->dx,
+                        (const void*)a->dw_gate, (const void*)a->dw_value, (const void*)a->dw_out})
+    if (ffn_misaligned(p)) return GTR_ERR_UNSUPPORTED;
+  if (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 255u) || a->workspace_bytes < f.total)
+    return GTR_ERR_WORKSPACE;
+  const size_t rows = (size_t)a->M * a->d * 2, kept = (size_t)a->M * a->hidden * 2, w = (size_t)a->d * a->hidden * 2;
+  const size_t dw = (size_t)a->d * a->hidden * dtype_size(a->dw_dtype);
+  const FfnRange ins[] = {{a->dy, rows}, {a->x, rows}, {a->w_gate, w}, {a->w_value, w}, {a->w_out, w}, {a->gate, kept}, {a->value, kept}};
+  const FfnRange outs[] = {{a->dx, rows}, {a->dw_gate, dw}, {a->dw_value, dw}, {a->dw_out, dw}, {a->workspace, f.total}};
+  for (int i = 0; i < 5; ++i) {
+    for (int j = 0; j < 7; ++j)
+      if (ffn_overlap(outs[i], ins[j])) return GTR_ERR_ALIAS;
+    for (int j = 0; j < i; ++j)
+      if (ffn_overlap(outs[i], outs[j])) return GTR_ERR_ALIAS;
+  }
+  return GTR_OK;
+}
+
+static gtr_status ffn_bwd_sizes(const gtr_ffn_bwd_args* a) {
+  if (!a) return GTR_ERR_NULL;
+  const gtr_status st = ffn_sizes(a->M, a->d, a->hidden, a->dtype, a->act);
+  if (st != GTR_OK) return st;
+  if (a->dw_dtype != a->dtype && a->dw_dtype != GTR_F32) return GTR_ERR_UNSUPPORTED;
+  return GTR_OK;
+}
+
+}  // namespace gtr
+
+using namespace gtr;
+
+extern "C" size_t gtr_ffn_fwd_workspace_size(const gtr_ffn_fwd_args* a) {
+  if (!a || ffn_sizes(a->M, a->d, a->hidden, a->dtype, a->act) != GTR_OK) return 0;
+  FfnFwdPlan f;
+  ffn_fwd_plan(a, &f);
+  return f.total;
+}
+
+extern "C" gtr_status gtr_ffn_fwd(const gtr_ffn_fwd_args* a, hipStream_t stream) {
+  if (!a) return GTR_ERR_NULL;
+  gtr_status st = ffn_sizes(a->M, a->d, a->hidden, a->dtype, a->act);
+  if (st != GTR_OK) return st;
+  FfnFwdPlan f;
+  ffn_fwd_plan(a, &f);
+  st = ffn_fwd_check(a, f);
+  if (st != GTR_OK) return st;
+  char* h = static_cast<char*>(a->workspace);
+  FfnGemm g = {};
+  g.nprod = 1;
+  g.cdt = a->dtype;
+  g.act = a->act;
+  g.p[0] = f.up;
+  g.p[0].c = h;
+  g.gate = static_cast<char*>(a->gate);
+  g.value = static_cast<char*>(a->value);
+  st = ffn_run<0, 0, kFfnGate>(g, a->dtype, f.pu, stream);
+  if (st != GTR_OK) return st;
+  g.p[0] = f.down;
+  g.p[0].a[0] = g.p[0].a[1] = h;
+  g.part = reinterpret_cast<float*>(h + f.h_bytes);
+  return ffn_run<0, 0, kFfnStore>(g, a->dtype, f.pd, stream);
+}
+
+extern "C" size_t gtr_ffn_bwd_workspace_size(const gtr_ffn_bwd_args* a) {
+  if (ffn_bwd_sizes(a) != GTR_OK) return 0;
+  FfnBwdPlan f;
+  ffn_bwd_plan(a, &f);
+  return f.total;
+}
+
+extern "C" gtr_status gtr_ffn_bwd(const gtr_ffn_bwd_args* a, hipStream_t stream) {
+  gtr_status st = ffn_bwd_sizes(a);
+  if (st != GTR_OK) return st;
+  FfnBwdPlan f;
+  ffn_bwd_plan(a, &f);
+  st = ffn_bwd_check(a, f);
+  if (st != GTR_OK) return st;
+  char* ws = static_cast<char*>(a->workspace);
+  FfnGemm g = {};
+  g.nprod = 1;
+  g.cdt = a->dtype;
+  g.act = a->act;
+  g.p[0] = f.dh;
+  g.gate = const_cast<char*>(static_cast<const char*>(a->gate));
+  g.value = const_cast<char*>(static_cast<const char*>(a->value));
+  g.dgate = ws + f.dg_off;
+  g.dvalue = ws + f.dv_off;
+  g.part = reinterpret_cast<float*>(ws + f.part_off);
+  st = ffn_run<0, 1, kFfnGateGrad>(g, a->dtype, f.ph, stream);
+  if (st != GTR_OK) return st;
+  if (f.ndw) {
+    for (int i = 0; i < f.ndw; ++i) g.p[i] = f.dw[i];
+    g.nprod = f.ndw;
+    g.cdt = a->dw_dtype;
+    st = ffn_run<1, 1, kFfnStore>(g, a->dtype, f.pw, stream);
+    if (st != GTR_OK) return st;
+  }
+  if (a->dx) {
+    g.p[0] = f.dx;
+    g.nprod = 1;
+    g.cdt = a->dtype;
+    st = ffn_run<0, 1, kFfnStore>(g, a->dtype, f.px, stream);
+  }
+  return st;
+}
