@@ -102,8 +102,9 @@ __device__ __forceinline__ i4 ffn_rsrc(const char* at, int64_t left) {
 
 // A tile of BT rows (or columns) by 64 K elements in LDS.
 //
-// Rows along K (T = 0): kPitch64 rows of 128 bytes with 16-byte pieces swizzled by
-// kSwz64 (gemm.h).
+// Rows along K (T = 0): rows of 128 bytes; piece c (16 bytes) of row r sits at c ^ (r
+// / 2 mod 8), so that the 16 rows of an operand read take 16 different places
+// modulo 256 bytes.
 //
 // Columns along K (T = 1): 64 rows, one per K element, of BT columns, read with
 // the transposing read ds_read_b64_tr_b16 in blocks of 4 K rows x 16 columns. One
@@ -118,6 +119,7 @@ struct FfnTile {
   static constexpr int RPC = 512 / BT;   // T = 1: K rows per transfer
   static_assert(BT % (8 * NW) == 0, "the tile splits evenly over the waves");
 
+  static __device__ __forceinline__ int row_swz(int r) { return (r >> 1) & 7; }
   static __device__ __forceinline__ int unit_swz(int k) {
     const int m = k & 3, q = (k >> 3) & 3;
     return BT == 256 ? m | q << 2 : BT == 128 ? m >> 1 | q << 1 : q;
@@ -126,21 +128,21 @@ struct FfnTile {
   static __device__ __forceinline__ unsigned voff(int c, int lane, int64_t ld) {
     if constexpr (T == 0) {
       const int row = 8 * c + (lane >> 3);
-      return (unsigned)(row * (int)ld * 2) + 16u * ((lane & 7) ^ kSwz64(row));
+      return (unsigned)(row * (int)ld * 2) + 16u * ((lane & 7) ^ row_swz(row));
     } else {
       const int k = RPC * c + lane / (BT / 8), p = lane % (BT / 8);
       return (unsigned)(k * (int)ld * 2) + 32u * ((p >> 1) ^ unit_swz(k)) + 16u * (p & 1);
     }
   }
   static __device__ __forceinline__ int piece_k(int c, int lane) {  // T = 0: K elements before this lane's piece
-    return 8 * ((lane & 7) ^ kSwz64(8 * c + (lane >> 3)));
+    return 8 * ((lane & 7) ^ row_swz(8 * c + (lane >> 3)));
   }
   // the MFMA operand of rows (columns) r0 .. r0 + 15, K elements 32 h .. 32 h + 31
   static __device__ __forceinline__ w4 frag(const char* s, int r0, int h, int lane) {
     const int r16 = lane & 15, kq = lane >> 4;
     if constexpr (T == 0) {
       const int row = r0 + r16;
-      return *reinterpret_cast<const w4*>(s + row * 128 + (((4 * h + kq) ^ kSwz64(r16)) << 4));
+      return *reinterpret_cast<const w4*>(s + row * 128 + (((4 * h + kq) ^ row_swz(r16)) << 4));
     } else {
       const int k = 8 * kq + (r16 >> 2);  // (of this half; its swizzle is that of k + 4 and k + 32)
       const char* p = s + (32 * h + k) * (BT * 2) + (((r0 >> 4) ^ unit_swz(k)) << 5) + 8 * (r16 & 3);
@@ -200,28 +202,34 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   int is = s0 % sps, iseg = s0 / sps;  // the next transfer's step and segment
   int64_t ao = a0 + is * astep, bo = b0 + is * bstep;
   const unsigned lbase = lds_addr(ring) + wave * 1024;
-  auto issue = [&](int buf) {
-    const unsigned l = lbase + buf * STAGE;
-    const i4 ra = ffn_rsrc(p.a[iseg] + ao, abytes - ao), rb = ffn_rsrc(p.b[DUAL ? 0 : iseg] + bo, bbytes - bo);
-    const i4 rv = DUAL ? ffn_rsrc(p.b[1] + bo, bbytes - bo) : rb;
-    const int kleft = K - 64 * is;
-    if ((!TA || !TB) && kleft < 64) {  // the last step of a segment: a row's next elements are another row's
-#pragma unroll
-      for (int q = 0; q < LA::P; ++q)
-        dma16_buf(ra, !TA && LA::piece_k(wave + NW * q, lane) >= kleft ? kFfnOob : va[q], l + NW * 1024 * q);
-#pragma unroll
-      for (int q = 0; q < LB::P; ++q)
-        dma16_buf(DUAL && q >= LB::P / 2 ? rv : rb, !TB && LB::piece_k(wave + NW * q, lane) >= kleft ? kFfnOob : vb[q],
-                  l + LA::kBytes + NW * 1024 * q);
-    } else {
-#pragma unroll
-      for (int q = 0; q < LA::P; ++q) dma16_buf(ra, va[q], l + NW * 1024 * q);
-#pragma unroll
-      for (int q = 0; q < LB::P; ++q) dma16_buf(DUAL && q >= LB::P / 2 ? rv : rb, vb[q], l + LA::kBytes + NW * 1024 * q);
-    }
+  i4 ra, rb, rv;
+  int kleft = 64, issued = 0;
+  // The next step's operands: their descriptors, and how many K elements it has.
+  // Past the last step the descriptors are empty: the transfers write zeros that no
+  // product reads, so that the loop has one form.
+  auto next = [&]() {
+    const bool more = issued++ < steps;
+    const int sg = more ? iseg : 0;
+    ra = ffn_rsrc(p.a[sg] + ao, more ? abytes - ao : 0);
+    rb = ffn_rsrc(p.b[DUAL ? 0 : sg] + bo, more ? bbytes - bo : 0);
+    if (DUAL) rv = ffn_rsrc(p.b[1] + bo, more ? bbytes - bo : 0);
+    kleft = K - 64 * is;
     ao += astep;
     bo += bstep;
     if (++is == sps) is = 0, ++iseg, ao = a0, bo = b0;
+  };
+  // This wave's transfer q of that step to a stage. In the last step of a segment a
+  // row's next elements are another row's: out of range instead. (A wave's transfers
+  // c are all even or all odd, so a lane's piece is at the same K element in each.)
+  const int pk = LA::piece_k(wave, lane);
+  auto transfer = [&](int buf, int q) {
+    const unsigned l = lbase + buf * STAGE;
+    if (q < LA::P) {
+      dma16_buf(ra, !TA && pk >= kleft ? kFfnOob : va[q], l + NW * 1024 * q);
+    } else {
+      const int u = q - LA::P;
+      dma16_buf(DUAL && u >= LB::P / 2 ? rv : rb, !TB && pk >= kleft ? kFfnOob : vb[u], l + LA::kBytes + NW * 1024 * u);
+    }
   };
 
   const int wm = wmi * (BM / WM);
@@ -230,46 +238,58 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   for (int i = 0; i < TI; ++i)
 #pragma unroll
     for (int j = 0; j < TJ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-  auto read = [&](int buf, int h, w4(&fa)[TI], w4(&fb)[TJ]) {
+  // operand q of half a step: B's column tiles, then A's row tiles
+  auto read = [&](int buf, int h, int q, w4(&fa)[TI], w4(&fb)[TJ]) {
     const char* s = ring + buf * STAGE;
-#pragma unroll
-    for (int j = 0; j < TJ; ++j) {
-      const int r0 = DUAL ? (j >> 1) * BC + wni * (BC / WN) + 16 * (j & 1) : wni * (BN / WN) + 16 * j;
-      fb[j] = LB::frag(s + LA::kBytes, r0, h, lane);
+    if (q < TJ) {
+      const int r0 = DUAL ? (q >> 1) * BC + wni * (BC / WN) + 16 * (q & 1) : wni * (BN / WN) + 16 * q;
+      fb[q] = LB::frag(s + LA::kBytes, r0, h, lane);
+    } else {
+      fa[q - TJ] = LA::frag(s, wm + 16 * (q - TJ), h, lane);
     }
-#pragma unroll
-    for (int i = 0; i < TI; ++i) fa[i] = LA::frag(s, wm + 16 * i, h, lane);
   };
-  auto mma = [&](const w4(&fa)[TI], const w4(&fb)[TJ]) {
+  // Half a step's products, a row of tiles at a time, and between the rows the reads
+  // of the next half's operands and (D) the transfers of a later step: the matrix
+  // cores work while the wave issues them.
+  constexpr int PL = LA::P + LB::P;
+  auto half = [&](const w4(&fa)[TI], const w4(&fb)[TJ], int rbuf, int rh, w4(&na)[TI], w4(&nb)[TJ], int dbuf) {
+    constexpr int RR = TI > 1 ? (TI + TJ + TI - 2) / (TI - 1) : TI + TJ;  // reads per row, all of them before the last row
+    constexpr int DR = (PL + TI - 1) / TI;
+    static_assert(RR * TI >= TI + TJ && DR * TI >= PL, "every read and every transfer has its row");
 #pragma unroll
-    for (int i = 0; i < TI; ++i)
+    for (int i = 0; i < TI; ++i) {
 #pragma unroll
       for (int j = 0; j < TJ; ++j) acc[i][j] = mfma(Op::get(fb[j]), Op::get(fa[i]), acc[i][j]);  // C^T tiles
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int q = i * RR; q < (i + 1) * RR && q < TI + TJ; ++q) read(rbuf, rh, q, na, nb);
+      if (dbuf >= 0) {
+#pragma unroll
+        for (int q = i * DR; q < (i + 1) * DR && q < PL; ++q) transfer(dbuf, q);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
   w4 fa0[TI], fb0[TJ], fa1[TI], fb1[TJ];
-  if (steps > 0) {
-    issue(0);
-    if (steps > 1) {
-      issue(1);
-      ring_wait<LA::P + LB::P>();
-    } else {
-      ring_wait<0>();
-    }
-    read(0, 0, fa0, fb0);
-  }
+  next();
+#pragma unroll
+  for (int q = 0; q < PL; ++q) transfer(0, q);
+  next();
+#pragma unroll
+  for (int q = 0; q < PL; ++q) transfer(1, q);
+  ring_wait<PL>();
+#pragma unroll
+  for (int q = 0; q < TI + TJ; ++q) read(0, 0, q, fa0, fb0);
   for (int k = 0; k < steps; ++k) {
-    read(k & 1, 1, fa1, fb1);
-    mma(fa0, fb0);
-    if (k + 1 < steps) {
-      // every wave has read this stage, and its transfers into the next one have landed
-      __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0), known to the compiler: no waits for these reads below
-      ring_wait<0>();
-      if (k + 2 < steps) issue(k & 1);
-      read((k + 1) & 1, 0, fa0, fb0);
-    }
-    mma(fa1, fb1);
+    half(fa0, fb0, k & 1, 1, fa1, fb1, -1);
+    // every wave has read this stage, and its transfers into the next one have landed
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0), known to the compiler: no waits for these reads below
+    ring_wait<0>();
+    next();
+    half(fa1, fb1, (k + 1) & 1, 0, fa0, fb0, k & 1);
   }
+  ring_wait<0>();  // no transfer is in flight when the work-group ends
 
   // Lane (r16, kq) holds C[row 16 i + r16][columns 16 j + 4 kq .. + 3] of its
   // wave's block. Two column tiles exchange lane rows, so that it holds 8
