@@ -92,12 +92,11 @@ __device__ __forceinline__ void swap_rows(float& a, float& b) {
 }
 constexpr unsigned kFfnOob = 0x80000000u;  // a byte offset past every descriptor's range
 
-// What is left of a matrix from `at` on, as a buffer descriptor.
-__device__ __forceinline__ i4 ffn_rsrc(const char* at, int64_t left) {
+// n bytes from `at` on as a buffer descriptor.
+__device__ __forceinline__ i4 ffn_rsrc(const char* at, int n) {
   const uint64_t p = reinterpret_cast<uint64_t>(at);
-  const int64_t n = left < 0 ? 0 : left > 0x7fffffff ? 0x7fffffff : left;
   return i4{__builtin_amdgcn_readfirstlane((int)(uint32_t)p), __builtin_amdgcn_readfirstlane((int)((uint32_t)(p >> 32) & 0xffffu)),
-            __builtin_amdgcn_readfirstlane((int)n), 0x00020000};
+            __builtin_amdgcn_readfirstlane(n), 0x00020000};
 }
 
 // A tile of BT rows (or columns) by 64 K elements in LDS.
@@ -196,27 +195,36 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
 #pragma unroll
   for (int q = 0; q < LB::P; ++q) vb[q] = LB::voff((wave + NW * q) % (DUAL ? BC / 8 : BN), lane, p.ldb);
 
-  const int64_t abytes = (TA ? (int64_t)K * p.lda : (int64_t)p.M * p.lda) * 2, bbytes = (TB ? (int64_t)K * p.ldb : (int64_t)p.N * p.ldb) * 2;
+  // Descriptors of a step's operands: they end where the tile's rows do (rows along
+  // K) or with the step's last K row (columns along K; past the last column of a
+  // row lies the next one, whose elements only columns that are not stored get).
   const int64_t astep = TA ? 128 * p.lda : 128, bstep = TB ? 128 * p.ldb : 128;
   const int64_t a0 = TA ? 2 * (int64_t)mb : 2 * (int64_t)mb * p.lda, b0 = TB ? 2 * (int64_t)nb : 2 * (int64_t)nb * p.ldb;
-  int is = s0 % sps, iseg = s0 / sps;  // the next transfer's step and segment
-  int64_t ao = a0 + is * astep, bo = b0 + is * bstep;
+  const int ktail = K - 64 * (sps - 1);  // K elements of a segment's last step
+  const int aend = TA ? 128 * (int)p.lda - 2 * mb : min(BM, p.M - mb) * (int)p.lda * 2;
+  const int bend = TB ? 128 * (int)p.ldb - 2 * nb : min(BC, p.N - nb) * (int)p.ldb * 2;
+  const int atail = TA ? ktail * 2 * (int)p.lda - 2 * mb : aend, btail = TB ? ktail * 2 * (int)p.ldb - 2 * nb : bend;
+  const int sg = s0 >= sps ? 1 : 0;
+  int is = s0 - sg * sps, left = steps;  // the next transfer's step in its segment; steps not transferred yet
+  const char *pa = p.a[sg] + a0 + is * astep, *pb = p.b[DUAL ? 0 : sg] + b0 + is * bstep;
+  const char *pa1 = p.a[1] + a0, *pb1 = p.b[1] + b0;  // the second segment (DUAL: pb1 - b's start is the second weight)
+  const int64_t pv = pb1 - (p.b[0] + b0);
   const unsigned lbase = lds_addr(ring) + wave * 1024;
   i4 ra, rb, rv;
-  int kleft = 64, issued = 0;
+  int kleft = 64;
   // The next step's operands: their descriptors, and how many K elements it has.
   // Past the last step the descriptors are empty: the transfers write zeros that no
   // product reads, so that the loop has one form.
   auto next = [&]() {
-    const bool more = issued++ < steps;
-    const int sg = more ? iseg : 0;
-    ra = ffn_rsrc(p.a[sg] + ao, more ? abytes - ao : 0);
-    rb = ffn_rsrc(p.b[DUAL ? 0 : sg] + bo, more ? bbytes - bo : 0);
-    if (DUAL) rv = ffn_rsrc(p.b[1] + bo, more ? bbytes - bo : 0);
-    kleft = K - 64 * is;
-    ao += astep;
-    bo += bstep;
-    if (++is == sps) is = 0, ++iseg, ao = a0, bo = b0;
+    const bool last = is == sps - 1, more = left > 0;
+    --left;
+    kleft = last ? ktail : 64;
+    ra = ffn_rsrc(pa, more ? last ? atail : aend : 0);
+    rb = ffn_rsrc(pb, more ? last ? btail : bend : 0);
+    if (DUAL) rv = ffn_rsrc(pb + pv, more ? bend : 0);
+    is = last ? 0 : is + 1;
+    pa = last ? pa1 : pa + astep;
+    pb = last ? pb1 : pb + bstep;
   };
   // This wave's transfer q of that step to a stage. In the last step of a segment a
   // row's next elements are another row's: out of range instead. (A wave's transfers
@@ -261,6 +269,7 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
 #pragma unroll
       for (int j = 0; j < TJ; ++j) acc[i][j] = mfma(Op::get(fb[j]), Op::get(fa[i]), acc[i][j]);  // C^T tiles
       __builtin_amdgcn_sched_barrier(0);
+      if (dbuf < 0 && i == TI / 2) next();
 #pragma unroll
       for (int q = i * RR; q < (i + 1) * RR && q < TI + TJ; ++q) read(rbuf, rh, q, na, nb);
       if (dbuf >= 0) {
@@ -286,7 +295,6 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
     // every wave has read this stage, and its transfers into the next one have landed
     __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0), known to the compiler: no waits for these reads below
     ring_wait<0>();
-    next();
     half(fa1, fb1, (k + 1) & 1, 0, fa0, fb0, k & 1);
   }
   ring_wait<0>();  // no transfer is in flight when the work-group ends
