@@ -70,13 +70,12 @@ static FfnPlan ffn_plan(const FfnProd* p, int nprod, int epi) {
 
 template <int DT, int TA, int TB, int EPI>
 static void ffn_launch_tile(const FfnGemm& g, int tile, unsigned grid, hipStream_t stream) {
-  constexpr int WM = EPI == kFfnGate ? 4 : 2, WN = EPI == kFfnGate ? 1 : 2;  // (64 x 64: both projections of a column in a wave)
   if (tile == 0)
     hipLaunchKernelGGL((ffn_gemm_kernel<DT, TA, TB, EPI, 256, 256, 2, 4>), dim3(grid), dim3(512), 0, stream, g);
   else if (tile == 1)
     hipLaunchKernelGGL((ffn_gemm_kernel<DT, TA, TB, EPI, 128, 128, 2, 2>), dim3(grid), dim3(256), 0, stream, g);
   else
-    hipLaunchKernelGGL((ffn_gemm_kernel<DT, TA, TB, EPI, 64, 64, WM, WN>), dim3(grid), dim3(256), 0, stream, g);
+    hipLaunchKernelGGL((ffn_gemm_kernel<DT, TA, TB, EPI, 64, 64, 2, 2>), dim3(grid), dim3(256), 0, stream, g);
 }
 
 // Fills in the tile counts and runs a launch of products. The plan's ksplit > 1 needs g.part.

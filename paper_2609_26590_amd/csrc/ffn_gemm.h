@@ -42,25 +42,34 @@ struct FfnGemm {
 // What an epilogue does with the product.
 enum { kFfnStore = 0, kFfnGate = 1, kFfnGateGrad = 2 };
 
-// 8 consecutive elements of type dt (16-bit or float32) at p.
-template <int DT>
-__device__ __forceinline__ void ffn_load8(const char* p, float (&x)[8]) {
-  load8(p, DT, 0, x);
+// N (4 or 8) consecutive elements of type DT at p (aligned to all of them, float32 to
+// four).
+template <int DT, int N>
+__device__ __forceinline__ void ffn_load(const char* p, float (&x)[N]) {
+  if constexpr (N == 8)
+    load8(p, DT, 0, x);
+  else
+    load4(p, DT, 0, x);
 }
-template <int DT>
-__device__ __forceinline__ w4 ffn_pack8(const float (&x)[8]) {
-  w4 r;
+template <int DT, int N>
+__device__ __forceinline__ void ffn_store(char* p, const float (&x)[N]) {
+  if constexpr (DT == GTR_F32) {
+    store_n<N>(p, GTR_F32, 0, x);
+  } else {
+    typedef unsigned v __attribute__((ext_vector_type(N / 2)));
+    v r;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if constexpr (DT == GTR_F16) {
-      r[e] = __builtin_bit_cast(unsigned short, (_Float16)x[2 * e]) |
-             (unsigned)__builtin_bit_cast(unsigned short, (_Float16)x[2 * e + 1]) << 16;
-    } else {
-      r[e] = __builtin_bit_cast(unsigned short, (__bf16)x[2 * e]) |
-             (unsigned)__builtin_bit_cast(unsigned short, (__bf16)x[2 * e + 1]) << 16;
+    for (int e = 0; e < N / 2; ++e) {
+      if constexpr (DT == GTR_F16) {
+        r[e] = __builtin_bit_cast(unsigned short, (_Float16)x[2 * e]) |
+               (unsigned)__builtin_bit_cast(unsigned short, (_Float16)x[2 * e + 1]) << 16;
+      } else {
+        r[e] = __builtin_bit_cast(unsigned short, (__bf16)x[2 * e]) |
+               (unsigned)__builtin_bit_cast(unsigned short, (__bf16)x[2 * e + 1]) << 16;
+      }
     }
+    *reinterpret_cast<v*>(p) = r;
   }
-  return r;
 }
 
 // act(g) and its derivative. SiLU: g s(g), s(g) (1 + g (1 - s(g))), s the logistic
@@ -121,7 +130,7 @@ struct FfnTile {
   static __device__ __forceinline__ int row_swz(int r) { return (r >> 1) & 7; }
   static __device__ __forceinline__ int unit_swz(int k) {
     const int m = k & 3, q = (k >> 3) & 3;
-    return BT == 256 ? m | q << 2 : BT == 128 ? m >> 1 | q << 1 : q;
+    return BT == 128 ? m >> 1 | q << 1 : BT == 64 ? q : q & 1;  // (32: two of the 16 share a place)
   }
   // byte offset of this lane's piece of transfer c (0 .. BT / 8 - 1), and its first K element
   static __device__ __forceinline__ unsigned voff(int c, int lane, int64_t ld) {
@@ -155,17 +164,30 @@ struct FfnTile {
 
 // C = A B. TA = 0: A is [M][K], TA = 1: A is [K][M]; TB = 0: B is [N][K], TB = 1:
 // B is [K][N]. WM x WN waves.
+//
+// A work-group's tile is cut in halves along both sides: A0 and A1 (BM / 2 rows
+// each), B0 and B1 (BN / 2 columns each; for the gated epilogue B0 is the gate's
+// weight and B1 the value's, so that a lane ends with both projections of the same
+// columns). A wave computes TI / 2 x TJ / 2 MFMA tiles of each of the four
+// quadrants. Two LDS stages of 64 K elements hold the four halves. A step runs in
+// two parts,
+//   A0 B0, A0 B1   (meanwhile: reads B1 and A1 of this step from LDS)
+//   A1 B0, A1 B1   (meanwhile: reads A0 and B0 of the next step)
+// with one barrier after each, so every half is free for the step after next a
+// whole step before it is read again: its transfer has three parts' time to
+// arrive.
 template <int DT, int TA, int TB, int EPI, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2))) ffn_gemm_kernel(FfnGemm g) {
   typedef Operand<DT, DT> Op;
   constexpr int NW = WM * WN;
-  constexpr int TI = BM / (16 * WM), TJ = BN / (16 * WN);
-  typedef FfnTile<TA, BM, NW> LA;
-  typedef FfnTile<TB, BN, NW> LB;
-  constexpr int STAGE = LA::kBytes + LB::kBytes;
+  constexpr int HM = BM / 2, HN = BN / 2;                      // a half's rows, columns
+  constexpr int TI = HM / (16 * WM), TJ = HN / (16 * WN);      // MFMA tiles of a wave in a quadrant
+  typedef FfnTile<TA, HM, NW> LA;
+  typedef FfnTile<TB, HN, NW> LB;
+  constexpr int STAGE = 2 * (LA::kBytes + LB::kBytes);
   constexpr bool DUAL = EPI == kFfnGate;
-  constexpr int BC = DUAL ? BN / 2 : BN;  // columns of C of a tile
-  static_assert(TJ % 2 == 0 && (!DUAL || (TJ == 4 && TB == 0)), "epilogue pairs");
+  constexpr int BC = DUAL ? HN : BN;  // columns of C of a tile
+  static_assert(!DUAL || TB == 0, "the gated epilogue reads linear-layer weights");
   __shared__ __attribute__((aligned(1024))) char ring[2 * STAGE];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -189,11 +211,16 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   const int s_per = (all + g.ksplit - 1) / g.ksplit;
   const int s0 = bz * s_per, steps = max(0, min(s0 + s_per, all) - s0);
 
-  unsigned va[LA::P], vb[LB::P];
+  unsigned va[2][LA::P], vb[2][LB::P];  // byte offsets of this lane's transfers
 #pragma unroll
-  for (int q = 0; q < LA::P; ++q) va[q] = LA::voff(wave + NW * q, lane, p.lda);
+  for (int h = 0; h < 2; ++h) {
 #pragma unroll
-  for (int q = 0; q < LB::P; ++q) vb[q] = LB::voff((wave + NW * q) % (DUAL ? BC / 8 : BN), lane, p.ldb);
+    for (int q = 0; q < LA::P; ++q)
+      va[h][q] = LA::voff(wave + NW * q, lane, p.lda) + h * HM * 2 * (TA ? 1 : (unsigned)p.lda);
+#pragma unroll
+    for (int q = 0; q < LB::P; ++q)
+      vb[h][q] = LB::voff(wave + NW * q, lane, p.ldb) + (DUAL ? 0 : h * HN * 2 * (TB ? 1 : (unsigned)p.ldb));
+  }
 
   // Descriptors of a step's operands: they end where the tile's rows do (rows along
   // K) or with the step's last K row (columns along K; past the last column of a
@@ -226,153 +253,187 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
     pa = last ? pa1 : pa + astep;
     pb = last ? pb1 : pb + bstep;
   };
-  // This wave's transfer q of that step to a stage. In the last step of a segment a
-  // row's next elements are another row's: out of range instead. (A wave's transfers
-  // c are all even or all odd, so a lane's piece is at the same K element in each.)
-  const int pk = LA::piece_k(wave, lane);
-  auto transfer = [&](int buf, int q) {
-    const unsigned l = lbase + buf * STAGE;
-    if (q < LA::P) {
-      dma16_buf(ra, !TA && pk >= kleft ? kFfnOob : va[q], l + NW * 1024 * q);
-    } else {
-      const int u = q - LA::P;
-      dma16_buf(DUAL && u >= LB::P / 2 ? rv : rb, !TB && pk >= kleft ? kFfnOob : vb[u], l + LA::kBytes + NW * 1024 * u);
-    }
-  };
-
-  const int wm = wmi * (BM / WM);
-  f4 acc[TI][TJ];
-#pragma unroll
-  for (int i = 0; i < TI; ++i)
-#pragma unroll
-    for (int j = 0; j < TJ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-  // operand q of half a step: B's column tiles, then A's row tiles
-  auto read = [&](int buf, int h, int q, w4(&fa)[TI], w4(&fb)[TJ]) {
-    const char* s = ring + buf * STAGE;
-    if (q < TJ) {
-      const int r0 = DUAL ? (q >> 1) * BC + wni * (BC / WN) + 16 * (q & 1) : wni * (BN / WN) + 16 * q;
-      fb[q] = LB::frag(s + LA::kBytes, r0, h, lane);
-    } else {
-      fa[q - TJ] = LA::frag(s, wm + 16 * (q - TJ), h, lane);
-    }
-  };
-  // Half a step's products, a row of tiles at a time, and between the rows the reads
-  // of the next half's operands and (D) the transfers of a later step: the matrix
-  // cores work while the wave issues them.
+  // This wave's transfer q of halves A_h and B_h of that step to a stage. In the last
+  // step of a segment a row's next elements are another row's: out of range instead.
+  // (A wave's transfers c are all even or all odd, so a lane's piece is at the same K
+  // element in each.)
   constexpr int PL = LA::P + LB::P;
-  auto half = [&](const w4(&fa)[TI], const w4(&fb)[TJ], int rbuf, int rh, w4(&na)[TI], w4(&nb)[TJ], int dbuf) {
-    constexpr int RR = TI > 1 ? (TI + TJ + TI - 2) / (TI - 1) : TI + TJ;  // reads per row, all of them before the last row
-    constexpr int DR = (PL + TI - 1) / TI;
-    static_assert(RR * TI >= TI + TJ && DR * TI >= PL, "every read and every transfer has its row");
-#pragma unroll
-    for (int i = 0; i < TI; ++i) {
-#pragma unroll
-      for (int j = 0; j < TJ; ++j) acc[i][j] = mfma(Op::get(fb[j]), Op::get(fa[i]), acc[i][j]);  // C^T tiles
-      __builtin_amdgcn_sched_barrier(0);
-      if (dbuf < 0 && i == TI / 2) next();
-#pragma unroll
-      for (int q = i * RR; q < (i + 1) * RR && q < TI + TJ; ++q) read(rbuf, rh, q, na, nb);
-      if (dbuf >= 0) {
-#pragma unroll
-        for (int q = i * DR; q < (i + 1) * DR && q < PL; ++q) transfer(dbuf, q);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
+  const int pk = LA::piece_k(wave, lane);
+  auto transfer = [&](int stage, int h, int q) {
+    const unsigned l = lbase + stage * STAGE;
+    if (q < LA::P)
+      dma16_buf(ra, !TA && pk >= kleft ? kFfnOob : va[h][q], l + h * LA::kBytes + NW * 1024 * q);
+    else
+      dma16_buf(DUAL && h ? rv : rb, !TB && pk >= kleft ? kFfnOob : vb[h][q - LA::P],
+                l + 2 * LA::kBytes + h * LB::kBytes + NW * 1024 * (q - LA::P));
   };
 
-  w4 fa0[TI], fb0[TJ], fa1[TI], fb1[TJ];
+  const int wm = wmi * (HM / WM), wn = wni * (HN / WN);
+  f4 acc[2][2][TI][TJ];  // quadrant (A half, B half)
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) acc[q >> 1][q & 1][i][j] = f4{0.f, 0.f, 0.f, 0.f};
+  w4 fa[2][2 * TI], fb[2][2 * TJ];  // operands of the halves: K elements 0 .. 31, then 32 .. 63
+  auto read_a = [&](int stage, int h, int q) {
+    fa[h][q] = LA::frag(ring + stage * STAGE + h * LA::kBytes, wm + 16 * (q % TI), q / TI, lane);
+  };
+  auto read_b = [&](int stage, int h, int q) {
+    fb[h][q] = LB::frag(ring + stage * STAGE + 2 * LA::kBytes + h * LB::kBytes, wn + 16 * (q % TJ), q / TJ, lane);
+  };
+  // A part of a step: the products of A_h with B0, then B1, a row of MFMA tiles at a
+  // time, and between the rows the reads and the transfers: the matrix cores work
+  // while the wave issues them.
+  constexpr int ROWS = 4 * TI;
+  constexpr int RR = (2 * TI + 2 * TJ) * 4 / (3 * ROWS) + ((2 * TI + 2 * TJ) * 4 % (3 * ROWS) != 0);  // reads per row
+  constexpr int DR = (PL + ROWS - 1) / ROWS;                                                      // transfers per row
+  static_assert((2 * TJ + RR - 1) / RR <= ROWS / 2 && (2 * TI + RR - 1) / RR <= ROWS / 2 && RR * ROWS >= 2 * TI + 2 * TJ,
+                "every operand is read in time");
+  auto part = [&](int h, int stage) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const int b = r / (2 * TI), kh = r / TI & 1, i = r % TI;
+#pragma unroll
+      for (int j = 0; j < TJ; ++j)
+        acc[h][b][i][j] = mfma(Op::get(fb[b][kh * TJ + j]), Op::get(fa[h][kh * TI + i]), acc[h][b][i][j]);  // C^T tiles
+      __builtin_amdgcn_sched_barrier(0);
+      if (h == 0) {
+#pragma unroll
+        for (int q = r * RR; q < (r + 1) * RR; ++q) {
+          if (q < 2 * TJ)
+            read_b(stage, 1, q);
+          else if (q < 2 * TJ + 2 * TI)
+            read_a(stage, 1, q - 2 * TJ);
+        }
+      } else {
+#pragma unroll
+        for (int q = r * RR; q < (r + 1) * RR; ++q)
+          if (q < 2 * TI) read_a(stage ^ 1, 0, q);
+#pragma unroll
+        for (int q = (r - ROWS / 2) * RR; q < (r - ROWS / 2 + 1) * RR; ++q)  // B0's registers are free after its products
+          if (q >= 0 && q < 2 * TJ) read_b(stage ^ 1, 0, q);
+        if (r == ROWS / 2) next();
+      }
+#pragma unroll
+      for (int q = r * DR; q < (r + 1) * DR && q < PL; ++q)
+        if (h == 0 || r < ROWS / 2) transfer(stage, h, q);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the transfers that the next part reads have landed, and every wave has read what
+    // the next part's transfers overwrite
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0), known to the compiler: no waits for these reads below
+    ring_wait<2 * PL>();
+  };
+  static_assert(PL <= ROWS / 2 * DR, "a part's transfers are issued before its step's descriptors change");
+
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    next();
+#pragma unroll
+    for (int q = 0; q < 2 * PL; ++q) transfer(k, q / PL, q % PL);
+  }
   next();
+  ring_wait<2 * PL>();
 #pragma unroll
-  for (int q = 0; q < PL; ++q) transfer(0, q);
-  next();
+  for (int q = 0; q < 2 * TI; ++q) read_a(0, 0, q);
 #pragma unroll
-  for (int q = 0; q < PL; ++q) transfer(1, q);
-  ring_wait<PL>();
-#pragma unroll
-  for (int q = 0; q < TI + TJ; ++q) read(0, 0, q, fa0, fb0);
+  for (int q = 0; q < 2 * TJ; ++q) read_b(0, 0, q);
+  ring_sync();
   for (int k = 0; k < steps; ++k) {
-    half(fa0, fb0, k & 1, 1, fa1, fb1, -1);
-    // every wave has read this stage, and its transfers into the next one have landed
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0), known to the compiler: no waits for these reads below
-    ring_wait<0>();
-    half(fa1, fb1, (k + 1) & 1, 0, fa0, fb0, k & 1);
+    part(0, k & 1);
+    part(1, k & 1);
   }
   ring_wait<0>();  // no transfer is in flight when the work-group ends
 
-  // Lane (r16, kq) holds C[row 16 i + r16][columns 16 j + 4 kq .. + 3] of its
-  // wave's block. Two column tiles exchange lane rows, so that it holds 8
-  // consecutive columns of one of them: 16 j' + 8 (kq / 2) .. + 7, j' = j + kq % 2.
+  // Lane (r16, kq) holds, of an MFMA tile of C, row r16 and columns 4 kq .. 4 kq + 3.
+  // Two column tiles side by side exchange lane rows, so that it holds 8 consecutive
+  // columns of one of them: 16 (kq % 2) + 8 (kq / 2) .. + 7 of the pair.
   const int64_t ldc = p.ldc;
   if (EPI == kFfnStore && g.ksplit > 1) {
     float* out = g.part + bz * g.part_slice + p.part_off;
 #pragma unroll
-    for (int i = 0; i < TI; ++i) {
-      const int m = mb + wm + 16 * i + r16;
+    for (int hi = 0; hi < 2 * TI; ++hi) {
+      const int m = mb + hi / TI * HM + wm + 16 * (hi % TI) + r16;
       if (m >= p.M) continue;
 #pragma unroll
-      for (int j = 0; j < TJ; ++j) {
-        const int n = nb + wni * (BN / WN) + 16 * j + 4 * kq;
-        if (n < p.N) *reinterpret_cast<f4*>(out + (int64_t)m * p.N + n) = acc[i][j];
+      for (int hj = 0; hj < 2 * TJ; ++hj) {
+        const int n = nb + hj / TJ * HN + wn + 16 * (hj % TJ) + 4 * kq;
+        if (n < p.N) *reinterpret_cast<f4*>(out + (int64_t)m * p.N + n) = acc[hi / TI][hj / TJ][hi % TI][hj % TJ];
       }
     }
     return;
   }
+  constexpr int CW = TJ % 2 ? 4 : 8, NQ = TJ * 4 / CW;  // consecutive columns of a lane, and how often in a half
+  const int cofs = CW == 8 ? 16 * (kq & 1) + 8 * (kq >> 1) : 4 * kq;
 #pragma unroll
-  for (int i = 0; i < TI; ++i) {
-    float x[TJ / 2][8];
+  for (int hi = 0; hi < 2 * TI; ++hi) {
+    float x[2][NQ][CW];
 #pragma unroll
-    for (int q = 0; q < TJ / 2; ++q)
+    for (int q = 0; q < 2 * NQ; ++q)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[q][e] = acc[i][2 * q][e];
-        x[q][4 + e] = acc[i][2 * q + 1][e];
-        swap_rows(x[q][e], x[q][4 + e]);
+        const int h = q / NQ, j = q % NQ;
+        if constexpr (CW == 8) {
+          x[h][j][e] = acc[hi / TI][h][hi % TI][2 * j][e];
+          x[h][j][4 + e] = acc[hi / TI][h][hi % TI][2 * j + 1][e];
+          swap_rows(x[h][j][e], x[h][j][4 + e]);
+        } else {
+          x[h][j][e] = acc[hi / TI][h][hi % TI][j][e];
+        }
       }
-    const int m = mb + wm + 16 * i + r16;
+    const int m = mb + hi / TI * HM + wm + 16 * (hi % TI) + r16;
     if (m >= p.M) continue;
     if constexpr (DUAL) {
-      const int n = nb + wni * (BC / WN) + 16 * (kq & 1) + 8 * (kq >> 1);
-      if (n < p.N) {
-        const int64_t off = 2 * ((int64_t)m * ldc + n);
-        if (g.gate) *reinterpret_cast<w4*>(g.gate + off) = ffn_pack8<DT>(x[0]);
-        if (g.value) *reinterpret_cast<w4*>(g.value + off) = ffn_pack8<DT>(x[1]);
-        float o[8], s;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = ffn_act(x[0][e], g.act, s) * x[1][e];
-        *reinterpret_cast<w4*>(p.c + off) = ffn_pack8<DT>(o);
+      for (int q = 0; q < NQ; ++q) {
+        const int n = nb + wn + 4 * CW * q + cofs;
+        if (n >= p.N) continue;
+        const int64_t off = 2 * ((int64_t)m * ldc + n);
+        if (g.gate) ffn_store<DT, CW>(g.gate + off, x[0][q]);
+        if (g.value) ffn_store<DT, CW>(g.value + off, x[1][q]);
+        float o[CW], s;
+#pragma unroll
+        for (int e = 0; e < CW; ++e) o[e] = ffn_act(x[0][q][e], g.act, s) * x[1][q][e];
+        ffn_store<DT, CW>(p.c + off, o);
       }
     } else {
 #pragma unroll
-      for (int q = 0; q < TJ / 2; ++q) {
-        const int n = nb + wni * (BN / WN) + 32 * q + 16 * (kq & 1) + 8 * (kq >> 1);
+      for (int hq = 0; hq < 2 * NQ; ++hq) {
+        float(&v)[CW] = x[hq / NQ][hq % NQ];
+        const int n = nb + hq / NQ * HN + wn + 4 * CW * (hq % NQ) + cofs;
         if (n >= p.N) continue;
         const int64_t off = (int64_t)m * ldc + n;
         if constexpr (EPI == kFfnGateGrad) {
-          float gt[8], vl[8], dg[8], dv[8], h[8];
-          ffn_load8<DT>(g.gate + 2 * off, gt);
-          ffn_load8<DT>(g.value + 2 * off, vl);
+          float gt[CW], vl[CW], dg[CW], dv[CW], hh[CW];
+          ffn_load<DT, CW>(g.gate + 2 * off, gt);
+          ffn_load<DT, CW>(g.value + 2 * off, vl);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
+          for (int e = 0; e < CW; ++e) {
             float s;
             const float a = ffn_act(gt[e], g.act, s);
-            dg[e] = x[q][e] * vl[e] * s;
-            dv[e] = x[q][e] * a;
-            h[e] = a * vl[e];
+            dg[e] = v[e] * vl[e] * s;
+            dv[e] = v[e] * a;
+            hh[e] = a * vl[e];
           }
-          *reinterpret_cast<w4*>(g.dgate + 2 * off) = ffn_pack8<DT>(dg);
-          *reinterpret_cast<w4*>(g.dvalue + 2 * off) = ffn_pack8<DT>(dv);
-          if (p.c) *reinterpret_cast<w4*>(p.c + 2 * off) = ffn_pack8<DT>(h);
+          ffn_store<DT, CW>(g.dgate + 2 * off, dg);
+          ffn_store<DT, CW>(g.dvalue + 2 * off, dv);
+          if (p.c) ffn_store<DT, CW>(p.c + 2 * off, hh);
         } else {
           if (p.res) {
-            float r[8];
-            load8(p.res, g.cdt, off, r);
+            float r[CW];
+            if (g.cdt == GTR_F32)
+              ffn_load<GTR_F32, CW>(p.res + 4 * off, r);
+            else
+              ffn_load<DT, CW>(p.res + 2 * off, r);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[q][e] += r[e];
+            for (int e = 0; e < CW; ++e) v[e] += r[e];
           }
           if (g.cdt == GTR_F32)
-            store_n<8>(p.c, GTR_F32, off, x[q]);
+            ffn_store<GTR_F32, CW>(p.c + 4 * off, v);
           else
-            *reinterpret_cast<w4*>(p.c + 2 * off) = ffn_pack8<DT>(x[q]);
+            ffn_store<DT, CW>(p.c + 2 * off, v);
         }
       }
     }
@@ -404,9 +465,9 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g) {
     for (int e = 0; e < 8; ++e) x[e] += y[e];
   }
   if (g.cdt == GTR_F32)
-    store_n<8>(p.c, GTR_F32, off, x);
+    ffn_store<GTR_F32, 8>(p.c + 4 * off, x);
   else
-    *reinterpret_cast<w4*>(p.c + 2 * off) = ffn_pack8<DT>(x);
+    ffn_store<DT, 8>(p.c + 2 * off, x);
 }
 
 }  // namespace gtr
