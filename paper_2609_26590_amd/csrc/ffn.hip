@@ -100,10 +100,7 @@ static gtr_status ffn_run(FfnGemm& g, int dt, const FfnPlan& plan, hipStream_t s
   if (hipGetLastError() != hipSuccess) return GTR_ERR_HIP;
   if (plan.ksplit > 1) {
     const unsigned blocks = (unsigned)((off / 8 + 255) / 256);
-    if (dt == GTR_F16)
-      hipLaunchKernelGGL(ffn_reduce_kernel<GTR_F16>, dim3(blocks), dim3(256), 0, stream, g);
-    else
-      hipLaunchKernelGGL(ffn_reduce_kernel<GTR_BF16>, dim3(blocks), dim3(256), 0, stream, g);
+    hipLaunchKernelGGL(ffn_reduce_kernel, dim3(blocks), dim3(256), 0, stream, g);
     if (hipGetLastError() != hipSuccess) return GTR_ERR_HIP;
   }
   return GTR_OK;

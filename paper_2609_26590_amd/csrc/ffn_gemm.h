@@ -42,35 +42,63 @@ struct FfnGemm {
 // What an epilogue does with the product.
 enum { kFfnStore = 0, kFfnGate = 1, kFfnGateGrad = 2 };
 
-// N (4 or 8) consecutive elements of type DT at p (aligned to all of them, float32 to
-// four).
-template <int DT, int N>
-__device__ __forceinline__ void ffn_load(const char* p, float (&x)[N]) {
-  if constexpr (N == 8)
-    load8(p, DT, 0, x);
-  else
-    load4(p, DT, 0, x);
-}
-template <int DT, int N>
-__device__ __forceinline__ void ffn_store(char* p, const float (&x)[N]) {
-  if constexpr (DT == GTR_F32) {
-    store_n<N>(p, GTR_F32, 0, x);
-  } else {
-    typedef unsigned v __attribute__((ext_vector_type(N / 2)));
-    v r;
+// N (4 or 8) 16-bit elements, or N / 2 float32: what one load or store of a lane moves.
+template <int N>
+struct FfnVec {
+  typedef unsigned V __attribute__((ext_vector_type(N / 2)));
+  V v;
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, unsigned off) {
+    if constexpr (N == 8)
+      v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+    else
+      v = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+  }
+  __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, unsigned off) const {
+    if constexpr (N == 8)
+      __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, 0);
+    else
+      __builtin_amdgcn_raw_buffer_store_b64(v, r, off, 0, 0);
+  }
+  template <int DT>
+  __device__ __forceinline__ void unpack(float (&x)[N]) const {
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) {
+      const unsigned u = v[e];
+      if constexpr (DT == GTR_F16) {
+        x[2 * e] = (float)__builtin_bit_cast(_Float16, (unsigned short)(u & 0xffffu));
+        x[2 * e + 1] = (float)__builtin_bit_cast(_Float16, (unsigned short)(u >> 16));
+      } else {
+        x[2 * e] = __builtin_bit_cast(float, u << 16);
+        x[2 * e + 1] = __builtin_bit_cast(float, u & 0xffff0000u);
+      }
+    }
+  }
+  __device__ __forceinline__ float f32(int e) const {
+    const unsigned u = v[e];
+    return __builtin_bit_cast(float, u);
+  }
+  template <int DT>
+  static __device__ __forceinline__ FfnVec pack(const float (&x)[N]) {
+    FfnVec r;
 #pragma unroll
     for (int e = 0; e < N / 2; ++e) {
       if constexpr (DT == GTR_F16) {
-        r[e] = __builtin_bit_cast(unsigned short, (_Float16)x[2 * e]) |
-               (unsigned)__builtin_bit_cast(unsigned short, (_Float16)x[2 * e + 1]) << 16;
+        r.v[e] = __builtin_bit_cast(unsigned short, (_Float16)x[2 * e]) |
+                 (unsigned)__builtin_bit_cast(unsigned short, (_Float16)x[2 * e + 1]) << 16;
       } else {
-        r[e] = __builtin_bit_cast(unsigned short, (__bf16)x[2 * e]) |
-               (unsigned)__builtin_bit_cast(unsigned short, (__bf16)x[2 * e + 1]) << 16;
+        r.v[e] = __builtin_bit_cast(unsigned short, (__bf16)x[2 * e]) |
+                 (unsigned)__builtin_bit_cast(unsigned short, (__bf16)x[2 * e + 1]) << 16;
       }
     }
-    *reinterpret_cast<v*>(p) = r;
+    return r;
   }
-}
+  static __device__ __forceinline__ FfnVec bits(const float* x) {
+    FfnVec r;
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) r.v[e] = __builtin_bit_cast(unsigned, x[e]);
+    return r;
+  }
+};
 
 // act(g) and its derivative. SiLU: g s(g), s(g) (1 + g (1 - s(g))), s the logistic
 // function; GELU: g P(g), P(g) + g phi(g), P and phi the normal distribution
@@ -87,10 +115,14 @@ __device__ __forceinline__ float ffn_act(float g, int act, float& slope) {
 }
 
 // One lane's 16 bytes at base + voff (descriptor-checked: zeros past the end) to LDS
-// byte lds + 16 lane. As dma16: no register is written and M0 is not the compiler's.
-__device__ __forceinline__ void dma16_buf(i4 rsrc, unsigned voff, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc)
-               : "memory");
+// byte lds + 16 lane; lds goes on by STEP. As dma16: no register is written and M0 is
+// not the compiler's. (The addition is the wait state that M0 needs.)
+template <int STEP>
+__device__ __forceinline__ void dma16_buf(i4 rsrc, unsigned voff, unsigned& lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_add_u32 %0, %0, %3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               : "+s"(lds)
+               : "v"(voff), "s"(rsrc), "n"(STEP)
+               : "memory", "scc");
 }
 // Lane rows (16 lanes) 1 and 3 of a against rows 0 and 2 of b.
 __device__ __forceinline__ void swap_rows(float& a, float& b) {
@@ -99,8 +131,6 @@ __device__ __forceinline__ void swap_rows(float& a, float& b) {
   a = __builtin_bit_cast(float, lo);
   b = __builtin_bit_cast(float, hi);
 }
-constexpr unsigned kFfnOob = 0x80000000u;  // a byte offset past every descriptor's range
-
 // n bytes from `at` on as a buffer descriptor.
 __device__ __forceinline__ i4 ffn_rsrc(const char* at, int n) {
   const uint64_t p = reinterpret_cast<uint64_t>(at);
@@ -117,9 +147,9 @@ __device__ __forceinline__ i4 ffn_rsrc(const char* at, int n) {
 // Columns along K (T = 1): 64 rows, one per K element, of BT columns, read with
 // the transposing read ds_read_b64_tr_b16 in blocks of 4 K rows x 16 columns. One
 // such instruction reads, for the four lane groups kq, the K rows 8 kq + 0..3 (or
-// + 4..7): 32 bytes of each of 16 rows. The 32-byte units of a row are permuted by
-// XOR with a function of the row that puts those 16 into 16 different places
-// modulo 512 bytes.
+// + 4..7), 32 bytes of each, half of the groups at a time. The 32-byte units of a row
+// are permuted by XOR with a function of the row that puts those 8 into 8 different
+// places modulo 256 bytes.
 template <int T, int BT, int NW>
 struct FfnTile {
   static constexpr int kBytes = BT * 128;
@@ -129,8 +159,8 @@ struct FfnTile {
 
   static __device__ __forceinline__ int row_swz(int r) { return (r >> 1) & 7; }
   static __device__ __forceinline__ int unit_swz(int k) {
-    const int m = k & 3, q = (k >> 3) & 3;
-    return BT == 128 ? m >> 1 | q << 1 : BT == 64 ? q : q & 1;  // (32: two of the 16 share a place)
+    const int m = k & 3, q = (k >> 3) & 1;
+    return BT == 128 ? m | q << 2 : BT == 64 ? m >> 1 | q << 1 : q;
   }
   // byte offset of this lane's piece of transfer c (0 .. BT / 8 - 1), and its first K element
   static __device__ __forceinline__ unsigned voff(int c, int lane, int64_t ld) {
@@ -145,18 +175,27 @@ struct FfnTile {
   static __device__ __forceinline__ int piece_k(int c, int lane) {  // T = 0: K elements before this lane's piece
     return 8 * ((lane & 7) ^ row_swz(8 * c + (lane >> 3)));
   }
-  // the MFMA operand of rows (columns) r0 .. r0 + 15, K elements 32 h .. 32 h + 31
-  static __device__ __forceinline__ w4 frag(const char* s, int r0, int h, int lane) {
+  // The MFMA operand of rows (columns) r0 + 16 i .. + 15, K elements 32 h .. 32 h + 31,
+  // is at one of kAddr LDS addresses of a lane and a constant from it.
+  static constexpr int kAddr(int n) { return T == 0 ? 2 : n; }  // n: how many i there are
+  static __device__ __forceinline__ unsigned addr(unsigned base, int r0, int x, int lane) {
     const int r16 = lane & 15, kq = lane >> 4;
     if constexpr (T == 0) {
-      const int row = r0 + r16;
-      return *reinterpret_cast<const w4*>(s + row * 128 + (((4 * h + kq) ^ row_swz(r16)) << 4));
+      return base + (r0 + r16) * 128 + (((4 * x + kq) ^ row_swz(r16)) << 4);
     } else {
-      const int k = 8 * kq + (r16 >> 2);  // (of this half; its swizzle is that of k + 4 and k + 32)
-      const char* p = s + (32 * h + k) * (BT * 2) + (((r0 >> 4) ^ unit_swz(k)) << 5) + 8 * (r16 & 3);
+      const int k = 8 * kq + (r16 >> 2);  // (its swizzle is that of k + 4 and k + 32)
+      return base + k * (BT * 2) + ((((r0 >> 4) + x) ^ unit_swz(k)) << 5) + 8 * (r16 & 3);
+    }
+  }
+  template <int N>
+  static __device__ __forceinline__ w4 frag(const unsigned (&at)[N], int i, int h) {
+    if constexpr (T == 0) {
+      typedef __attribute__((address_space(3))) const w4* lp;
+      return *(lp)(uintptr_t)(at[h] + i * 2048);
+    } else {
       typedef __attribute__((address_space(3))) s16v4* lp;
-      const s16v4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)p);
-      const s16v4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + 4 * BT * 2));
+      const s16v4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(uintptr_t)(at[i] + 64 * BT * h));
+      const s16v4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(uintptr_t)(at[i] + 64 * BT * h + 8 * BT));
       return __builtin_bit_cast(w4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   }
@@ -238,14 +277,28 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   const int64_t pv = pb1 - (p.b[0] + b0);
   const unsigned lbase = lds_addr(ring) + wave * 1024;
   i4 ra, rb, rv;
-  int kleft = 64;
-  // The next step's operands: their descriptors, and how many K elements it has.
-  // Past the last step the descriptors are empty: the transfers write zeros that no
-  // product reads, so that the loop has one form.
+  // In the last step of a segment that is not whole, the next elements of a row along
+  // K are another row's: the lanes whose pieces are past the end get offsets past every
+  // descriptor's range. (A wave's transfers c are all even or all odd, so a lane's
+  // piece is at the same K element in each.)
+  const unsigned past = LA::piece_k(wave, lane) >= ktail ? 0x80000000u : 0u;
+  const int tailstep = ktail < 64 ? sps - 1 : -1;
+  int masked = 0;
+  // The next step's operands. Past the last step the descriptors are empty: the
+  // transfers write zeros that no product reads, so that the loop has one form.
   auto next = [&]() {
     const bool last = is == sps - 1, more = left > 0;
     --left;
-    kleft = last ? ktail : 64;
+    if ((!TA || !TB) && masked != (is == tailstep ? 1 : 0)) {
+      masked ^= 1;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int q = 0; q < LA::P; ++q) va[h][q] ^= TA ? 0u : past;
+#pragma unroll
+        for (int q = 0; q < LB::P; ++q) vb[h][q] ^= TB ? 0u : past;
+      }
+    }
     ra = ffn_rsrc(pa, more ? last ? atail : aend : 0);
     rb = ffn_rsrc(pb, more ? last ? btail : bend : 0);
     if (DUAL) rv = ffn_rsrc(pb + pv, more ? bend : 0);
@@ -253,20 +306,21 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
     pa = last ? pa1 : pa + astep;
     pb = last ? pb1 : pb + bstep;
   };
-  // This wave's transfer q of halves A_h and B_h of that step to a stage. In the last
-  // step of a segment a row's next elements are another row's: out of range instead.
-  // (A wave's transfers c are all even or all odd, so a lane's piece is at the same K
-  // element in each.)
+  // This wave's transfer q of halves A_h and B_h of that step to LDS address l on
+  // (transfers in order: l goes on from one to the next).
   constexpr int PL = LA::P + LB::P;
-  const int pk = LA::piece_k(wave, lane);
-  auto transfer = [&](int stage, int h, int q) {
-    const unsigned l = lbase + stage * STAGE;
-    if (q < LA::P)
-      dma16_buf(ra, !TA && pk >= kleft ? kFfnOob : va[h][q], l + h * LA::kBytes + NW * 1024 * q);
+  auto transfer = [&](unsigned& l, int h, int q) {
+    constexpr int S = NW * 1024;
+    if (q < LA::P - 1)
+      dma16_buf<S>(ra, va[h][q], l);
+    else if (q == LA::P - 1 && h == 0)
+      dma16_buf<2 * LA::kBytes - S*(LA::P - 1)>(ra, va[h][q], l);
+    else if (q == LA::P - 1)
+      dma16_buf<LA::kBytes + LB::kBytes - S*(LA::P - 1)>(ra, va[h][q], l);
     else
-      dma16_buf(DUAL && h ? rv : rb, !TB && pk >= kleft ? kFfnOob : vb[h][q - LA::P],
-                l + 2 * LA::kBytes + h * LB::kBytes + NW * 1024 * (q - LA::P));
+      dma16_buf<S>(DUAL && h ? rv : rb, vb[h][q - LA::P], l);
   };
+  auto half_at = [&](int stage, int h) { return lbase + stage * STAGE + h * LA::kBytes; };
 
   const int wm = wmi * (HM / WM), wn = wni * (HN / WN);
   f4 acc[2][2][TI][TJ];  // quadrant (A half, B half)
@@ -277,12 +331,31 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
 #pragma unroll
       for (int j = 0; j < TJ; ++j) acc[q >> 1][q & 1][i][j] = f4{0.f, 0.f, 0.f, 0.f};
   w4 fa[2][2 * TI], fb[2][2 * TJ];  // operands of the halves: K elements 0 .. 31, then 32 .. 63
-  auto read_a = [&](int stage, int h, int q) {
-    fa[h][q] = LA::frag(ring + stage * STAGE + h * LA::kBytes, wm + 16 * (q % TI), q / TI, lane);
+  constexpr int NA = LA::kAddr(TI), NB = LB::kAddr(TJ);
+  unsigned aa[NA], ab[NB];  // of A0 and B0 in the current stage; A1 and B1 are a constant further
+#pragma unroll
+  for (int x = 0; x < NA; ++x) aa[x] = LA::addr(lds_addr(ring), wm, x, lane);
+#pragma unroll
+  for (int x = 0; x < NB; ++x) ab[x] = LB::addr(lds_addr(ring) + 2 * LA::kBytes, wn, x, lane);
+  auto read_a = [&](int h, int q) {
+    unsigned at[NA];
+#pragma unroll
+    for (int x = 0; x < NA; ++x) at[x] = aa[x] + h * LA::kBytes;
+    fa[h][q] = LA::frag(at, q % TI, q / TI);
   };
-  auto read_b = [&](int stage, int h, int q) {
-    fb[h][q] = LB::frag(ring + stage * STAGE + 2 * LA::kBytes + h * LB::kBytes, wn + 16 * (q % TJ), q / TJ, lane);
+  auto read_b = [&](int h, int q) {
+    unsigned at[NB];
+#pragma unroll
+    for (int x = 0; x < NB; ++x) at[x] = ab[x] + h * LB::kBytes;
+    fb[h][q] = LB::frag(at, q % TJ, q / TJ);
   };
+  auto other_stage = [&]() {
+#pragma unroll
+    for (int x = 0; x < NA; ++x) aa[x] ^= STAGE;
+#pragma unroll
+    for (int x = 0; x < NB; ++x) ab[x] ^= STAGE;
+  };
+
   // A part of a step: the products of A_h with B0, then B1, a row of MFMA tiles at a
   // time, and between the rows the reads and the transfers: the matrix cores work
   // while the wave issues them.
@@ -292,6 +365,7 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   static_assert((2 * TJ + RR - 1) / RR <= ROWS / 2 && (2 * TI + RR - 1) / RR <= ROWS / 2 && RR * ROWS >= 2 * TI + 2 * TJ,
                 "every operand is read in time");
   auto part = [&](int h, int stage) {
+    unsigned l = half_at(stage, h);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
       const int b = r / (2 * TI), kh = r / TI & 1, i = r % TI;
@@ -303,22 +377,22 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
 #pragma unroll
         for (int q = r * RR; q < (r + 1) * RR; ++q) {
           if (q < 2 * TJ)
-            read_b(stage, 1, q);
+            read_b(1, q);
           else if (q < 2 * TJ + 2 * TI)
-            read_a(stage, 1, q - 2 * TJ);
+            read_a(1, q - 2 * TJ);
         }
+        if (r == ROWS - 1) other_stage();
       } else {
 #pragma unroll
         for (int q = r * RR; q < (r + 1) * RR; ++q)
-          if (q < 2 * TI) read_a(stage ^ 1, 0, q);
+          if (q < 2 * TI) read_a(0, q);
 #pragma unroll
         for (int q = (r - ROWS / 2) * RR; q < (r - ROWS / 2 + 1) * RR; ++q)  // B0's registers are free after its products
-          if (q >= 0 && q < 2 * TJ) read_b(stage ^ 1, 0, q);
+          if (q >= 0 && q < 2 * TJ) read_b(0, q);
         if (r == ROWS / 2) next();
       }
 #pragma unroll
-      for (int q = r * DR; q < (r + 1) * DR && q < PL; ++q)
-        if (h == 0 || r < ROWS / 2) transfer(stage, h, q);
+      for (int q = r * DR; q < (r + 1) * DR && q < PL; ++q) transfer(l, h, q);
       __builtin_amdgcn_sched_barrier(0);
     }
     // the transfers that the next part reads have landed, and every wave has read what
@@ -332,14 +406,18 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   for (int k = 0; k < 2; ++k) {
     next();
 #pragma unroll
-    for (int q = 0; q < 2 * PL; ++q) transfer(k, q / PL, q % PL);
+    for (int h = 0; h < 2; ++h) {
+      unsigned l = half_at(k, h);
+#pragma unroll
+      for (int q = 0; q < PL; ++q) transfer(l, h, q);
+    }
   }
   next();
   ring_wait<2 * PL>();
 #pragma unroll
-  for (int q = 0; q < 2 * TI; ++q) read_a(0, 0, q);
+  for (int q = 0; q < 2 * TI; ++q) read_a(0, q);
 #pragma unroll
-  for (int q = 0; q < 2 * TJ; ++q) read_b(0, 0, q);
+  for (int q = 0; q < 2 * TJ; ++q) read_b(0, q);
   ring_sync();
   for (int k = 0; k < steps; ++k) {
     part(0, k & 1);
@@ -350,90 +428,114 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   // Lane (r16, kq) holds, of an MFMA tile of C, row r16 and columns 4 kq .. 4 kq + 3.
   // Two column tiles side by side exchange lane rows, so that it holds 8 consecutive
   // columns of one of them: 16 (kq % 2) + 8 (kq / 2) .. + 7 of the pair.
-  const int64_t ldc = p.ldc;
-  if (EPI == kFfnStore && g.ksplit > 1) {
-    float* out = g.part + bz * g.part_slice + p.part_off;
-#pragma unroll
-    for (int hi = 0; hi < 2 * TI; ++hi) {
-      const int m = mb + hi / TI * HM + wm + 16 * (hi % TI) + r16;
-      if (m >= p.M) continue;
-#pragma unroll
-      for (int hj = 0; hj < 2 * TJ; ++hj) {
-        const int n = nb + hj / TJ * HN + wn + 16 * (hj % TJ) + 4 * kq;
-        if (n < p.N) *reinterpret_cast<f4*>(out + (int64_t)m * p.N + n) = acc[hi / TI][hj / TJ][hi % TI][hj % TJ];
-      }
-    }
-    return;
-  }
+  // Loads and stores go through descriptors of the tile's rows, columns past the last
+  // out of range; what the epilogue reads of TI rows is on its way before the first of
+  // them is used.
   constexpr int CW = TJ % 2 ? 4 : 8, NQ = TJ * 4 / CW;  // consecutive columns of a lane, and how often in a half
   const int cofs = CW == 8 ? 16 * (kq & 1) + 8 * (kq >> 1) : 4 * kq;
+  const int rows = min(BM, p.M - mb);
+  const bool cut = EPI == kFfnStore && g.ksplit > 1;
+  const int cdt = cut ? (int)GTR_F32 : EPI == kFfnStore ? g.cdt : DT;
+  const unsigned es = cdt == GTR_F32 ? 4 : 2;
+  const int64_t ldc = cut ? p.N : p.ldc;
+  const int64_t first_at = ((int64_t)mb * ldc + nb) * es;  // the tile's first element
+  const int range = (int)((rows * ldc - nb) * es);
+  auto tile_of = [&](const char* c) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(c) + first_at, 0, c ? range : 0, 0x00020000); };
+  unsigned col[DUAL ? 1 : 2][NQ];  // a lane's columns, in bytes from the tile's first
 #pragma unroll
-  for (int hi = 0; hi < 2 * TI; ++hi) {
-    float x[2][NQ][CW];
+  for (int q = 0; q < (DUAL ? NQ : 2 * NQ); ++q) {
+    const int c = q / NQ * HN + wn + 4 * CW * (q % NQ) + cofs;
+    col[q / NQ][q % NQ] = nb + c < p.N ? c * es : 0x80000000u;
+  }
+  const auto rc = tile_of(cut ? reinterpret_cast<const char*>(g.part + bz * g.part_slice + p.part_off) : p.c);
+  const auto rres = tile_of(EPI == kFfnStore && !cut ? p.res : nullptr);
+  const auto rg = tile_of(g.gate), rl = tile_of(g.value), rdg = tile_of(g.dgate), rdl = tile_of(g.dvalue);
+  const bool res32 = EPI == kFfnStore && p.res && !cut && cdt == GTR_F32, res16 = EPI == kFfnStore && p.res && !cut && cdt != GTR_F32;
 #pragma unroll
-    for (int q = 0; q < 2 * NQ; ++q)
+  for (int h = 0; h < 2; ++h) {  // the rows of A_h
+    FfnVec<CW> e0[TI][2 * NQ], e1[TI][2 * NQ];
+    auto at = [&](int i, int q) {
+      return (unsigned)((h * HM + wm + 16 * i + r16) * (int)ldc) * es + col[DUAL ? 0 : q / NQ][q % NQ];
+    };
+    if (EPI == kFfnGateGrad || res16 || res32) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int h = q / NQ, j = q % NQ;
-        if constexpr (CW == 8) {
-          x[h][j][e] = acc[hi / TI][h][hi % TI][2 * j][e];
-          x[h][j][4 + e] = acc[hi / TI][h][hi % TI][2 * j + 1][e];
-          swap_rows(x[h][j][e], x[h][j][4 + e]);
-        } else {
-          x[h][j][e] = acc[hi / TI][h][hi % TI][j][e];
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int q = 0; q < 2 * NQ; ++q) {
+          const unsigned o = at(i, q);
+          if constexpr (EPI == kFfnGateGrad) {
+            e0[i][q].load(rg, o);
+            e1[i][q].load(rl, o);
+          } else {
+            e0[i][q].load(rres, o);
+            if (res32) e1[i][q].load(rres, o + CW * 2);
+          }
         }
-      }
-    const int m = mb + hi / TI * HM + wm + 16 * (hi % TI) + r16;
-    if (m >= p.M) continue;
-    if constexpr (DUAL) {
+    }
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        const int n = nb + wn + 4 * CW * q + cofs;
-        if (n >= p.N) continue;
-        const int64_t off = 2 * ((int64_t)m * ldc + n);
-        if (g.gate) ffn_store<DT, CW>(g.gate + off, x[0][q]);
-        if (g.value) ffn_store<DT, CW>(g.value + off, x[1][q]);
-        float o[CW], s;
+    for (int i = 0; i < TI; ++i) {
+      float x[2][NQ][CW];
 #pragma unroll
-        for (int e = 0; e < CW; ++e) o[e] = ffn_act(x[0][q][e], g.act, s) * x[1][q][e];
-        ffn_store<DT, CW>(p.c + off, o);
-      }
-    } else {
+      for (int q = 0; q < 2 * NQ; ++q)
 #pragma unroll
-      for (int hq = 0; hq < 2 * NQ; ++hq) {
-        float(&v)[CW] = x[hq / NQ][hq % NQ];
-        const int n = nb + hq / NQ * HN + wn + 4 * CW * (hq % NQ) + cofs;
-        if (n >= p.N) continue;
-        const int64_t off = (int64_t)m * ldc + n;
-        if constexpr (EPI == kFfnGateGrad) {
-          float gt[CW], vl[CW], dg[CW], dv[CW], hh[CW];
-          ffn_load<DT, CW>(g.gate + 2 * off, gt);
-          ffn_load<DT, CW>(g.value + 2 * off, vl);
-#pragma unroll
-          for (int e = 0; e < CW; ++e) {
-            float s;
-            const float a = ffn_act(gt[e], g.act, s);
-            dg[e] = v[e] * vl[e] * s;
-            dv[e] = v[e] * a;
-            hh[e] = a * vl[e];
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (CW == 8) {
+            x[q / NQ][q % NQ][e] = acc[h][q / NQ][i][2 * (q % NQ)][e];
+            x[q / NQ][q % NQ][4 + e] = acc[h][q / NQ][i][2 * (q % NQ) + 1][e];
+            swap_rows(x[q / NQ][q % NQ][e], x[q / NQ][q % NQ][4 + e]);
+          } else {
+            x[q / NQ][q % NQ][e] = acc[h][q / NQ][i][q % NQ][e];
           }
-          ffn_store<DT, CW>(g.dgate + 2 * off, dg);
-          ffn_store<DT, CW>(g.dvalue + 2 * off, dv);
-          if (p.c) ffn_store<DT, CW>(p.c + 2 * off, hh);
-        } else {
-          if (p.res) {
-            float r[CW];
-            if (g.cdt == GTR_F32)
-              ffn_load<GTR_F32, CW>(p.res + 4 * off, r);
-            else
-              ffn_load<DT, CW>(p.res + 2 * off, r);
+        }
+      if constexpr (DUAL) {
 #pragma unroll
-            for (int e = 0; e < CW; ++e) v[e] += r[e];
+        for (int q = 0; q < NQ; ++q) {
+          const unsigned o = at(i, q);
+          if (g.gate) FfnVec<CW>::template pack<DT>(x[0][q]).store(rg, o);
+          if (g.value) FfnVec<CW>::template pack<DT>(x[1][q]).store(rl, o);
+          float y[CW], s;
+#pragma unroll
+          for (int e = 0; e < CW; ++e) y[e] = ffn_act(x[0][q][e], g.act, s) * x[1][q][e];
+          FfnVec<CW>::template pack<DT>(y).store(rc, o);
+        }
+      } else {
+#pragma unroll
+        for (int q = 0; q < 2 * NQ; ++q) {
+          float(&v)[CW] = x[q / NQ][q % NQ];
+          const unsigned o = at(i, q);
+          if constexpr (EPI == kFfnGateGrad) {
+            float gt[CW], vl[CW], dg[CW], dv[CW], hh[CW];
+            e0[i][q].template unpack<DT>(gt);
+            e1[i][q].template unpack<DT>(vl);
+#pragma unroll
+            for (int e = 0; e < CW; ++e) {
+              float s;
+              const float a = ffn_act(gt[e], g.act, s);
+              dg[e] = v[e] * vl[e] * s;
+              dv[e] = v[e] * a;
+              hh[e] = a * vl[e];
+            }
+            FfnVec<CW>::template pack<DT>(dg).store(rdg, o);
+            FfnVec<CW>::template pack<DT>(dv).store(rdl, o);
+            if (p.c) FfnVec<CW>::template pack<DT>(hh).store(rc, o);
+          } else {
+            if (res16) {
+              float r[CW];
+              e0[i][q].template unpack<DT>(r);
+#pragma unroll
+              for (int e = 0; e < CW; ++e) v[e] += r[e];
+            }
+            if (res32) {
+#pragma unroll
+              for (int e = 0; e < CW; ++e) v[e] += e < CW / 2 ? e0[i][q].f32(e) : e1[i][q].f32(e - CW / 2);
+            }
+            if (cdt == GTR_F32) {
+              FfnVec<CW>::bits(v).store(rc, o);
+              FfnVec<CW>::bits(v + CW / 2).store(rc, o + CW * 2);
+            } else {
+              FfnVec<CW>::template pack<DT>(v).store(rc, o);
+            }
           }
-          if (g.cdt == GTR_F32)
-            ffn_store<GTR_F32, CW>(p.c + 4 * off, v);
-          else
-            ffn_store<DT, CW>(p.c + 2 * off, v);
         }
       }
     }
@@ -441,7 +543,6 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
 }
 
 // C = the sum of the slices' partial sums (+ res), 8 elements per thread.
-template <int DT>
 __global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g) {
   int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (t >= g.part_slice) return;
@@ -464,10 +565,7 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] += y[e];
   }
-  if (g.cdt == GTR_F32)
-    ffn_store<GTR_F32, 8>(p.c + 4 * off, x);
-  else
-    ffn_store<DT, 8>(p.c + 2 * off, x);
+  store_n<8>(p.c, g.cdt, off, x);
 }
 
 }  // namespace gtr
