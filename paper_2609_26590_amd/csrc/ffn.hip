@@ -4,8 +4,8 @@
 //   forward:   h = act(x W_g^T) * (x W_v^T)     one launch: both projections, the activation and the product
 //              y = h W_o^T (+ residual)
 //   backward:  dh = dy W_o, dg = dh v act'(g), dv = dh act(g), h = act(g) v   one launch
-//              dW_g = dg^T x, dW_v = dv^T x, dW_o = dy^T h                    one launch
-//              dx = dg W_g + dv W_v                                           one launch, one sum over both
+//              dW_g = dg^T x, dW_v = dv^T x, dW_o = dy^T h,
+//              dx = dg W_g + dv W_v (one sum over both)                       one launch
 //
 // A product whose tiles do not fill the chip is cut along K; the partial sums are
 // added in a fixed order by a second launch.
@@ -23,53 +23,129 @@ constexpr int64_t kFfnMaxWidth = 1 << 20;
 
 // Tiles a product can run in: 256 x 256 with one work-group of 8 waves per CU,
 // 128 x 128 with two of 4 waves, 64 x 64 with four of 4 waves.
-struct FfnTiles {
-  int bm, bn, per_cu;
-  float step, fixed;  // us of a 64-deep step with the CU full, of the rest of a tile
-};
-constexpr FfnTiles kFfnTiles[] = {{256, 256, 1, 1.2f, 6.f}, {128, 128, 2, 0.8f, 4.f}, {64, 64, 4, 0.55f, 3.f}};
+constexpr int kFfnTile[3] = {256, 128, 64}, kFfnPerCu[3] = {1, 2, 4};
+enum { kRowRow = 0, kRowCol = 1, kColCol = 2 };  // operands: both along K, A alone, none
 
 struct FfnPlan {
-  int tile, ksplit;
+  int tile, ksplit, steps;  // steps: 64-deep steps of a slice
   int64_t tiles;
+  float us;  // estimate of a work-group's time, the CU full
 };
 
+// Estimates in us, from timings of each tile on its own: a step with `o` work-groups
+// on the CU, and what a work-group takes besides its steps.
+static float ffn_step(int tile, int lay, int o) {
+  static const float one[3][3] = {{1.0f, 1.0f, 1.1f}, {0.45f, 0.5f, 0.5f}, {0.25f, 0.28f, 0.35f}};
+  static const float full[3][3] = {{1.4f, 1.45f, 1.5f}, {1.05f, 1.4f, 1.4f}, {0.8f, 1.3f, 1.6f}};
+  const int n = kFfnPerCu[tile];
+  return n == 1 ? full[tile][lay] : one[tile][lay] + (full[tile][lay] - one[tile][lay]) * (float)(o - 1) / (float)(n - 1);
+}
+static float ffn_fixed(int tile, int epi) {
+  static const float plain[3] = {9.f, 6.f, 4.5f};
+  return plain[tile] + (epi == kFfnStore ? 0.f : 0.5f * plain[tile]);
+}
+static int64_t ffn_tiles(const FfnProd* p, int nprod, int tile, int epi) {
+  const int bm = kFfnTile[tile], bn = epi == kFfnGate ? bm / 2 : bm;
+  int64_t n = 0;
+  for (int i = 0; i < nprod; ++i) n += (int64_t)((p[i].M + bm - 1) / bm) * ((p[i].N + bn - 1) / bn);
+  return n;
+}
+static int ffn_steps(const FfnProd& p) { return (p.K + 63) / 64 * p.nseg; }
+static int64_t ffn_elems(const FfnProd* p, int nprod) {
+  int64_t n = 0;
+  for (int i = 0; i < nprod; ++i) n += (int64_t)p[i].M * p[i].N;
+  return n;
+}
+// Of partial sums: the launch, and their bytes written and read again.
+static float ffn_cut_us(int64_t elems, int ks) { return 4.f + (float)elems * (float)(ks + 1) * 4.f / 3e6f; }
+
 // The tile size and the number of K slices with the least estimated time.
-// elems: elements of C.
-static FfnPlan ffn_plan(const FfnProd* p, int nprod, int epi) {
-  FfnPlan best = {0, 1, 0};
+static FfnPlan ffn_plan(const FfnProd* p, int nprod, int lay, int epi) {
+  FfnPlan best = {};
   float least = 0.f;
+  const int steps = ffn_steps(p[0]);
+  const int64_t elems = ffn_elems(p, nprod);
   for (int c = 0; c < 3; ++c) {
-    const FfnTiles& t = kFfnTiles[c];
-    const int bn = epi == kFfnGate ? t.bn / 2 : t.bn;
-    int64_t tiles = 0, elems = 0;
-    int steps = 0;
-    for (int i = 0; i < nprod; ++i) {
-      tiles += (int64_t)((p[i].M + t.bm - 1) / t.bm) * ((p[i].N + bn - 1) / bn);
-      elems += (int64_t)p[i].M * p[i].N;
-      const int s = (p[i].K + 63) / 64 * p[i].nseg;
-      steps = s > steps ? s : steps;
-    }
-    const int slots = kFfnCus * t.per_cu;
-    int most = 1;
-    if (epi == kFfnStore) most = steps / 4 < 32 ? steps / 4 : 32;
-    for (int ks = 1; ks <= (most < 1 ? 1 : most); ++ks) {
+    const int64_t tiles = ffn_tiles(p, nprod, c, epi), slots = (int64_t)kFfnCus * kFfnPerCu[c];
+    const int most = epi == kFfnStore && steps >= 8 ? (steps / 4 < 32 ? steps / 4 : 32) : 1;
+    for (int ks = 1; ks <= most; ++ks) {
       const int per = (steps + ks - 1) / ks;
       if (ks > 1 && (steps + per - 1) / per != ks) continue;  // a slice would be empty
-      const int64_t rounds = (tiles * ks + slots - 1) / slots;
-      float us = (float)rounds * (per * t.step + t.fixed);
-      if (ks > 1) us += 4.f + (float)elems * (ks + 1) * 4.f / 3e6f;
+      const int64_t n = tiles * ks, rest = n % slots;
+      const float tile_us = per * ffn_step(c, lay, kFfnPerCu[c]) + ffn_fixed(c, epi);
+      float us = (float)(n / slots) * tile_us;
+      if (rest) us += per * ffn_step(c, lay, (int)((rest + kFfnCus - 1) / kFfnCus)) + ffn_fixed(c, epi);
+      if (ks > 1) us += ffn_cut_us(elems, ks);
       if (least == 0.f || us < least) {
         least = us;
-        best = {c, ks, tiles};
+        best = {c, ks, per, tiles, tile_us};
       }
     }
   }
   return best;
 }
 
+// One tile size for the gradients of the input (nx = 1 or 0 products) and of the
+// weights, which share a launch, and the K slices of each: the launch takes the work
+// of all tiles spread over the chip, and at least the longest tile; per CU that is
+// not full, the tiles run faster.
+static void ffn_plan_grads(const FfnProd* x, int nx, const FfnProd* w, int nw, FfnPlan* px, FfnPlan* pw) {
+  float least = 0.f;
+  const int sx = nx ? ffn_steps(*x) : 0, sw = nw ? ffn_steps(*w) : 0;
+  for (int c = 0; c < 3; ++c) {
+    const int64_t tx = ffn_tiles(x, nx, c, kFfnStore), tw = ffn_tiles(w, nw, c, kFfnStore), slots = (int64_t)kFfnCus * kFfnPerCu[c];
+    const int mx = sx >= 8 ? (sx / 4 < 32 ? sx / 4 : 32) : 1, mw = sw >= 8 ? (sw / 4 < 32 ? sw / 4 : 32) : 1;
+    for (int kx = 1; kx <= mx; ++kx) {
+      const int perx = (sx + kx - 1) / kx;
+      if (kx > 1 && (sx + perx - 1) / perx != kx) continue;
+      if (kx > 1 && tx * (kx - 1) >= slots) break;  // cut no further than full
+      for (int kw = 1; kw <= mw; ++kw) {
+        const int perw = (sw + kw - 1) / kw;
+        if (kw > 1 && (sw + perw - 1) / perw != kw) continue;
+        if (kw > 1 && tw * (kw - 1) >= slots) break;
+        const int64_t n = tx * kx + tw * kw;
+        const int o = n >= slots ? kFfnPerCu[c] : (int)((n + kFfnCus - 1) / kFfnCus);
+        const float fixed = ffn_fixed(c, kFfnStore);
+        const float ux = nx ? perx * ffn_step(c, kRowCol, o) + fixed : 0.f, uw = nw ? perw * ffn_step(c, kColCol, o) + fixed : 0.f;
+        const float longest = ux > uw ? ux : uw, shortest = ux < uw && nx ? ux : nw ? uw : ux;
+        float us = ((float)(tx * kx) * ux + (float)(tw * kw) * uw) / (float)(kFfnCus * o);
+        us = n > slots ? us + 0.5f * shortest : us;
+        us = us < longest ? longest : us;
+        if (kx > 1 || kw > 1)
+          us += ffn_cut_us((kx > 1 ? ffn_elems(x, nx) * (kx + 1) : 0) + (kw > 1 ? ffn_elems(w, nw) * (kw + 1) : 0), 0);
+        if (least == 0.f || us < least) {
+          least = us;
+          *px = {c, kx, perx, tx, ux};
+          *pw = {c, kw, perw, tw, uw};
+        }
+      }
+    }
+  }
+}
+
+// Tile counts and the layout of partial sums.
+static void ffn_prepare(FfnGemm& g, const FfnPlan& plan, int epi) {
+  const int bm = kFfnTile[plan.tile], bn = epi == kFfnGate ? bm / 2 : bm;
+  int64_t off = 0;
+  for (int i = 0; i < g.nprod; ++i) {
+    g.p[i].gx = (g.p[i].M + bm - 1) / bm;
+    g.p[i].gy = (g.p[i].N + bn - 1) / bn;
+    g.p[i].part_off = off;
+    off += (int64_t)g.p[i].M * g.p[i].N;
+  }
+  g.ksplit = plan.ksplit;
+  g.part_slice = off;
+}
+
+static gtr_status ffn_add_slices(const FfnGemm& g, const FfnGemm& h, hipStream_t stream) {
+  const int64_t n = (g.ksplit > 1 ? g.part_slice : 0) + (h.ksplit > 1 ? h.part_slice : 0);
+  if (!n) return GTR_OK;
+  hipLaunchKernelGGL(ffn_reduce_kernel, dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, stream, g, h);
+  return hipGetLastError() == hipSuccess ? GTR_OK : GTR_ERR_HIP;
+}
+
 template <int DT, int TA, int TB, int EPI>
-static void ffn_launch_tile(const FfnGemm& g, int tile, unsigned grid, hipStream_t stream) {
+static void ffn_launch(const FfnGemm& g, int tile, unsigned grid, hipStream_t stream) {
   if (tile == 0)
     hipLaunchKernelGGL((ffn_gemm_kernel<DT, TA, TB, EPI, 256, 256, 2, 4>), dim3(grid), dim3(512), 0, stream, g);
   else if (tile == 1)
@@ -78,32 +154,44 @@ static void ffn_launch_tile(const FfnGemm& g, int tile, unsigned grid, hipStream
     hipLaunchKernelGGL((ffn_gemm_kernel<DT, TA, TB, EPI, 64, 64, 2, 2>), dim3(grid), dim3(256), 0, stream, g);
 }
 
-// Fills in the tile counts and runs a launch of products. The plan's ksplit > 1 needs g.part.
+// One product in a launch of its own. A plan with K slices needs g.part.
 template <int TA, int TB, int EPI>
 static gtr_status ffn_run(FfnGemm& g, int dt, const FfnPlan& plan, hipStream_t stream) {
-  const FfnTiles& t = kFfnTiles[plan.tile];
-  const int bn = EPI == kFfnGate ? t.bn / 2 : t.bn;
-  int64_t off = 0;
-  for (int i = 0; i < g.nprod; ++i) {
-    g.p[i].gx = (g.p[i].M + t.bm - 1) / t.bm;
-    g.p[i].gy = (g.p[i].N + bn - 1) / bn;
-    g.p[i].part_off = off;
-    off += (int64_t)g.p[i].M * g.p[i].N;
-  }
-  g.ksplit = plan.ksplit;
-  g.part_slice = off;
+  ffn_prepare(g, plan, EPI);
   const unsigned grid = (unsigned)(plan.tiles * plan.ksplit);
   if (dt == GTR_F16)
-    ffn_launch_tile<GTR_F16, TA, TB, EPI>(g, plan.tile, grid, stream);
+    ffn_launch<GTR_F16, TA, TB, EPI>(g, plan.tile, grid, stream);
   else
-    ffn_launch_tile<GTR_BF16, TA, TB, EPI>(g, plan.tile, grid, stream);
+    ffn_launch<GTR_BF16, TA, TB, EPI>(g, plan.tile, grid, stream);
   if (hipGetLastError() != hipSuccess) return GTR_ERR_HIP;
-  if (plan.ksplit > 1) {
-    const unsigned blocks = (unsigned)((off / 8 + 255) / 256);
-    hipLaunchKernelGGL(ffn_reduce_kernel, dim3(blocks), dim3(256), 0, stream, g);
-    if (hipGetLastError() != hipSuccess) return GTR_ERR_HIP;
-  }
-  return GTR_OK;
+  FfnGemm none = {};
+  return ffn_add_slices(g, none, stream);
+}
+
+template <int DT>
+static void ffn_launch_grads(const FfnGemm& x, const FfnGemm& w, int tile, int nx, int nw, int x_first, hipStream_t stream) {
+  const unsigned grid = (unsigned)(x_first ? (nx + 7) / 8 * 8 + nw : (nw + 7) / 8 * 8 + nx);
+  if (tile == 0)
+    hipLaunchKernelGGL((ffn_grad_kernel<DT, 256, 256, 2, 4>), dim3(grid), dim3(512), 0, stream, x, w, nx, nw, x_first);
+  else if (tile == 1)
+    hipLaunchKernelGGL((ffn_grad_kernel<DT, 128, 128, 2, 2>), dim3(grid), dim3(256), 0, stream, x, w, nx, nw, x_first);
+  else
+    hipLaunchKernelGGL((ffn_grad_kernel<DT, 64, 64, 2, 2>), dim3(grid), dim3(256), 0, stream, x, w, nx, nw, x_first);
+}
+
+// The gradients of input and weights (either may have no product), the longer tiles
+// first, and their K slices' sums.
+static gtr_status ffn_run_grads(FfnGemm& x, FfnGemm& w, int dt, const FfnPlan& px, const FfnPlan& pw, hipStream_t stream) {
+  ffn_prepare(x, px, kFfnStore);
+  ffn_prepare(w, pw, kFfnStore);
+  const int nx = x.nprod ? (int)(px.tiles * px.ksplit) : 0, nw = w.nprod ? (int)(pw.tiles * pw.ksplit) : 0;
+  const int x_first = nx && (!nw || px.us >= pw.us);
+  if (dt == GTR_F16)
+    ffn_launch_grads<GTR_F16>(x, w, px.tile, nx, nw, x_first, stream);
+  else
+    ffn_launch_grads<GTR_BF16>(x, w, px.tile, nx, nw, x_first, stream);
+  if (hipGetLastError() != hipSuccess) return GTR_ERR_HIP;
+  return ffn_add_slices(x, w, stream);
 }
 
 static FfnProd ffn_prod(const void* a, const void* b, void* c, int64_t lda, int64_t ldb, int64_t M, int64_t N, int64_t K) {
@@ -157,8 +245,8 @@ static void ffn_fwd_plan(const gtr_ffn_fwd_args* a, FfnFwdPlan* f) {
   f->up.b[1] = static_cast<const char*>(a->w_value);
   f->down = ffn_prod(nullptr, a->w_out, a->y, a->hidden, a->hidden, a->M, a->d, a->hidden);
   f->down.res = static_cast<const char*>(a->residual);
-  f->pu = ffn_plan(&f->up, 1, kFfnGate);
-  f->pd = ffn_plan(&f->down, 1, kFfnStore);
+  f->pu = ffn_plan(&f->up, 1, kRowRow, kFfnGate);
+  f->pd = ffn_plan(&f->down, 1, kRowRow, kFfnStore);
   f->h_bytes = ffn_align((size_t)a->M * a->hidden * 2);
   f->total = f->h_bytes + (f->pd.ksplit > 1 ? ffn_align((size_t)f->pd.ksplit * a->M * a->d * 4) : 0);
 }
@@ -189,7 +277,7 @@ struct FfnBwdPlan {
   FfnProd dh, dx, dw[3];
   int ndw;
   FfnPlan ph, px, pw;
-  size_t kept, dg_off, dv_off, h_off, part_off, total;
+  size_t kept, dg_off, dv_off, h_off, part_off, xpart, total;
 };
 
 static void ffn_bwd_plan(const gtr_ffn_bwd_args* a, FfnBwdPlan* f) {
@@ -211,16 +299,12 @@ static void ffn_bwd_plan(const gtr_ffn_bwd_args* a, FfnBwdPlan* f) {
   if (a->dw_value) f->dw[f->ndw++] = ffn_prod(dv, a->x, a->dw_value, h, d, h, d, M);
   if (a->dw_out) f->dw[f->ndw++] = ffn_prod(a->dy, hh, a->dw_out, d, h, d, h, M);
   for (int i = 0; i < f->ndw; ++i) f->dw[i].res = a->accumulate ? f->dw[i].c : nullptr;
-  f->ph = ffn_plan(&f->dh, 1, kFfnGateGrad);
-  f->px = ffn_plan(&f->dx, 1, kFfnStore);
-  f->pw = ffn_plan(f->dw, f->ndw, kFfnStore);
-  size_t part = 0;
-  if (a->dx && f->px.ksplit > 1) part = (size_t)f->px.ksplit * M * d * 4;
-  if (f->ndw && f->pw.ksplit > 1) {
-    const size_t n = (size_t)f->pw.ksplit * f->ndw * d * h * 4;
-    part = n > part ? n : part;
-  }
-  f->total = f->part_off + ffn_align(part);
+  f->ph = ffn_plan(&f->dh, 1, kRowCol, kFfnGateGrad);
+  f->px = f->pw = FfnPlan{0, 1, 0, 0, 0.f};
+  ffn_plan_grads(&f->dx, a->dx ? 1 : 0, f->dw, f->ndw, &f->px, &f->pw);
+  f->xpart = a->dx && f->px.ksplit > 1 ? ffn_align((size_t)f->px.ksplit * M * d * 4) : 0;
+  const size_t wpart = f->ndw && f->pw.ksplit > 1 ? ffn_align((size_t)f->pw.ksplit * f->ndw * d * h * 4) : 0;
+  f->total = f->part_off + f->xpart + wpart;
 }
 
 static gtr_status ffn_bwd_check(const gtr_ffn_bwd_args* a, const FfnBwdPlan& f) {
@@ -313,21 +397,16 @@ extern "C" gtr_status gtr_ffn_bwd(const gtr_ffn_bwd_args* a, hipStream_t stream)
   g.value = const_cast<char*>(static_cast<const char*>(a->value));
   g.dgate = ws + f.dg_off;
   g.dvalue = ws + f.dv_off;
-  g.part = reinterpret_cast<float*>(ws + f.part_off);
   st = ffn_run<0, 1, kFfnGateGrad>(g, a->dtype, f.ph, stream);
   if (st != GTR_OK) return st;
-  if (f.ndw) {
-    for (int i = 0; i < f.ndw; ++i) g.p[i] = f.dw[i];
-    g.nprod = f.ndw;
-    g.cdt = a->dw_dtype;
-    st = ffn_run<1, 1, kFfnStore>(g, a->dtype, f.pw, stream);
-    if (st != GTR_OK) return st;
-  }
-  if (a->dx) {
-    g.p[0] = f.dx;
-    g.nprod = 1;
-    g.cdt = a->dtype;
-    st = ffn_run<0, 1, kFfnStore>(g, a->dtype, f.px, stream);
-  }
-  return st;
+  FfnGemm x = {}, w = {};
+  x.nprod = a->dx ? 1 : 0;
+  x.cdt = a->dtype;
+  x.p[0] = f.dx;
+  x.part = reinterpret_cast<float*>(ws + f.part_off);
+  w.nprod = f.ndw;
+  w.cdt = a->dw_dtype;
+  for (int i = 0; i < f.ndw; ++i) w.p[i] = f.dw[i];
+  w.part = reinterpret_cast<float*>(ws + f.part_off + f.xpart);
+  return ffn_run_grads(x, w, a->dtype, f.px, f.pw, stream);
 }

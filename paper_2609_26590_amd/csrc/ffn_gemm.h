@@ -201,6 +201,9 @@ struct FfnTile {
   }
 };
 
+template <int BM, int BN>
+constexpr int kFfnLds = 2 * (BM + BN) * 128;
+
 // C = A B. TA = 0: A is [M][K], TA = 1: A is [K][M]; TB = 0: B is [N][K], TB = 1:
 // B is [K][N]. WM x WN waves.
 //
@@ -215,8 +218,18 @@ struct FfnTile {
 // with one barrier after each, so every half is free for the step after next a
 // whole step before it is read again: its transfer has three parts' time to
 // arrive.
+//
+// What the epilogue reads (a residual, the projections) is fetched before the
+// products where the registers have room for it (tiles under 256 x 256: short
+// products, whose epilogue would wait for it), else before the epilogue, half of it
+// at a time.
+//
+// b: the work-group's number of T, in the order of dispatch. Work-group b runs on XCD
+// b % 8 (round-robin dispatch); each XCD takes a contiguous range of the tiles, in
+// groups of 8 row tiles, rows fastest: a patch of 8 x 4 tiles that share operands runs
+// on an XCD's 32 CUs at a time.
 template <int DT, int TA, int TB, int EPI, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2))) ffn_gemm_kernel(FfnGemm g) {
+__device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, int T) {
   typedef Operand<DT, DT> Op;
   constexpr int NW = WM * WN;
   constexpr int HM = BM / 2, HN = BN / 2;                      // a half's rows, columns
@@ -224,16 +237,16 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   typedef FfnTile<TA, HM, NW> LA;
   typedef FfnTile<TB, HN, NW> LB;
   constexpr int STAGE = 2 * (LA::kBytes + LB::kBytes);
+  static_assert(2 * STAGE == kFfnLds<BM, BN>, "two stages");
   constexpr bool DUAL = EPI == kFfnGate;
   constexpr int BC = DUAL ? HN : BN;  // columns of C of a tile
   static_assert(!DUAL || TB == 0, "the gated epilogue reads linear-layer weights");
-  __shared__ __attribute__((aligned(1024))) char ring[2 * STAGE];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wmi = wave / WN, wni = wave % WN;
   const int r16 = lane & 15, kq = lane >> 4;
   // work-group -> tile
-  const int T = gridDim.x, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+  const int xcd = b & 7, slot = b >> 3;
   int jt = xcd * (T >> 3) + min(xcd, T & 7) + slot;
   const int per = T / g.ksplit, bz = jt / per;
   jt -= bz * per;
@@ -368,10 +381,10 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
     unsigned l = half_at(stage, h);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const int b = r / (2 * TI), kh = r / TI & 1, i = r % TI;
+      const int bh = r / (2 * TI), kh = r / TI & 1, i = r % TI;
 #pragma unroll
       for (int j = 0; j < TJ; ++j)
-        acc[h][b][i][j] = mfma(Op::get(fb[b][kh * TJ + j]), Op::get(fa[h][kh * TI + i]), acc[h][b][i][j]);  // C^T tiles
+        acc[h][bh][i][j] = mfma(Op::get(fb[bh][kh * TJ + j]), Op::get(fa[h][kh * TI + i]), acc[h][bh][i][j]);  // C^T tiles
       __builtin_amdgcn_sched_barrier(0);
       if (h == 0) {
 #pragma unroll
@@ -402,6 +415,58 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   };
   static_assert(PL <= ROWS / 2 * DR, "a part's transfers are issued before its step's descriptors change");
 
+  // Lane (r16, kq) holds, of an MFMA tile of C, row r16 and columns 4 kq .. 4 kq + 3.
+  // Two column tiles side by side exchange lane rows, so that it holds 8 consecutive
+  // columns of one of them: 16 (kq % 2) + 8 (kq / 2) .. + 7 of the pair.
+  // Loads and stores go through descriptors of the tile's rows, columns past the last
+  // out of range.
+  constexpr int CW = TJ % 2 ? 4 : 8, NQ = TJ * 4 / CW;  // consecutive columns of a lane, and how often in a half
+  const int cofs = CW == 8 ? 16 * (kq & 1) + 8 * (kq >> 1) : 4 * kq;
+  const int rows = min(BM, p.M - mb);
+  const bool cut = EPI == kFfnStore && g.ksplit > 1;
+  const int cdt = cut ? (int)GTR_F32 : EPI == kFfnStore ? g.cdt : DT;
+  const unsigned es = cdt == GTR_F32 ? 4 : 2;
+  const int64_t ldc = cut ? p.N : p.ldc;
+  const int64_t first_at = ((int64_t)mb * ldc + nb) * es;  // the tile's first element
+  const int range = (int)((rows * ldc - nb) * es);
+  auto tile_of = [&](const char* c) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(c) + first_at, 0, c ? range : 0, 0x00020000); };
+  unsigned col[DUAL ? 1 : 2][NQ];  // a lane's columns, in bytes from the tile's first
+#pragma unroll
+  for (int q = 0; q < (DUAL ? NQ : 2 * NQ); ++q) {
+    const int c = q / NQ * HN + wn + 4 * CW * (q % NQ) + cofs;
+    col[q / NQ][q % NQ] = nb + c < p.N ? c * es : 0x80000000u;
+  }
+  const auto rc = tile_of(cut ? reinterpret_cast<const char*>(g.part + bz * g.part_slice + p.part_off) : p.c);
+  const auto rres = tile_of(EPI == kFfnStore && !cut ? p.res : nullptr);
+  const auto rg = tile_of(g.gate), rl = tile_of(g.value), rdg = tile_of(g.dgate), rdl = tile_of(g.dvalue);
+  const bool res32 = EPI == kFfnStore && p.res && !cut && cdt == GTR_F32, res16 = EPI == kFfnStore && p.res && !cut && cdt != GTR_F32;
+  constexpr bool EARLY = BM < 256;
+  FfnVec<CW> e0[EARLY ? 2 : 1][TI][2 * NQ], e1[EARLY ? 2 : 1][TI][2 * NQ];  // what the epilogue reads
+  auto at = [&](int h, int i, int q) {
+    return (unsigned)((h * HM + wm + 16 * i + r16) * (int)ldc) * es + col[DUAL ? 0 : q / NQ][q % NQ];
+  };
+  auto fetch = [&](int h) {
+    if (EPI == kFfnGateGrad || res16 || res32) {
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int q = 0; q < 2 * NQ; ++q) {
+          const unsigned o = at(h, i, q);
+          if constexpr (EPI == kFfnGateGrad) {
+            e0[EARLY ? h : 0][i][q].load(rg, o);
+            e1[EARLY ? h : 0][i][q].load(rl, o);
+          } else {
+            e0[EARLY ? h : 0][i][q].load(rres, o);
+            if (res32) e1[EARLY ? h : 0][i][q].load(rres, o + CW * 2);
+          }
+        }
+    }
+  };
+  if (EARLY) {
+    fetch(0);
+    fetch(1);
+  }
+
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     next();
@@ -425,53 +490,9 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   }
   ring_wait<0>();  // no transfer is in flight when the work-group ends
 
-  // Lane (r16, kq) holds, of an MFMA tile of C, row r16 and columns 4 kq .. 4 kq + 3.
-  // Two column tiles side by side exchange lane rows, so that it holds 8 consecutive
-  // columns of one of them: 16 (kq % 2) + 8 (kq / 2) .. + 7 of the pair.
-  // Loads and stores go through descriptors of the tile's rows, columns past the last
-  // out of range; what the epilogue reads of TI rows is on its way before the first of
-  // them is used.
-  constexpr int CW = TJ % 2 ? 4 : 8, NQ = TJ * 4 / CW;  // consecutive columns of a lane, and how often in a half
-  const int cofs = CW == 8 ? 16 * (kq & 1) + 8 * (kq >> 1) : 4 * kq;
-  const int rows = min(BM, p.M - mb);
-  const bool cut = EPI == kFfnStore && g.ksplit > 1;
-  const int cdt = cut ? (int)GTR_F32 : EPI == kFfnStore ? g.cdt : DT;
-  const unsigned es = cdt == GTR_F32 ? 4 : 2;
-  const int64_t ldc = cut ? p.N : p.ldc;
-  const int64_t first_at = ((int64_t)mb * ldc + nb) * es;  // the tile's first element
-  const int range = (int)((rows * ldc - nb) * es);
-  auto tile_of = [&](const char* c) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(c) + first_at, 0, c ? range : 0, 0x00020000); };
-  unsigned col[DUAL ? 1 : 2][NQ];  // a lane's columns, in bytes from the tile's first
-#pragma unroll
-  for (int q = 0; q < (DUAL ? NQ : 2 * NQ); ++q) {
-    const int c = q / NQ * HN + wn + 4 * CW * (q % NQ) + cofs;
-    col[q / NQ][q % NQ] = nb + c < p.N ? c * es : 0x80000000u;
-  }
-  const auto rc = tile_of(cut ? reinterpret_cast<const char*>(g.part + bz * g.part_slice + p.part_off) : p.c);
-  const auto rres = tile_of(EPI == kFfnStore && !cut ? p.res : nullptr);
-  const auto rg = tile_of(g.gate), rl = tile_of(g.value), rdg = tile_of(g.dgate), rdl = tile_of(g.dvalue);
-  const bool res32 = EPI == kFfnStore && p.res && !cut && cdt == GTR_F32, res16 = EPI == kFfnStore && p.res && !cut && cdt != GTR_F32;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {  // the rows of A_h
-    FfnVec<CW> e0[TI][2 * NQ], e1[TI][2 * NQ];
-    auto at = [&](int i, int q) {
-      return (unsigned)((h * HM + wm + 16 * i + r16) * (int)ldc) * es + col[DUAL ? 0 : q / NQ][q % NQ];
-    };
-    if (EPI == kFfnGateGrad || res16 || res32) {
-#pragma unroll
-      for (int i = 0; i < TI; ++i)
-#pragma unroll
-        for (int q = 0; q < 2 * NQ; ++q) {
-          const unsigned o = at(i, q);
-          if constexpr (EPI == kFfnGateGrad) {
-            e0[i][q].load(rg, o);
-            e1[i][q].load(rl, o);
-          } else {
-            e0[i][q].load(rres, o);
-            if (res32) e1[i][q].load(rres, o + CW * 2);
-          }
-        }
-    }
+    if (!EARLY) fetch(h);
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
       float x[2][NQ][CW];
@@ -490,7 +511,7 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
       if constexpr (DUAL) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-          const unsigned o = at(i, q);
+          const unsigned o = at(h, i, q);
           if (g.gate) FfnVec<CW>::template pack<DT>(x[0][q]).store(rg, o);
           if (g.value) FfnVec<CW>::template pack<DT>(x[1][q]).store(rl, o);
           float y[CW], s;
@@ -502,11 +523,11 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
 #pragma unroll
         for (int q = 0; q < 2 * NQ; ++q) {
           float(&v)[CW] = x[q / NQ][q % NQ];
-          const unsigned o = at(i, q);
+          const unsigned o = at(h, i, q);
           if constexpr (EPI == kFfnGateGrad) {
             float gt[CW], vl[CW], dg[CW], dv[CW], hh[CW];
-            e0[i][q].template unpack<DT>(gt);
-            e1[i][q].template unpack<DT>(vl);
+            e0[EARLY ? h : 0][i][q].template unpack<DT>(gt);
+            e1[EARLY ? h : 0][i][q].template unpack<DT>(vl);
 #pragma unroll
             for (int e = 0; e < CW; ++e) {
               float s;
@@ -521,13 +542,13 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
           } else {
             if (res16) {
               float r[CW];
-              e0[i][q].template unpack<DT>(r);
+              e0[EARLY ? h : 0][i][q].template unpack<DT>(r);
 #pragma unroll
               for (int e = 0; e < CW; ++e) v[e] += r[e];
             }
             if (res32) {
 #pragma unroll
-              for (int e = 0; e < CW; ++e) v[e] += e < CW / 2 ? e0[i][q].f32(e) : e1[i][q].f32(e - CW / 2);
+              for (int e = 0; e < CW; ++e) v[e] += e < CW / 2 ? e0[EARLY ? h : 0][i][q].f32(e) : e1[EARLY ? h : 0][i][q].f32(e - CW / 2);
             }
             if (cdt == GTR_F32) {
               FfnVec<CW>::bits(v).store(rc, o);
@@ -542,10 +563,33 @@ __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_
   }
 }
 
-// C = the sum of the slices' partial sums (+ res), 8 elements per thread.
-__global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g) {
-  int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-  if (t >= g.part_slice) return;
+template <int DT, int TA, int TB, int EPI, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2))) ffn_gemm_kernel(FfnGemm g) {
+  __shared__ __attribute__((aligned(1024))) char ring[kFfnLds<BM, BN>];
+  ffn_tile<DT, TA, TB, EPI, BM, BN, WM, WN>(g, ring, blockIdx.x, gridDim.x);
+}
+
+// The gradients of the input and of the weights in one launch: neither needs the
+// other, and a short batch's products do not fill the chip one by one. The nx
+// work-groups of dx and the nw of dw follow each other, dx first or last, the first
+// count rounded up to a multiple of 8 for the second's XCDs.
+template <int DT, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2)))
+ffn_grad_kernel(FfnGemm dx, FfnGemm dw, int nx, int nw, int x_first) {
+  __shared__ __attribute__((aligned(1024))) char ring[kFfnLds<BM, BN>];
+  const int n0 = x_first ? nx : nw, r0 = (n0 + 7) & ~7;
+  const bool head = (int)blockIdx.x < r0;
+  const int b = head ? blockIdx.x : blockIdx.x - r0;
+  if (head && b >= n0) return;
+  if (head == (x_first != 0))
+    ffn_tile<DT, 0, 1, kFfnStore, BM, BN, WM, WN>(dx, ring, b, nx);
+  else
+    ffn_tile<DT, 1, 1, kFfnStore, BM, BN, WM, WN>(dw, ring, b, nw);
+}
+
+// C = the sum of the slices' partial sums (+ res), 8 elements per thread: of g, then
+// of h.
+__device__ __forceinline__ void ffn_reduce(const FfnGemm& g, int64_t t) {
   int pi = 0;
   while (pi + 1 < g.nprod && t >= g.p[pi + 1].part_off) ++pi;
   const FfnProd& p = g.p[pi];
@@ -566,6 +610,14 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g) {
     for (int e = 0; e < 8; ++e) x[e] += y[e];
   }
   store_n<8>(p.c, g.cdt, off, x);
+}
+__global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g, FfnGemm h) {
+  const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  const int64_t ng = g.ksplit > 1 ? g.part_slice : 0, nh = h.ksplit > 1 ? h.part_slice : 0;
+  if (t < ng)
+    ffn_reduce(g, t);
+  else if (t - ng < nh)
+    ffn_reduce(h, t - ng);
 }
 
 }  // namespace gtr
