@@ -599,18 +599,16 @@ def gtr_add(a: torch.Tensor, b: torch.Tensor, *, out: Optional[torch.Tensor] = N
 # ---------------------------------------------------------------------------
 # training a channel mixer: gtr_layernorm_fwd / gtr_layernorm_bwd, gtr_ffn_fwd / gtr_ffn_bwd
 # ---------------------------------------------------------------------------
-def _on_stream(stream, tensors, body):
-    """body() with the tensors' device and ``stream`` (default: that device's current stream) current, so that what it
-    allocates belongs to the stream that uses it. Tensors used on a stream that is not their own are kept from being
+def _on_stream(fn, stream, tensors, args):
+    """fn(*args) with the tensors' device and ``stream`` (default: that device's current stream) current, so that what
+    it allocates belongs to the stream that uses it. Tensors used on a stream that is not their own are kept from being
     handed out again before that stream is done with them."""
     dev = tensors[0].device
-    if dev.type != "cuda":
-        raise ValueError("tensors must be on the GPU")
     if stream is None:
         if dev.index == torch._C._cuda_getDevice():
-            return body()
+            return fn(*args)
         with torch.cuda.device(dev):
-            return body()
+            return fn(*args)
     if stream.device != dev:
         raise ValueError(f"stream is on {stream.device}, the tensors on {dev}")
     if int(stream.cuda_stream) != torch._C._cuda_getCurrentRawStream(dev.index):
@@ -618,24 +616,26 @@ def _on_stream(stream, tensors, body):
             if t is not None:
                 t.record_stream(stream)
     with torch.cuda.stream(stream):
-        return body()
+        return fn(*args)
 
 
-def _launch(fn: str, args, dev: torch.device, workspace: Optional["Workspace"], sized: bool = True) -> None:
-    """One call on the current stream. Without a ``workspace`` the scratch memory is the caching allocator's: it belongs
+def _is(t: Optional[torch.Tensor], shape, dtype, index: int) -> bool:
+    """Whether t is None or contiguous, of this shape and type, on GPU ``index`` (what _check explains where it is not)."""
+    return t is None or (t.shape == shape and t.dtype == dtype and t.get_device() == index and t.is_contiguous())
+
+
+def _rows(name: str, t: torch.Tensor) -> None:
+    _dev_contig(name, t)
+    if t.dim() < 1 or t.dtype not in _DT:
+        raise ValueError(f"{name} must be [..., d] of float32, float16 or bfloat16")
+
+
+def _scratch(need: int, dev: torch.device, workspace: Optional["Workspace"]) -> torch.Tensor:
+    """Scratch memory of a call on the current stream. Without a ``workspace`` it is the caching allocator's: it belongs
     to this stream (and, in a graph capture, to the graph), so that no two calls in flight share it."""
-    lib = load()
-    if sized:
-        need = int(getattr(lib, fn + "_workspace_size")(ctypes.byref(args)))
-        if need:
-            if workspace is None:
-                buf = torch.empty(need, dtype=torch.uint8, device=dev)
-            else:
-                buf = workspace.get(need, torch.cuda.current_stream(dev))
-            args.workspace, args.workspace_bytes = buf.data_ptr(), buf.numel()
-    st = getattr(lib, fn)(ctypes.byref(args), torch._C._cuda_getCurrentRawStream(dev.index))
-    if st:
-        raise GtrError(fn, st)
+    if workspace is not None:
+        return workspace.get(need, torch.cuda.current_stream(dev))
+    return torch.empty(need, dtype=torch.uint8, device=dev)
 
 
 def gtr_layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
@@ -644,23 +644,31 @@ def gtr_layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bi
     """Layer normalisation over the last dimension of x (float32, fp16 or bf16; any width up to 16384) that keeps the
     rows' statistics. weight, bias [d] float32. ``out`` may be x. Returns ``(y, mean, rstd)``, the statistics float32 of
     shape x.shape[:-1]."""
-    def body():
-        d, rows = x.shape[-1], x.shape[:-1]
-        y = torch.empty_like(x) if out is None else out
-        mu = torch.empty(rows, dtype=torch.float32, device=x.device) if mean is None else mean
-        rs = torch.empty(rows, dtype=torch.float32, device=x.device) if rstd is None else rstd
-        _check("out", y, x.shape, (x.dtype,), x.device)
-        _check("weight", weight, (d,), (torch.float32,), x.device)
-        _check("bias", bias, (d,), (torch.float32,), x.device)
-        _check("mean", mu, rows, (torch.float32,), x.device)
-        _check("rstd", rs, rows, (torch.float32,), x.device)
-        a = LayernormFwdArgs(_ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mu), _ptr(rs), _DT[x.dtype], d,
-                             x.numel() // d if d else 0, float(eps))
-        _launch("gtr_layernorm_fwd", a, x.device, None, sized=False)
-        return y, mu, rs
-
     _rows("x", x)
-    return _on_stream(stream, (x, weight, bias, out, mean, rstd), body)
+    return _on_stream(_layernorm_fwd, stream, (x, weight, bias, out, mean, rstd), (x, weight, bias, eps, out, mean, rstd))
+
+
+def _layernorm_fwd(x, weight, bias, eps, y, mu, rs):
+    shape, dev, dt = x.shape, x.device, x.dtype
+    d, rows, index = shape[-1], shape[:-1], dev.index
+    if y is None:
+        y = torch.empty_like(x)
+    if mu is None:
+        mu = torch.empty(rows, dtype=torch.float32, device=dev)
+    if rs is None:
+        rs = torch.empty(rows, dtype=torch.float32, device=dev)
+    if not (_is(y, shape, dt, index) and _is(weight, (d,), torch.float32, index) and
+            _is(bias, (d,), torch.float32, index) and _is(mu, rows, torch.float32, index) and
+            _is(rs, rows, torch.float32, index)):
+        _check("out", y, shape, (dt,), dev)
+        for name, t, want in (("weight", weight, (d,)), ("bias", bias, (d,)), ("mean", mu, rows), ("rstd", rs, rows)):
+            _check(name, t, want, (torch.float32,), dev)
+    a = LayernormFwdArgs(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mu.data_ptr(), rs.data_ptr(), _DT[dt], d,
+                         x.numel() // d if d else 0, eps)
+    st = load().gtr_layernorm_fwd(ctypes.byref(a), torch._C._cuda_getCurrentRawStream(index))
+    if st:
+        raise GtrError("gtr_layernorm_fwd", st)
+    return y, mu, rs
 
 
 def gtr_layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -671,41 +679,56 @@ def gtr_layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rst
     """Gradients of :func:`gtr_layernorm_fwd`: ``(dx, dw, db)``, dx in x's type, dw and db [d] float32 summed over the
     rows. ``dres`` (x's shape and type, a residual path's gradient) is added to dx. ``out`` (for dx) may be dy, x or
     dres. ``accumulate``: dw and db are added to what the given ``dw`` and ``db`` hold. What is not wanted is None."""
-    def body():
-        d, dev = x.shape[-1], x.device
-        for name, t in (("dy", dy), ("dres", dres), ("out", out)):
-            _check(name, t, x.shape, (x.dtype,), dev)
-        for name, t in (("mean", mean), ("rstd", rstd)):
-            _check(name, t, x.shape[:-1], (torch.float32,), dev)
-        for name, t in (("weight", weight), ("dw", dw), ("db", db)):
-            _check(name, t, (d,), (torch.float32,), dev)
-        dx = None if not want_dx else torch.empty_like(x) if out is None else out
-        w_ = None if not want_dw else torch.empty(d, dtype=torch.float32, device=dev) if dw is None else dw
-        b_ = None if not want_dw else torch.empty(d, dtype=torch.float32, device=dev) if db is None else db
-        a = LayernormBwdArgs(_ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(dres), _ptr(dx), _ptr(w_),
-                             _ptr(b_), _DT[x.dtype], d, x.numel() // d if d else 0, int(bool(accumulate)))
-        _launch("gtr_layernorm_bwd", a, dev, workspace, sized=want_dw)
-        return dx, w_, b_
-
     _rows("x", x)
     if accumulate and want_dw and (dw is None or db is None):
         raise ValueError("accumulate needs dw and db")
-    return _on_stream(stream, (x, dy, mean, rstd, weight, dres, out, dw, db), body)
+    return _on_stream(_layernorm_bwd, stream, (x, dy, mean, rstd, weight, dres, out, dw, db),
+                      (dy, x, mean, rstd, weight, dres, want_dx, want_dw, out, dw, db, accumulate, workspace))
 
 
-def _rows(name: str, t: torch.Tensor) -> None:
-    _dev_contig(name, t)
-    if t.dim() < 1 or t.dtype not in _DT:
-        raise ValueError(f"{name} must be [..., d] of float32, float16 or bfloat16")
+def _layernorm_bwd(dy, x, mean, rstd, weight, dres, want_dx, want_dw, dx, dw, db, accumulate, workspace):
+    shape, dev, dt = x.shape, x.device, x.dtype
+    d, rows, index, f32 = shape[-1], shape[:-1], dev.index, torch.float32
+    if not (_is(dy, shape, dt, index) and _is(dres, shape, dt, index) and _is(dx, shape, dt, index) and
+            _is(mean, rows, f32, index) and _is(rstd, rows, f32, index) and _is(weight, (d,), f32, index) and
+            _is(dw, (d,), f32, index) and _is(db, (d,), f32, index)):
+        for name, t in (("dy", dy), ("dres", dres), ("out", dx)):
+            _check(name, t, shape, (dt,), dev)
+        for name, t, want in (("mean", mean, rows), ("rstd", rstd, rows), ("weight", weight, (d,)), ("dw", dw, (d,)),
+                              ("db", db, (d,))):
+            _check(name, t, want, (f32,), dev)
+    if not want_dx:
+        dx = None
+    elif dx is None:
+        dx = torch.empty_like(x)
+    if not want_dw:
+        dw = db = None
+    else:
+        dw = torch.empty(d, dtype=f32, device=dev) if dw is None else dw
+        db = torch.empty(d, dtype=f32, device=dev) if db is None else db
+    a = LayernormBwdArgs(dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), _ptr(dres),
+                         _ptr(dx), _ptr(dw), _ptr(db), _DT[dt], d, x.numel() // d if d else 0, bool(accumulate))
+    lib, ref = load(), ctypes.byref(a)
+    need = lib.gtr_layernorm_bwd_workspace_size(ref) if want_dw else 0
+    if need:
+        buf = _scratch(need, dev, workspace)
+        a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel()
+    st = lib.gtr_layernorm_bwd(ref, torch._C._cuda_getCurrentRawStream(index))
+    if st:
+        raise GtrError("gtr_layernorm_bwd", st)
+    return dx, dw, db
 
 
-def _ffn_weights(x, w_gate, w_value, w_out) -> tuple:
-    if x.dtype == torch.float32:
+def _ffn_shape(x, w_gate, w_value, w_out) -> tuple:
+    dt, dev = x.dtype, x.device
+    if dt == torch.float32:
         raise ValueError("x must be float16 or bfloat16")
-    d, hidden = x.shape[-1], w_gate.shape[0]
-    _check("w_gate", w_gate, (hidden, d), (x.dtype,), x.device)
-    _check("w_value", w_value, (hidden, d), (x.dtype,), x.device)
-    _check("w_out", w_out, (d, hidden), (x.dtype,), x.device)
+    d, hidden, index = x.shape[-1], w_gate.shape[0], dev.index
+    if not (_is(w_gate, (hidden, d), dt, index) and _is(w_value, (hidden, d), dt, index) and
+            _is(w_out, (d, hidden), dt, index)):
+        _check("w_gate", w_gate, (hidden, d), (dt,), dev)
+        _check("w_value", w_value, (hidden, d), (dt,), dev)
+        _check("w_out", w_out, (d, hidden), (dt,), dev)
     return d, hidden, x.numel() // d if d else 0
 
 
@@ -724,24 +747,37 @@ def gtr_ffn_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor, w_
     x [..., d] (fp16 or bf16), w_gate and w_value [hidden, d], w_out [d, hidden] (same type; d and hidden multiples of
     8), ``residual`` of x's shape and type (may be ``out``). ``act``: "silu" or "gelu". Returns ``(y, gate, value)``:
     the two projections [..., hidden] for :func:`gtr_ffn_bwd` with ``save`` (or where given), else None."""
-    def body():
-        d, hidden, M = _ffn_weights(x, w_gate, w_value, w_out)
-        dev, kept = x.device, (*x.shape[:-1], hidden)
-        y = torch.empty_like(x) if out is None else out
-        g = torch.empty(kept, dtype=x.dtype, device=dev) if gate is None and save else gate
-        v = torch.empty(kept, dtype=x.dtype, device=dev) if value is None and save else value
-        _check("out", y, x.shape, (x.dtype,), dev)
-        _check("residual", residual, x.shape, (x.dtype,), dev)
-        _check("gate", g, kept, (x.dtype,), dev)
-        _check("value", v, kept, (x.dtype,), dev)
-        a = FfnFwdArgs(_ptr(x), _ptr(w_gate), _ptr(w_value), _ptr(w_out), _ptr(residual), _ptr(y), _ptr(g), _ptr(v),
-                       _DT[x.dtype], kind, M, d, hidden)
-        _launch("gtr_ffn_fwd", a, dev, workspace)
-        return y, g, v
-
     _rows("x", x)
-    kind = _act(act)
-    return _on_stream(stream, (x, w_gate, w_value, w_out, residual, out, gate, value), body)
+    return _on_stream(_ffn_fwd, stream, (x, w_gate, w_value, w_out, residual, out, gate, value),
+                      (x, w_gate, w_value, w_out, _act(act), residual, save, out, gate, value, workspace))
+
+
+def _ffn_fwd(x, w_gate, w_value, w_out, act, residual, save, y, gate, value, workspace):
+    d, hidden, M = _ffn_shape(x, w_gate, w_value, w_out)
+    shape, dev, dt = x.shape, x.device, x.dtype
+    kept, index = (*shape[:-1], hidden), dev.index
+    if y is None:
+        y = torch.empty_like(x)
+    if save and gate is None:
+        gate = torch.empty(kept, dtype=dt, device=dev)
+    if save and value is None:
+        value = torch.empty(kept, dtype=dt, device=dev)
+    if not (_is(y, shape, dt, index) and _is(residual, shape, dt, index) and _is(gate, kept, dt, index) and
+            _is(value, kept, dt, index)):
+        for name, t, want in (("out", y, shape), ("residual", residual, shape), ("gate", gate, kept),
+                              ("value", value, kept)):
+            _check(name, t, want, (dt,), dev)
+    a = FfnFwdArgs(x.data_ptr(), w_gate.data_ptr(), w_value.data_ptr(), w_out.data_ptr(), _ptr(residual), y.data_ptr(),
+                   _ptr(gate), _ptr(value), _DT[dt], act, M, d, hidden)
+    lib, ref = load(), ctypes.byref(a)
+    need = lib.gtr_ffn_fwd_workspace_size(ref)
+    if need:
+        buf = _scratch(need, dev, workspace)
+        a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel()
+    st = lib.gtr_ffn_fwd(ref, torch._C._cuda_getCurrentRawStream(index))
+    if st:
+        raise GtrError("gtr_ffn_fwd", st)
+    return y, gate, value
 
 
 def gtr_ffn_bwd(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor, w_out: torch.Tensor,
@@ -754,31 +790,50 @@ def gtr_ffn_bwd(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_value
 
     The weights' gradients are in ``dw_dtype`` (x's type, the default, or float32) or in that of the tensors given;
     ``accumulate`` adds to what those hold. The residual's gradient is dy itself. What is not wanted is None."""
-    def body():
-        d, hidden, M = _ffn_weights(x, w_gate, w_value, w_out)
-        dev, kept = x.device, (*x.shape[:-1], hidden)
-        _check("dy", dy, x.shape, (x.dtype,), dev)
-        _check("out", out, x.shape, (x.dtype,), dev)
-        _check("gate", gate, kept, (x.dtype,), dev)
-        _check("value", value, kept, (x.dtype,), dev)
-        dx = None if not want_dx else torch.empty_like(x) if out is None else out
-        given = next((t.dtype for t in (dw_gate, dw_value, dw_out) if t is not None), x.dtype)
-        dt = given if dw_dtype is None else dw_dtype
-        if dt not in (x.dtype, torch.float32):
-            raise ValueError("dw_dtype must be x's type or float32")
-        dws = []
-        for name, t, shape in (("dw_gate", dw_gate, (hidden, d)), ("dw_value", dw_value, (hidden, d)),
-                               ("dw_out", dw_out, (d, hidden))):
-            _check(name, t, shape, (dt,), dev)
-            dws.append(None if not want_dw else torch.empty(shape, dtype=dt, device=dev) if t is None else t)
-        a = FfnBwdArgs(_ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_value), _ptr(w_out), _ptr(gate), _ptr(value), _ptr(dx),
-                       _ptr(dws[0]), _ptr(dws[1]), _ptr(dws[2]), _DT[x.dtype], _DT[dt], kind, int(bool(accumulate)), M, d,
-                       hidden)
-        _launch("gtr_ffn_bwd", a, dev, workspace)
-        return (dx, *dws)
-
     _rows("x", x)
-    kind = _act(act)
     if accumulate and want_dw and (dw_gate is None or dw_value is None or dw_out is None):
         raise ValueError("accumulate needs dw_gate, dw_value and dw_out")
-    return _on_stream(stream, (x, dy, w_gate, w_value, w_out, gate, value, out, dw_gate, dw_value, dw_out), body)
+    return _on_stream(_ffn_bwd, stream, (x, dy, w_gate, w_value, w_out, gate, value, out, dw_gate, dw_value, dw_out),
+                      (dy, x, w_gate, w_value, w_out, gate, value, _act(act), want_dx, want_dw, dw_dtype, out, dw_gate,
+                       dw_value, dw_out, accumulate, workspace))
+
+
+def _ffn_bwd(dy, x, w_gate, w_value, w_out, gate, value, act, want_dx, want_dw, dw_dtype, dx, dwg, dwv, dwo, accumulate,
+             workspace):
+    d, hidden, M = _ffn_shape(x, w_gate, w_value, w_out)
+    shape, dev, dt = x.shape, x.device, x.dtype
+    kept, index = (*shape[:-1], hidden), dev.index
+    wt = dw_dtype
+    if wt is None:
+        wt = next((t.dtype for t in (dwg, dwv, dwo) if t is not None), dt)
+    if wt is not dt and wt is not torch.float32:
+        raise ValueError("dw_dtype must be x's type or float32")
+    if not (_is(dy, shape, dt, index) and _is(dx, shape, dt, index) and _is(gate, kept, dt, index) and
+            _is(value, kept, dt, index) and gate is not None and value is not None and
+            _is(dwg, (hidden, d), wt, index) and _is(dwv, (hidden, d), wt, index) and _is(dwo, (d, hidden), wt, index)):
+        for name, t, want, types in (("dy", dy, shape, (dt,)), ("out", dx, shape, (dt,)), ("gate", gate, kept, (dt,)),
+                                     ("value", value, kept, (dt,)), ("dw_gate", dwg, (hidden, d), (wt,)),
+                                     ("dw_value", dwv, (hidden, d), (wt,)), ("dw_out", dwo, (d, hidden), (wt,))):
+            _check(name, t, want, types, dev)
+    if not want_dx:
+        dx = None
+    elif dx is None:
+        dx = torch.empty_like(x)
+    if not want_dw:
+        dwg = dwv = dwo = None
+    else:
+        dwg = torch.empty((hidden, d), dtype=wt, device=dev) if dwg is None else dwg
+        dwv = torch.empty((hidden, d), dtype=wt, device=dev) if dwv is None else dwv
+        dwo = torch.empty((d, hidden), dtype=wt, device=dev) if dwo is None else dwo
+    a = FfnBwdArgs(dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_value.data_ptr(), w_out.data_ptr(), _ptr(gate),
+                   _ptr(value), _ptr(dx), _ptr(dwg), _ptr(dwv), _ptr(dwo), _DT[dt], _DT[wt], act, bool(accumulate), M, d,
+                   hidden)
+    lib, ref = load(), ctypes.byref(a)
+    need = lib.gtr_ffn_bwd_workspace_size(ref)
+    if need:
+        buf = _scratch(need, dev, workspace)
+        a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel()
+    st = lib.gtr_ffn_bwd(ref, torch._C._cuda_getCurrentRawStream(index))
+    if st:
+        raise GtrError("gtr_ffn_bwd", st)
+    return dx, dwg, dwv, dwo

@@ -620,4 +620,87 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g, FfnGemm h) {
     ffn_reduce(h, t - ng);
 }
 
+// ---------------------------------------------------------------------------
+// A few tokens (up to 16): the weights' bytes are the work, each read once. A
+// work-group takes 16 columns of C; its waves take the 64-deep pieces of K in turn,
+// U of them in flight, and multiply a weight's 16 rows (one 16-byte load per lane and
+// 32 K elements, straight into the MFMA operand) with the tokens' rows, which stay in
+// cache. The waves' sums meet in LDS and are added in their order.
+// ---------------------------------------------------------------------------
+struct FfnFew {
+  const char* x;       // [M][K]
+  const char* w[2];    // [N][K]: gate and value, or one weight
+  char* c;             // [M][N]
+  const char* res;     // [M][N] or null (one weight)
+  char *gate, *value;  // [M][N] or null (two weights)
+  int M, N, K, act;
+};
+
+template <int DT, int NB>
+__global__ void __launch_bounds__(512) ffn_few_kernel(FfnFew g) {
+  typedef Operand<DT, DT> Op;
+  constexpr int U = 4, NW = 8;
+  __shared__ f4 sums[NW][NB][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r16 = lane & 15, kq = lane >> 4, n0 = blockIdx.x * 16;
+  const int K = g.K, pieces = (K + 63) / 64;
+  // this lane's rows; past the last one the last one again, which is not stored
+  const char *wr[NB], *xr = g.x + (int64_t)min(r16, g.M - 1) * K * 2;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) wr[b] = g.w[b] + (int64_t)min(n0 + r16, g.N - 1) * K * 2;
+  f4 acc[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = f4{0.f, 0.f, 0.f, 0.f};
+  for (int p = wave; p < pieces; p += NW * U) {
+    w4 fw[2 * U][NB], fx[2 * U];
+#pragma unroll
+    for (int u = 0; u < 2 * U; ++u) {
+      const int k = 64 * (p + NW * (u >> 1)) + 32 * (u & 1) + 8 * kq;
+      const bool in = k < K;  // (K is a multiple of 8)
+      const int64_t o = 2 * (int64_t)(in ? k : 0);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        fw[u][b] = *reinterpret_cast<const w4*>(wr[b] + o);
+        if (!in) fw[u][b] = w4{0, 0, 0, 0};
+      }
+      fx[u] = *reinterpret_cast<const w4*>(xr + o);
+      if (!in) fx[u] = w4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int u = 0; u < 2 * U; ++u)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] = mfma(Op::get(fw[u][b]), Op::get(fx[u]), acc[b]);
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) sums[wave][b][lane] = acc[b];
+  __syncthreads();
+  const int m = r16, n = n0 + 4 * kq;  // columns n .. n + 3 of token m
+  if (threadIdx.x >= 64 || m >= g.M || n >= g.N) return;
+  float s[NB][4];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    f4 v = sums[0][b][lane];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) v += sums[i][b][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[b][e] = v[e];
+  }
+  const int64_t off = (int64_t)m * g.N + n;
+  if constexpr (NB == 2) {
+    if (g.gate) store_n<4>(g.gate, DT, off, s[0]);
+    if (g.value) store_n<4>(g.value, DT, off, s[1]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float slope;
+      s[0][e] = ffn_act(s[0][e], g.act, slope) * s[1][e];
+    }
+  } else if (g.res) {
+    float r[4];
+    load4(g.res, DT, off, r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[0][e] += r[e];
+  }
+  store_n<4>(g.c, DT, off, s[0]);
+}
+
 }  // namespace gtr
