@@ -8,7 +8,9 @@
 //             dx = rstd (t - sum t / d - xh sum (t xh) / d) (+ dres)
 //             dw = sum over the rows of dy xh,  db = sum over the rows of dy
 //
-// What bounds both is memory: each reads its rows once and writes them once. A
+// What bounds both is memory: each reads its rows once and writes them once (32768 x
+// 4096 bf16 forward 101.6 us, 5.3 TB/s; 16384 x 4096 bf16 backward with a residual 97
+// us, 5.5 TB/s; a large copy reaches 5.1), and for short batches the launches. A
 // row lives in the registers of the lanes that share it (so the forward pass
 // takes the squares about the mean, with no second read), in 16-byte vectors at
 // whatever address the row starts: the vector loads and stores of this machine
@@ -41,7 +43,6 @@ struct Ln<GTR_F32> {
     for (int e = 0; e < 4; ++e) r.u[e] = __builtin_bit_cast(unsigned, x[e]);
     return r;
   }
-  static __device__ __forceinline__ float get(const char* p) { return *reinterpret_cast<const float*>(p); }
   static __device__ __forceinline__ void put(char* p, float x) { *reinterpret_cast<float*>(p) = x; }
 };
 template <>
@@ -63,7 +64,6 @@ struct Ln<GTR_F16> {
     for (int e = 0; e < 4; ++e) r.u[e] = bits(x[2 * e]) | bits(x[2 * e + 1]) << 16;
     return r;
   }
-  static __device__ __forceinline__ float get(const char* p) { return (float)*reinterpret_cast<const _Float16*>(p); }
   static __device__ __forceinline__ void put(char* p, float x) { *reinterpret_cast<_Float16*>(p) = (_Float16)x; }
 };
 template <>
@@ -85,70 +85,97 @@ struct Ln<GTR_BF16> {
     }
     return r;
   }
-  static __device__ __forceinline__ float get(const char* p) {
-    return bf16_bits_to_f32(*reinterpret_cast<const unsigned short*>(p));
-  }
   static __device__ __forceinline__ void put(char* p, float x) {
     *reinterpret_cast<unsigned short*>(p) = f32_to_bf16_bits(x);
   }
 };
 
-// Elements c .. c + VE - 1 of a row of d (zeros past its end). The row's last
-// vector may be a part of one: its elements go one by one.
-template <int DT>
-__device__ __forceinline__ void load_vec(const char* row, int c, int d, float (&x)[Ln<DT>::VE]) {
-  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES;
-  if (c + VE <= d) {
-    Ln<DT>::unpack(*reinterpret_cast<const Vec16*>(row + (int64_t)c * ES), x);
-  } else {
-#pragma unroll
-    for (int e = 0; e < VE; ++e) x[e] = c + e < d ? Ln<DT>::get(row + (int64_t)(c + e) * ES) : 0.f;
+// A lane's vector of a row: VE columns from c on. A row whose width is no multiple of
+// VE ends with a vector that starts early, at d - VE, and holds `skip` columns that
+// are the vector's before it: they count as zeros and are not stored. (Where the whole
+// row is shorter than a vector, TINY, its elements go one by one.) Lanes past the
+// row's end have the last vector with every column skipped.
+template <int DT, bool TINY>
+struct LnCols {
+  static constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES;
+  int c, skip;
+  __device__ __forceinline__ LnCols(int index, int d) {
+    const int at = index * VE;
+    c = TINY ? at : min(at, d - VE);
+    skip = TINY ? max(0, min(VE, VE - (d - at))) : min(VE, at - c);  // TINY: columns past the end
   }
-}
-template <int DT>
-__device__ __forceinline__ void store_vec(char* row, int c, int d, const float (&x)[Ln<DT>::VE]) {
-  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES;
-  if (c + VE <= d) {
-    *reinterpret_cast<Vec16*>(row + (int64_t)c * ES) = Ln<DT>::pack(x);
-  } else {
+  __device__ __forceinline__ bool has(int e) const { return TINY ? e < VE - skip : e >= skip; }
+  __device__ __forceinline__ Vec16 load(const char* row) const {
+    if constexpr (!TINY) {
+      return *reinterpret_cast<const Vec16*>(row + (int64_t)c * ES);
+    } else {
+      Vec16 r = {{0, 0, 0, 0}};
 #pragma unroll
-    for (int e = 0; e < VE; ++e)
-      if (c + e < d) Ln<DT>::put(row + (int64_t)(c + e) * ES, x[e]);
-  }
-}
-// Elements c .. c + VE - 1 of a float32 vector of d, `fill` past its end or
-// everywhere if there is no vector.
-template <int VE>
-__device__ __forceinline__ void load_f32(const float* p, int c, int d, float fill, float (&x)[VE]) {
-  if (p && c + VE <= d) {
-#pragma unroll
-    for (int h = 0; h < VE / 4; ++h) {
-      const Vec16 r = *reinterpret_cast<const Vec16*>(p + c + 4 * h);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * h + e] = __builtin_bit_cast(float, r.u[e]);
+      for (int e = 0; e < VE; ++e)
+        if (has(e)) {
+          if constexpr (ES == 4)
+            r.u[e] = *reinterpret_cast<const unsigned*>(row + (int64_t)(c + e) * ES);
+          else
+            r.u[e / 2] |= (unsigned)*reinterpret_cast<const unsigned short*>(row + (int64_t)(c + e) * ES) << (16 * (e & 1));
+        }
+      return r;
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < VE; ++e) x[e] = p && c + e < d ? p[c + e] : fill;
   }
-}
+  __device__ __forceinline__ void unpack(const Vec16& r, float (&x)[VE]) const {
+    Ln<DT>::unpack(r, x);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) x[e] = has(e) ? x[e] : 0.f;
+  }
+  __device__ __forceinline__ void store(char* row, const float (&x)[VE]) const {
+    if (skip == 0) {
+      *reinterpret_cast<Vec16*>(row + (int64_t)c * ES) = Ln<DT>::pack(x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VE; ++e)
+        if (has(e)) Ln<DT>::put(row + (int64_t)(c + e) * ES, x[e]);
+    }
+  }
+  // of a float32 vector of d, or `fill` everywhere if there is none
+  __device__ __forceinline__ void load_f32(const float* p, float fill, float (&x)[VE]) const {
+    if (TINY || !p) {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) x[e] = p && has(e) ? p[c + e] : fill;
+    } else {
+#pragma unroll
+      for (int h = 0; h < VE / 4; ++h) {
+        const Vec16 r = *reinterpret_cast<const Vec16*>(p + c + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * h + e] = __builtin_bit_cast(float, r.u[e]);
+      }
+    }
+  }
+};
 
-// Sum over the T lanes that share a row, in every one of them. For a row of a
-// whole work-group (T > 64) the waves' sums meet in `part`, which holds one slot per
-// wave and is not written again before the next barrier but one.
-template <int T>
-__device__ __forceinline__ float row_sum(float x, float* part) {
-  x = row_bcast<15>(row_inclusive_scan(x));
-  if constexpr (T >= 32) x += __shfl_xor(x, 16, kWave);
-  if constexpr (T >= 64) x += __shfl_xor(x, 32, kWave);
-  if constexpr (T > 64) {
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = 0.f;
+// A row is shared by T lanes: 16, 32 or 64 of a wave, or (T = 0) by all of a work-group
+// of up to 1024. Sums of N values over them, in every one of them. For T = 0 the waves'
+// sums meet in `part`, which holds a slot per wave and value and is not written again
+// before the next barrier but one.
+constexpr int kLnWaves = 16;
+template <int T, int N>
+__device__ __forceinline__ void row_sums(float (&x)[N], float (*part)[T ? 1 : kLnWaves]) {
 #pragma unroll
-    for (int w = 0; w < T / 64; ++w) x += part[w];
+  for (int n = 0; n < N; ++n) {
+    x[n] = row_bcast<15>(row_inclusive_scan(x[n]));
+    if constexpr (T != 16) x[n] += __shfl_xor(x[n], 16, kWave);
+    if constexpr (T != 16 && T != 32) x[n] += __shfl_xor(x[n], 32, kWave);
   }
-  return x;
+  if constexpr (T == 0) {
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int n = 0; n < N; ++n) part[n][threadIdx.x >> 6] = x[n];
+    __syncthreads();
+    const int waves = blockDim.x >> 6;
+#pragma unroll
+    for (int n = 0; n < N; ++n) x[n] = 0.f;
+    for (int w = 0; w < waves; ++w)
+#pragma unroll
+      for (int n = 0; n < N; ++n) x[n] += part[n][w];
+  }
 }
 
 struct LnFwd {
@@ -161,48 +188,73 @@ struct LnFwd {
   float eps;
 };
 
-// T lanes share a row, NV vectors each.
-template <int DT, int T, int NV>
-__global__ void __launch_bounds__(T > 64 ? T : 256) ln_fwd_kernel(LnFwd g) {
-  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES, NT = T > 64 ? T : 256;
-  __shared__ float part[2][T > 64 ? T / 64 : 1];
-  const int64_t row = (int64_t)blockIdx.x * (NT / T) + threadIdx.x / T;
-  const int l = threadIdx.x % T, d = g.d;
-  if (row >= g.M) return;  // (T > 64: one row per work-group, all its threads or none)
-  const char* xr = g.x + row * d * ES;
-  float v[NV][VE], wv[NV][VE], bv[NV][VE];
-  float s = 0.f;
+// NV vectors per lane. A work-group takes the rows r = its index, + the grid, ..
+// (256 / T of them at a time, one if T is 0), keeps the affine weights in registers
+// (read for every row they are four times its bytes) and has the next row on its way
+// while it works on one (AHEAD: where that fits the registers).
+// One vector per lane takes at most 64 registers: two work-groups of 16 waves per CU
+// (8192 x 8192 bf16: 64.5 us, with one 80.5).
+template <int DT, int T, int NV, bool TINY>
+__global__ void __launch_bounds__(T ? 256 : 64 * kLnWaves) __attribute__((amdgpu_waves_per_eu(NV == 1 ? 8 : 4)))
+ln_fwd_kernel(LnFwd g) {
+  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES, R = T ? 256 / (T ? T : 1) : 1;
+  constexpr bool AHEAD = T || NV == 1;
+  const int TT = T ? T : blockDim.x;
+  __shared__ float part[2][2][T ? 1 : kLnWaves];
+  const int l = T ? threadIdx.x % (T ? T : 1) : threadIdx.x, d = g.d;
+  const int64_t step = (int64_t)gridDim.x * R;
+  int64_t row = (int64_t)blockIdx.x * R + (T ? threadIdx.x / (T ? T : 1) : 0);
+  if (row >= g.M) return;  // (T = 0: all threads of the work-group or none, here and in the loop)
+  Vec16 next[NV];
+  auto fetch = [&](int64_t r) {
 #pragma unroll
-  for (int q = 0; q < NV; ++q) load_vec<DT>(xr, (l + T * q) * VE, d, v[q]);
+    for (int q = 0; q < NV; ++q) next[q] = LnCols<DT, TINY>(l + TT * q, d).load(g.x + r * d * ES);
+  };
+  if (AHEAD) fetch(row);
+  float wv[NV][VE], bv[NV][VE];
 #pragma unroll
   for (int q = 0; q < NV; ++q) {
-    load_f32<VE>(g.w, (l + T * q) * VE, d, 1.f, wv[q]);
-    load_f32<VE>(g.b, (l + T * q) * VE, d, 0.f, bv[q]);
+    const LnCols<DT, TINY> k(l + TT * q, d);
+    k.load_f32(g.w, 1.f, wv[q]);
+    k.load_f32(g.b, 0.f, bv[q]);
   }
+  const float dn = (float)d;
+  for (int flip = 0; row < g.M; row += step, flip ^= 1) {
+    float v[NV][VE], s[1] = {0.f};
+    if (!AHEAD) fetch(row);
 #pragma unroll
-  for (int q = 0; q < NV; ++q)
+    for (int q = 0; q < NV; ++q) LnCols<DT, TINY>(l + TT * q, d).unpack(next[q], v[q]);
+    if (AHEAD && row + step < g.M) fetch(row + step);
 #pragma unroll
-    for (int e = 0; e < VE; ++e) s += v[q][e];
-  const float mean = row_sum<T>(s, part[0]) / (float)d;
-  s = 0.f;
+    for (int q = 0; q < NV; ++q)
 #pragma unroll
-  for (int q = 0; q < NV; ++q)
+      for (int e = 0; e < VE; ++e) s[0] += v[q][e];
+    row_sums<T, 1>(s, &part[flip][0]);
+    const float mean = s[0] / dn;  // (a quotient, not a product with 1 / d: the mean of equal values is theirs)
+    s[0] = 0.f;
 #pragma unroll
-    for (int e = 0; e < VE; ++e) {
-      v[q][e] -= mean;
-      if ((l + T * q) * VE + e < d) s = fmaf(v[q][e], v[q][e], s);
+    for (int q = 0; q < NV; ++q) {
+      const LnCols<DT, TINY> k(l + TT * q, d);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        v[q][e] -= mean;
+        const float u = k.has(e) ? v[q][e] : 0.f;
+        s[0] = fmaf(u, u, s[0]);
+      }
     }
-  const float rs = 1.f / sqrtf(row_sum<T>(s, part[1]) / (float)d + g.eps);
+    row_sums<T, 1>(s, &part[flip][1]);
+    const float rs = 1.f / sqrtf(s[0] / dn + g.eps);
 #pragma unroll
-  for (int q = 0; q < NV; ++q) {
-    float o[VE];
+    for (int q = 0; q < NV; ++q) {
+      float o[VE];
 #pragma unroll
-    for (int e = 0; e < VE; ++e) o[e] = fmaf(v[q][e] * rs, wv[q][e], bv[q][e]);
-    if ((l + T * q) * VE < d) store_vec<DT>(g.y + row * d * ES, (l + T * q) * VE, d, o);
-  }
-  if (l == 0) {
-    if (g.mean) g.mean[row] = mean;
-    if (g.rstd) g.rstd[row] = rs;
+      for (int e = 0; e < VE; ++e) o[e] = fmaf(v[q][e] * rs, wv[q][e], bv[q][e]);
+      LnCols<DT, TINY>(l + TT * q, d).store(g.y + row * d * ES, o);
+    }
+    if (l == 0) {
+      if (g.mean) g.mean[row] = mean;
+      if (g.rstd) g.rstd[row] = rs;
+    }
   }
 }
 
@@ -216,65 +268,82 @@ struct LnBwd {
   int d;
 };
 
-// A work-group takes the rows r = its index, + the grid, .. (NT / T of them at a
-// time) and keeps the sums over its rows of dy xh and dy in registers: each
-// lane's own columns. The sums of the rows it holds at a time are then added in a
-// fixed order, and one partial sum per work-group goes to memory, where
-// ln_reduce_kernel adds them in a fixed order too: a call's result does not
-// depend on the order in which work-groups run.
-template <int DT, int T, int NV>
-__global__ void __launch_bounds__(T > 64 ? T : 256) ln_bwd_kernel(LnBwd g) {
-  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES, NT = T > 64 ? T : 256, R = NT / T;
-  __shared__ float part[2][2][T > 64 ? T / 64 : 1];
+// Rows as in the forward pass, the sums over them of dy xh and dy in registers: each
+// lane's own columns. The sums of the rows that a work-group holds at a time are then
+// added in a fixed order, and one partial sum per work-group goes to memory, where
+// ln_reduce_kernel adds them in a fixed order too: a call's result does not depend
+// on the order in which work-groups run.
+template <int DT, int T, int NV, bool TINY>
+__global__ void __launch_bounds__(T ? 256 : 64 * kLnWaves) ln_bwd_kernel(LnBwd g) {
+  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES, R = T ? 256 / (T ? T : 1) : 1;
+  constexpr bool AHEAD = T || NV == 1;
+  const int TT = T ? T : blockDim.x;
+  __shared__ float part[2][2][T ? 1 : kLnWaves];
   __shared__ float cols[R > 1 ? 2 * T * NV * VE : 1];
-  const int l = threadIdx.x % T, grp = threadIdx.x / T, d = g.d;
+  const int l = T ? threadIdx.x % (T ? T : 1) : threadIdx.x, grp = T ? threadIdx.x / (T ? T : 1) : 0, d = g.d;
+  const int64_t step = (int64_t)gridDim.x * R;
+  int64_t row = (int64_t)blockIdx.x * R + grp;
   float wv[NV][VE], aw[NV][VE], ab[NV][VE];
+  Vec16 ny[NV], nx[NV], nr[NV];
+  float nm = 0.f, ns = 0.f;
+  auto fetch = [&](int64_t r) {
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      const LnCols<DT, TINY> k(l + TT * q, d);
+      ny[q] = k.load(g.dy + r * d * ES);
+      nx[q] = k.load(g.x + r * d * ES);
+      if (g.dres) nr[q] = k.load(g.dres + r * d * ES);
+    }
+    nm = g.mean[r];
+    ns = g.rstd[r];
+  };
+  if (AHEAD && row < g.M) fetch(row);
 #pragma unroll
   for (int q = 0; q < NV; ++q) {
-    load_f32<VE>(g.w, (l + T * q) * VE, d, 1.f, wv[q]);
+    LnCols<DT, TINY>(l + TT * q, d).load_f32(g.w, 1.f, wv[q]);
 #pragma unroll
     for (int e = 0; e < VE; ++e) aw[q][e] = ab[q][e] = 0.f;
   }
   const float inv = 1.f / (float)d;
-  int flip = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < g.M; r0 += (int64_t)gridDim.x * R, flip ^= 1) {
-    const int64_t row = r0 + grp;
-    if (R == 1 || row < g.M) {
-      float y[NV][VE], h[NV][VE];
+  for (int flip = 0; row < g.M; row += step, flip ^= 1) {  // (T = 0: all threads of the work-group or none)
+    float y[NV][VE], h[NV][VE];
+    Vec16 r[NV];
+    if (!AHEAD) fetch(row);
+    const float mean = nm, rs = ns;
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      LnCols<DT, TINY>(l + TT * q, d).unpack(ny[q], y[q]);
+      Ln<DT>::unpack(nx[q], h[q]);
+      r[q] = nr[q];
+    }
+    if (AHEAD && row + step < g.M) fetch(row + step);
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        h[q][e] = (h[q][e] - mean) * rs;  // (of a skipped column dy is 0: every sum gets 0 there)
+        aw[q][e] = fmaf(y[q][e], h[q][e], aw[q][e]);
+        ab[q][e] += y[q][e];
+        y[q][e] *= wv[q][e];
+        s[0] += y[q][e];
+        s[1] = fmaf(y[q][e], h[q][e], s[1]);
+      }
+    if (g.dx) {
+      row_sums<T, 2>(s, part[flip]);
+      const float m1 = s[0] * inv, m2 = s[1] * inv;
 #pragma unroll
       for (int q = 0; q < NV; ++q) {
-        load_vec<DT>(g.dy + row * d * ES, (l + T * q) * VE, d, y[q]);
-        load_vec<DT>(g.x + row * d * ES, (l + T * q) * VE, d, h[q]);
-      }
-      const float mean = g.mean[row], rs = g.rstd[row];
-      float s1 = 0.f, s2 = 0.f;
+        float o[VE];
 #pragma unroll
-      for (int q = 0; q < NV; ++q)
+        for (int e = 0; e < VE; ++e) o[e] = rs * (y[q][e] - m1 - h[q][e] * m2);
+        if (g.dres) {
+          float z[VE];
+          Ln<DT>::unpack(r[q], z);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-          h[q][e] = (h[q][e] - mean) * rs;  // (past the row's end dy is 0, so every sum gets 0 there)
-          aw[q][e] = fmaf(y[q][e], h[q][e], aw[q][e]);
-          ab[q][e] += y[q][e];
-          y[q][e] *= wv[q][e];
-          s1 += y[q][e];
-          s2 = fmaf(y[q][e], h[q][e], s2);
+          for (int e = 0; e < VE; ++e) o[e] += z[e];
         }
-      if (g.dx) {
-        const float m1 = row_sum<T>(s1, part[flip][0]) * inv, m2 = row_sum<T>(s2, part[flip][1]) * inv;
-#pragma unroll
-        for (int q = 0; q < NV; ++q) {
-          const int c = (l + T * q) * VE;
-          float o[VE];
-#pragma unroll
-          for (int e = 0; e < VE; ++e) o[e] = rs * (y[q][e] - m1 - h[q][e] * m2);
-          if (g.dres) {
-            float z[VE];
-            load_vec<DT>(g.dres + row * d * ES, c, d, z);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) o[e] += z[e];
-          }
-          if (c < d) store_vec<DT>(g.dx + row * d * ES, c, d, o);
-        }
+        LnCols<DT, TINY>(l + TT * q, d).store(g.dx + row * d * ES, o);
       }
     }
   }
@@ -299,21 +368,23 @@ __global__ void __launch_bounds__(T > 64 ? T : 256) ln_bwd_kernel(LnBwd g) {
       }
       __syncthreads();
     }
-    for (int c = threadIdx.x; c < d; c += NT) {
-      out[c] = cols[2 * c];
-      out[d + c] = cols[2 * c + 1];
+    // place c of `cols` is a lane's element, which the row's last vector has later
+    for (int c = threadIdx.x; c < d; c += 256) {
+      const int last = (d - 1) / VE * VE, at = !TINY && c >= last ? c + (last + VE - d) : c;
+      out[c] = cols[2 * at];
+      out[d + c] = cols[2 * at + 1];
     }
   } else {
 #pragma unroll
-    for (int q = 0; q < NV; ++q)
+    for (int q = 0; q < NV; ++q) {
+      const LnCols<DT, TINY> k(l + TT * q, d);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const int c = (l + T * q) * VE + e;
-        if (c < d) {
-          out[c] = aw[q][e];
-          out[d + c] = ab[q][e];
+      for (int e = 0; e < VE; ++e)
+        if (k.has(e)) {
+          out[k.c + e] = aw[q][e];
+          out[d + k.c + e] = ab[q][e];
         }
-      }
+    }
   }
 }
 
@@ -341,84 +412,81 @@ __global__ void __launch_bounds__(1024) ln_reduce_kernel(const float* __restrict
   }
 }
 
-// How a row is shared: T lanes (a part of a wave, a wave, or a whole work-group)
-// with NV vectors each, at most `most` of them.
-struct LnShape {
-  int T, NV;
-};
-static LnShape ln_shape(int d, int VE, int most) {
-  const int n = (d + VE - 1) / VE;
-  if (n <= 16) return {16, 1};
-  if (n <= 32) return {32, 1};
-  for (int T : {64, 256})
-    if (n <= T * most) return {T, (n + T - 1) / T};
-  return {1024, (n + 1023) / 1024};
-}
+// How a row is shared: by the fewest lanes of a wave that hold it with one vector each,
+// a wave with two (no barrier: 25,600 x 768 bf16 backward 26.5 us against 39.2 as two waves), the fewest waves of a work-group, or all 16 with more vectors.
 constexpr int kLnMaxWidth = 16384;
-static int ln_vec(int dt) { return dt == GTR_F32 ? 4 : 8; }
-// Vectors per lane: the backward pass holds five values per element (dy, xh, w and
-// both sums), the forward pass three.
-static int ln_most(int dt, bool bwd) { return bwd && dt != GTR_F32 ? 2 : 4; }
-static int ln_rows(const LnShape& s) { return s.T > 64 ? 1 : 256 / s.T; }  // of a work-group at a time
+struct LnShape {
+  int T, threads, NV;  // template arguments T and NV, the work-group's size
+  bool tiny;
+};
+static LnShape ln_shape(int d, int dt) {
+  const int VE = dt == GTR_F32 ? 4 : 8, n = (d + VE - 1) / VE;
+  for (int T : {16, 32, 64})
+    if (n <= T) return {T, 256, 1, d < VE};
+  if (n <= 128) return {64, 256, 2, false};
+  const int nv = (n + 1023) / 1024, lanes = (n + nv - 1) / nv;
+  return {0, (lanes + 63) / 64 * 64, nv, false};
+}
+static int ln_rows(const LnShape& s) { return s.T ? 256 / s.T : 1; }  // of a work-group at a time
 
-// Work-groups of the backward pass. Each costs a partial sum (16 bytes per column
-// written and read back), each row 6 to 16 bytes per column: at least 8 rows per
-// slot above 256 work-groups, which a short batch needs to fill the chip.
+// Work-groups of the forward pass: up to 32 waves' per CU four times over (32768 x 4096
+// bf16: 101.6 us; with those of one time 128, with one row each 173).
+static int64_t ln_fwd_groups(int64_t M, const LnShape& s) {
+  const int R = ln_rows(s);
+  const int64_t all = (M + R - 1) / R, most = 256 * 8192 / s.threads;
+  return all < most ? all : most;
+}
+// Work-groups of the backward pass: 8 waves per CU, which have 6 KB of a 4096-wide
+// row's operands each on their way (16384 x 4096 bf16 with a residual: 97 us; with
+// twice as many 111, with four times 118, each costing a partial sum); at least 8 rows
+// per slot above 256 work-groups, which a short batch needs to fill the chip.
 static int64_t ln_bwd_groups(int64_t M, const LnShape& s) {
   const int R = ln_rows(s);
-  const int64_t all = (M + R - 1) / R;
+  const int64_t all = (M + R - 1) / R, most = 256 * 512 / s.threads;
   int64_t g = all / 8;
-  g = g < 256 ? 256 : g > 1024 ? 1024 : g;
+  g = g > most ? most : g;
+  g = g < 256 ? 256 : g;
   return g < all ? g : all;
-}
-
-template <template <int, int, int> class F, class A>
-static bool ln_dispatch(int dt, const LnShape& s, const A& a) {
-#define GTR_LN_NV(DT, TT)                                       \
-  if (s.T == TT) {                                              \
-    if (s.NV == 1) return F<DT, TT, 1>::go(a), true;            \
-    if (s.NV == 2) return F<DT, TT, 2>::go(a), true;            \
-    if constexpr (F<DT, TT, 1>::kMost > 2) {                    \
-      if (s.NV == 3) return F<DT, TT, 3>::go(a), true;          \
-      if (s.NV == 4) return F<DT, TT, 4>::go(a), true;          \
-    }                                                           \
-  }
-#define GTR_LN_T(DT)                                            \
-  if (dt == DT) {                                               \
-    if (s.T == 16) return F<DT, 16, 1>::go(a), true;            \
-    if (s.T == 32) return F<DT, 32, 1>::go(a), true;            \
-    GTR_LN_NV(DT, 64)                                           \
-    GTR_LN_NV(DT, 256)                                          \
-    GTR_LN_NV(DT, 1024)                                         \
-  }
-  GTR_LN_T(GTR_F32)
-  GTR_LN_T(GTR_F16)
-  GTR_LN_T(GTR_BF16)
-#undef GTR_LN_T
-#undef GTR_LN_NV
-  return false;
 }
 
 template <class P>
 struct LnLaunch {
   P p;
+  LnShape s;
   unsigned grid;
   hipStream_t stream;
 };
-template <int DT, int T, int NV>
-struct LnFwdGo {
-  static constexpr int kMost = 4;
-  static void go(const LnLaunch<LnFwd>& a) {
-    hipLaunchKernelGGL((ln_fwd_kernel<DT, T, NV>), dim3(a.grid), dim3(T > 64 ? T : 256), 0, a.stream, a.p);
+template <int DT, int T, int NV, bool TINY = false>
+static void ln_go(const LnLaunch<LnFwd>& a) {
+  hipLaunchKernelGGL((ln_fwd_kernel<DT, T, NV, TINY>), dim3(a.grid), dim3(a.s.threads), 0, a.stream, a.p);
+}
+template <int DT, int T, int NV, bool TINY = false>
+static void ln_go(const LnLaunch<LnBwd>& a) {
+  hipLaunchKernelGGL((ln_bwd_kernel<DT, T, NV, TINY>), dim3(a.grid), dim3(a.s.threads), 0, a.stream, a.p);
+}
+template <int DT, class L>
+static void ln_launch_as(const L& a) {
+  if (a.s.tiny) return ln_go<DT, 16, 1, true>(a);
+  if (a.s.T == 16) return ln_go<DT, 16, 1>(a);
+  if (a.s.T == 32) return ln_go<DT, 32, 1>(a);
+  if (a.s.T == 64) return a.s.NV == 1 ? ln_go<DT, 64, 1>(a) : ln_go<DT, 64, 2>(a);
+  if (a.s.NV == 1) return ln_go<DT, 0, 1>(a);
+  if constexpr (DT == GTR_F32) {  // (4 elements per vector: up to 4 of them at the largest width)
+    if (a.s.NV == 3) return ln_go<DT, 0, 3>(a);
+    if (a.s.NV == 4) return ln_go<DT, 0, 4>(a);
   }
-};
-template <int DT, int T, int NV>
-struct LnBwdGo {
-  static constexpr int kMost = DT == GTR_F32 ? 4 : 2;
-  static void go(const LnLaunch<LnBwd>& a) {
-    hipLaunchKernelGGL((ln_bwd_kernel<DT, T, NV>), dim3(a.grid), dim3(T > 64 ? T : 256), 0, a.stream, a.p);
-  }
-};
+  ln_go<DT, 0, 2>(a);
+}
+template <class L>
+static gtr_status ln_launch(int dt, const L& a) {
+  if (dt == GTR_F32)
+    ln_launch_as<GTR_F32>(a);
+  else if (dt == GTR_F16)
+    ln_launch_as<GTR_F16>(a);
+  else
+    ln_launch_as<GTR_BF16>(a);
+  return hipGetLastError() == hipSuccess ? GTR_OK : GTR_ERR_HIP;
+}
 
 struct LnRange {
   const void* p;
@@ -443,7 +511,7 @@ static gtr_status ln_bwd_check(const gtr_layernorm_bwd_args* a, bool pointers, s
   if (!a) return GTR_ERR_NULL;
   const gtr_status st = ln_sizes(a->M, a->d, a->dtype);
   if (st != GTR_OK) return st;
-  const LnShape s = ln_shape(a->d, ln_vec(a->dtype), ln_most(a->dtype, true));
+  const LnShape s = ln_shape(a->d, a->dtype);
   *need = ((size_t)ln_bwd_groups(a->M, s) * 2 * a->d * 4 + 255) & ~(size_t)255;
   if (!pointers) return GTR_OK;
   if (!a->dy || !a->x || !a->mean || !a->rstd || (!a->dx && !a->dw && !a->db)) return GTR_ERR_NULL;
@@ -490,12 +558,9 @@ extern "C" gtr_status gtr_layernorm_fwd(const gtr_layernorm_fwd_args* a, hipStre
     for (int j = 0; j < i; ++j)
       if (ln_overlap(outs[i], outs[j])) return GTR_ERR_ALIAS;
   }
-  const LnShape s = ln_shape(a->d, ln_vec(a->dtype), ln_most(a->dtype, false));
-  const int R = ln_rows(s);
+  const LnShape s = ln_shape(a->d, a->dtype);
   const LnFwd p = {static_cast<const char*>(a->x), a->w, a->b, static_cast<char*>(a->y), a->mean, a->rstd, a->M, a->d, a->eps};
-  const LnLaunch<LnFwd> l = {p, (unsigned)((a->M + R - 1) / R), stream};
-  if (!ln_dispatch<LnFwdGo>(a->dtype, s, l)) return GTR_ERR_UNSUPPORTED;
-  return hipGetLastError() == hipSuccess ? GTR_OK : GTR_ERR_HIP;
+  return ln_launch(a->dtype, LnLaunch<LnFwd>{p, s, (unsigned)ln_fwd_groups(a->M, s), stream});
 }
 
 extern "C" size_t gtr_layernorm_bwd_workspace_size(const gtr_layernorm_bwd_args* a) {
@@ -507,15 +572,14 @@ extern "C" gtr_status gtr_layernorm_bwd(const gtr_layernorm_bwd_args* a, hipStre
   size_t need;
   const gtr_status st = ln_bwd_check(a, true, &need);
   if (st != GTR_OK) return st;
-  const LnShape s = ln_shape(a->d, ln_vec(a->dtype), ln_most(a->dtype, true));
+  const LnShape s = ln_shape(a->d, a->dtype);
   const int64_t G = ln_bwd_groups(a->M, s);
   const bool sums = a->dw || a->db;
   const LnBwd p = {static_cast<const char*>(a->dy), static_cast<const char*>(a->x), a->mean, a->rstd, a->w,
                    static_cast<const char*>(a->dres), static_cast<char*>(a->dx),
                    sums ? static_cast<float*>(a->workspace) : nullptr, a->M, a->d};
-  const LnLaunch<LnBwd> l = {p, (unsigned)G, stream};
-  if (!ln_dispatch<LnBwdGo>(a->dtype, s, l)) return GTR_ERR_UNSUPPORTED;
-  if (hipGetLastError() != hipSuccess) return GTR_ERR_HIP;
+  const gtr_status run = ln_launch(a->dtype, LnLaunch<LnBwd>{p, s, (unsigned)G, stream});
+  if (run != GTR_OK) return run;
   if (sums) {
     hipLaunchKernelGGL(ln_reduce_kernel, dim3((unsigned)((2 * (int64_t)a->d + 31) / 32)), dim3(1024), 0, stream, p.part,
                        (int)G, a->d, a->dw, a->db, a->accumulate);
