@@ -443,8 +443,8 @@ gtr_status gtr_layernorm_fwd(const gtr_layernorm_fwd_args* args, hipStream_t str
  * mean, rstd : [M] float32 as gtr_layernorm_fwd left them; w as there
  * dw, db : [d] float32, or NULL where not wanted; accumulate 1: added to what
  *          they hold
- * workspace : for dw and db: 256-byte aligned, at least
- *          gtr_layernorm_bwd_workspace_size(args) bytes, no initialisation
+ * workspace : for dw and db, where gtr_layernorm_bwd_workspace_size(args) is not
+ *          0: 256-byte aligned, at least that many bytes, no initialisation
  *          needed; calls that overlap in time must not share one.
  * Sizes and types as for gtr_layernorm_fwd.
  */
@@ -466,7 +466,8 @@ typedef struct {
   size_t workspace_bytes;
 } gtr_layernorm_bwd_args;
 
-/* 0 if the sizes or the type are invalid; pointers are ignored (host only). */
+/* 0 if the call needs none (short batches, unless dx is dy or x) or the sizes or
+ * the type are invalid; other pointers are ignored (host only). */
 size_t gtr_layernorm_bwd_workspace_size(const gtr_layernorm_bwd_args* args);
 gtr_status gtr_layernorm_bwd(const gtr_layernorm_bwd_args* args, hipStream_t stream);
 

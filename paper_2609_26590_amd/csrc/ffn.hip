@@ -33,16 +33,18 @@ struct FfnPlan {
 };
 
 // Estimates in us, from timings of each tile on its own: a step with `o` work-groups
-// on the CU, and what a work-group takes besides its steps.
+// on the CU, and what a work-group takes besides its steps, `fill` being the share of
+// the chip's places that are taken (the gradients' epilogue moves 10 bytes per element
+// of C, which bound it once many do so together).
 static float ffn_step(int tile, int lay, int o) {
-  static const float one[3][3] = {{1.0f, 1.0f, 1.1f}, {0.45f, 0.5f, 0.5f}, {0.25f, 0.28f, 0.35f}};
-  static const float full[3][3] = {{1.4f, 1.45f, 1.5f}, {1.05f, 1.4f, 1.4f}, {0.8f, 1.3f, 1.6f}};
+  static const float one[3][3] = {{1.0f, 1.0f, 1.1f}, {0.38f, 0.42f, 0.45f}, {0.24f, 0.25f, 0.3f}};
+  static const float full[3][3] = {{1.42f, 1.45f, 1.35f}, {0.97f, 1.05f, 1.15f}, {0.82f, 1.19f, 1.46f}};
   const int n = kFfnPerCu[tile];
   return n == 1 ? full[tile][lay] : one[tile][lay] + (full[tile][lay] - one[tile][lay]) * (float)(o - 1) / (float)(n - 1);
 }
-static float ffn_fixed(int tile, int epi) {
-  static const float plain[3] = {9.f, 6.f, 4.5f};
-  return plain[tile] + (epi == kFfnStore ? 0.f : 0.5f * plain[tile]);
+static float ffn_fixed(int tile, int epi, float fill) {
+  static const float us[3][3] = {{9.f, 5.f, 4.f}, {9.f, 4.6f, 2.5f}, {8.f, 5.f, 4.f}}, more[3] = {26.f, 12.f, 3.5f};
+  return us[epi][tile] + (epi == kFfnGateGrad ? more[tile] * (fill < 1.f ? fill : 1.f) : 0.f);
 }
 static int64_t ffn_tiles(const FfnProd* p, int nprod, int tile, int epi) {
   const int bm = kFfnTile[tile], bn = epi == kFfnGate ? bm / 2 : bm;
@@ -71,10 +73,15 @@ static FfnPlan ffn_plan(const FfnProd* p, int nprod, int lay, int epi) {
     for (int ks = 1; ks <= most; ++ks) {
       const int per = (steps + ks - 1) / ks;
       if (ks > 1 && (steps + per - 1) / per != ks) continue;  // a slice would be empty
-      const int64_t n = tiles * ks, rest = n % slots;
-      const float tile_us = per * ffn_step(c, lay, kFfnPerCu[c]) + ffn_fixed(c, epi);
-      float us = (float)(n / slots) * tile_us;
-      if (rest) us += per * ffn_step(c, lay, (int)((rest + kFfnCus - 1) / kFfnCus)) + ffn_fixed(c, epi);
+      const int64_t n = tiles * ks;
+      const float tile_us = per * ffn_step(c, lay, kFfnPerCu[c]) + ffn_fixed(c, epi, 1.f);
+      float us;
+      if (n <= slots)
+        us = per * ffn_step(c, lay, (int)((n + kFfnCus - 1) / kFfnCus)) + ffn_fixed(c, epi, (float)n / (float)slots);
+      else if (kFfnPerCu[c] == 1)
+        us = (float)((n + slots - 1) / slots) * tile_us;
+      else  // a CU's work-groups do not start and end together: no whole rounds
+        us = (float)n / (float)slots * tile_us;
       if (ks > 1) us += ffn_cut_us(elems, ks);
       if (least == 0.f || us < least) {
         least = us;
@@ -105,7 +112,7 @@ static void ffn_plan_grads(const FfnProd* x, int nx, const FfnProd* w, int nw, F
         if (kw > 1 && tw * (kw - 1) >= slots) break;
         const int64_t n = tx * kx + tw * kw;
         const int o = n >= slots ? kFfnPerCu[c] : (int)((n + kFfnCus - 1) / kFfnCus);
-        const float fixed = ffn_fixed(c, kFfnStore);
+        const float fixed = ffn_fixed(c, kFfnStore, 1.f);
         const float ux = nx ? perx * ffn_step(c, kRowCol, o) + fixed : 0.f, uw = nw ? perw * ffn_step(c, kColCol, o) + fixed : 0.f;
         const float longest = ux > uw ? ux : uw, shortest = ux < uw && nx ? ux : nw ? uw : ux;
         float us = ((float)(tx * kx) * ux + (float)(tw * kw) * uw) / (float)(kFfnCus * o);

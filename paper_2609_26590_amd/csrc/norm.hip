@@ -266,6 +266,11 @@ struct LnBwd {
   float* part;  // [work-groups][2][d]: this call's sums of dy xh and of dy, or null
   int64_t M;
   int d;
+  // sums by columns (ln_columns) instead of by partial sums: how many work-groups take
+  // the rows, the others take the columns of dw and db
+  int rows;  // 0: all of them
+  float *dw, *db;
+  int accumulate;
 };
 
 // Rows as in the forward pass, the sums over them of dy xh and dy in registers: each
@@ -273,15 +278,73 @@ struct LnBwd {
 // added in a fixed order, and one partial sum per work-group goes to memory, where
 // ln_reduce_kernel adds them in a fixed order too: a call's result does not depend
 // on the order in which work-groups run.
+//
+// A short batch's sums are cheaper the other way (g.rows): work-groups behind those of
+// the rows take two vectors' columns each over all rows and read dy and x again, from
+// cache, and the call is one launch.
+template <int DT, bool TINY>
+__device__ __forceinline__ void ln_columns(const LnBwd& g, int pair) {
+  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES, U = 4;
+  __shared__ float sums[kLnWaves][2][2 * VE];
+  const LnCols<DT, TINY> k(2 * pair + (threadIdx.x & 1), g.d);
+  const int lanes = blockDim.x / 2;  // rows at a time
+  const int64_t at = (int64_t)g.d * ES;
+  float a[2 * VE];  // sums of dy xh, of dy
+#pragma unroll
+  for (int e = 0; e < 2 * VE; ++e) a[e] = 0.f;
+  for (int64_t r0 = threadIdx.x >> 1; r0 < g.M; r0 += U * lanes) {
+    Vec16 vy[U], vx[U];
+    float mean[U], rs[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = r0 + u * lanes < g.M ? r0 + u * lanes : r0;
+      vy[u] = k.load(g.dy + r * at);
+      vx[u] = k.load(g.x + r * at);
+      mean[u] = g.mean[r];
+      rs[u] = g.rstd[r];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (r0 + u * lanes >= g.M) continue;
+      float y[VE], h[VE];
+      k.unpack(vy[u], y);
+      Ln<DT>::unpack(vx[u], h);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        a[e] = fmaf(y[e], (h[e] - mean[u]) * rs[u], a[e]);
+        a[VE + e] += y[e];
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 2 * VE; ++e) {
+#pragma unroll
+    for (int o = 2; o < 64; o <<= 1) a[e] += __shfl_xor(a[e], o, kWave);
+    if ((threadIdx.x & 63) < 2) sums[threadIdx.x >> 6][threadIdx.x & 1][e] = a[e];
+  }
+  __syncthreads();
+  if (threadIdx.x >= 4 * VE) return;
+  const int v = threadIdx.x / (2 * VE), e = threadIdx.x % (2 * VE);
+  const LnCols<DT, TINY> kv(2 * pair + v, g.d);
+  float t = 0.f;
+  for (int w = 0; w < (int)blockDim.x / 64; ++w) t += sums[w][v][e];
+  float* out = e < VE ? g.dw : g.db;
+  const int c = kv.c + e % VE;
+  if (out && kv.has(e % VE)) out[c] = g.accumulate ? out[c] + t : t;
+}
+
 template <int DT, int T, int NV, bool TINY>
 __global__ void __launch_bounds__(T ? 256 : 64 * kLnWaves) ln_bwd_kernel(LnBwd g) {
+  if (g.rows && (int)blockIdx.x >= g.rows) return ln_columns<DT, TINY>(g, blockIdx.x - g.rows);
+  if (g.rows && !g.dx) return;
+  const int groups = g.rows ? g.rows : gridDim.x;
   constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES, R = T ? 256 / (T ? T : 1) : 1;
   constexpr bool AHEAD = T || NV == 1;
   const int TT = T ? T : blockDim.x;
   __shared__ float part[2][2][T ? 1 : kLnWaves];
   __shared__ float cols[R > 1 ? 2 * T * NV * VE : 1];
   const int l = T ? threadIdx.x % (T ? T : 1) : threadIdx.x, grp = T ? threadIdx.x / (T ? T : 1) : 0, d = g.d;
-  const int64_t step = (int64_t)gridDim.x * R;
+  const int64_t step = (int64_t)groups * R;
   int64_t row = (int64_t)blockIdx.x * R + grp;
   float wv[NV][VE], aw[NV][VE], ab[NV][VE];
   Vec16 ny[NV], nx[NV], nr[NV];
@@ -449,6 +512,15 @@ static int64_t ln_bwd_groups(int64_t M, const LnShape& s) {
   return g < all ? g : all;
 }
 
+// Whether dw and db are summed by columns: where a batch is short, its second reading
+// comes from cache, and dx does not overwrite what is read. 1600 x 384 fp16, calls one
+// after the other: 11.2 us
+// against 12.9 with partial sums and their launch; 2000 x 1024 17.5 against 13.0.
+static bool ln_by_columns(const gtr_layernorm_bwd_args* a) {
+  return a->M <= 2048 && a->M * a->d * (int64_t)dtype_size(a->dtype) <= 3 << 20 &&
+         !(a->dx && (a->dx == a->dy || a->dx == a->x));
+}
+
 template <class P>
 struct LnLaunch {
   P p;
@@ -513,6 +585,7 @@ static gtr_status ln_bwd_check(const gtr_layernorm_bwd_args* a, bool pointers, s
   if (st != GTR_OK) return st;
   const LnShape s = ln_shape(a->d, a->dtype);
   *need = ((size_t)ln_bwd_groups(a->M, s) * 2 * a->d * 4 + 255) & ~(size_t)255;
+  if (ln_by_columns(a)) *need = 0;
   if (!pointers) return GTR_OK;
   if (!a->dy || !a->x || !a->mean || !a->rstd || (!a->dx && !a->dw && !a->db)) return GTR_ERR_NULL;
   const size_t es = dtype_size(a->dtype), bytes = (size_t)a->M * a->d * es;
@@ -521,12 +594,12 @@ static gtr_status ln_bwd_check(const gtr_layernorm_bwd_args* a, bool pointers, s
       ln_misaligned(a->db, 4))
     return GTR_ERR_UNSUPPORTED;
   const bool sums = a->dw || a->db;
-  if (sums && (!a->workspace || ln_misaligned(a->workspace, 256) || a->workspace_bytes < *need))
+  if (sums && *need && (!a->workspace || ln_misaligned(a->workspace, 256) || a->workspace_bytes < *need))
     return GTR_ERR_WORKSPACE;
   const LnRange ins[] = {{a->dy, bytes}, {a->x, bytes}, {a->dres, bytes}, {a->mean, (size_t)a->M * 4},
                          {a->rstd, (size_t)a->M * 4}, {a->w, (size_t)a->d * 4}};
   const LnRange outs[] = {{a->dx, bytes}, {a->dw, (size_t)a->d * 4}, {a->db, (size_t)a->d * 4},
-                          {sums ? a->workspace : nullptr, *need}};
+                          {sums && *need ? a->workspace : nullptr, *need}};
   for (int i = 0; i < 4; ++i) {
     for (int j = 0; j < 6; ++j)
       if (ln_overlap(outs[i], ins[j]) && !(i == 0 && j < 3 && outs[i].p == ins[j].p)) return GTR_ERR_ALIAS;
@@ -574,16 +647,20 @@ extern "C" gtr_status gtr_layernorm_bwd(const gtr_layernorm_bwd_args* a, hipStre
   if (st != GTR_OK) return st;
   const LnShape s = ln_shape(a->d, a->dtype);
   const int64_t G = ln_bwd_groups(a->M, s);
-  const bool sums = a->dw || a->db;
-  const LnBwd p = {static_cast<const char*>(a->dy), static_cast<const char*>(a->x), a->mean, a->rstd, a->w,
-                   static_cast<const char*>(a->dres), static_cast<char*>(a->dx),
-                   sums ? static_cast<float*>(a->workspace) : nullptr, a->M, a->d};
-  const gtr_status run = ln_launch(a->dtype, LnLaunch<LnBwd>{p, s, (unsigned)G, stream});
-  if (run != GTR_OK) return run;
-  if (sums) {
-    hipLaunchKernelGGL(ln_reduce_kernel, dim3((unsigned)((2 * (int64_t)a->d + 31) / 32)), dim3(1024), 0, stream, p.part,
-                       (int)G, a->d, a->dw, a->db, a->accumulate);
-    if (hipGetLastError() != hipSuccess) return GTR_ERR_HIP;
+  const bool sums = a->dw || a->db, columns = sums && ln_by_columns(a);
+  LnBwd p = {static_cast<const char*>(a->dy), static_cast<const char*>(a->x), a->mean, a->rstd, a->w,
+             static_cast<const char*>(a->dres), static_cast<char*>(a->dx),
+             sums && !columns ? static_cast<float*>(a->workspace) : nullptr, a->M, a->d, 0, a->dw, a->db, a->accumulate};
+  int64_t grid = G;
+  if (columns) {
+    const int VE = a->dtype == GTR_F32 ? 4 : 8;
+    // (without dx the rows have nothing to do, but a launch has a work-group for them)
+    p.rows = a->dx ? (int)G : 1;
+    grid = p.rows + (a->d + 2 * VE - 1) / (2 * VE);
   }
-  return GTR_OK;
+  const gtr_status run = ln_launch(a->dtype, LnLaunch<LnBwd>{p, s, (unsigned)grid, stream});
+  if (run != GTR_OK || !sums || columns) return run;
+  hipLaunchKernelGGL(ln_reduce_kernel, dim3((unsigned)((2 * (int64_t)a->d + 31) / 32)), dim3(1024), 0, stream, p.part,
+                     (int)G, a->d, a->dw, a->db, a->accumulate);
+  return hipGetLastError() == hipSuccess ? GTR_OK : GTR_ERR_HIP;
 }

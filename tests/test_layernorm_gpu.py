@@ -114,7 +114,8 @@ def test_options(gtr, dtype):
 @pytest.mark.parametrize("M,d", [(40, 384), (6, 3001), (3, 12293)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
 def test_in_place_and_repeatable(gtr, M, d, dtype):
-    """The output over each input that it may be, bit for bit as beside them; the same call again, bit for bit."""
+    """The output over each input that it may be, bit for bit as beside them (the weights' gradients, which are summed
+    another way where dx overwrites what they are formed from, within their bounds); the same call again, bit for bit."""
     x, w, b, dy, dres = inputs(M, d, dtype, 3)
     y, mean, rstd = gtr.gtr_layernorm_fwd(x, w, b)
     assert torch.equal(gtr.gtr_layernorm_fwd(z := x.clone(), w, b, out=z)[0], y)
@@ -122,7 +123,10 @@ def test_in_place_and_repeatable(gtr, M, d, dtype):
     for k in range(3):
         t = [dy.clone(), x.clone(), dres.clone()]
         got = gtr.gtr_layernorm_bwd(t[0], t[1], mean, rstd, w, dres=t[2], out=t[k])
-        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert torch.equal(got[0], want[0])
+        check_backward(got, dy, x, w, dres)
+    again = gtr.gtr_layernorm_bwd(dy, x, mean, rstd, w, dres=dres)
+    assert all(torch.equal(a, b) for a, b in zip(again, want))
 
 
 @pytest.mark.parametrize("shift", [100.0, 3000.0])
