@@ -79,16 +79,16 @@ struct FfnVec {
   }
   template <int DT>
   static __device__ __forceinline__ FfnVec pack(const float (&x)[N]) {
+    typedef _Float16 hh __attribute__((ext_vector_type(2)));
+    typedef __bf16 bb __attribute__((ext_vector_type(2)));
     FfnVec r;
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) {
-      if constexpr (DT == GTR_F16) {
-        r.v[e] = __builtin_bit_cast(unsigned short, (_Float16)x[2 * e]) |
-                 (unsigned)__builtin_bit_cast(unsigned short, (_Float16)x[2 * e + 1]) << 16;
-      } else {
-        r.v[e] = __builtin_bit_cast(unsigned short, (__bf16)x[2 * e]) |
-                 (unsigned)__builtin_bit_cast(unsigned short, (__bf16)x[2 * e + 1]) << 16;
-      }
+    for (int e = 0; e < N / 2; ++e) {  // pairs, which convert in one instruction
+      const f2 p = {x[2 * e], x[2 * e + 1]};
+      if constexpr (DT == GTR_F16)
+        r.v[e] = __builtin_bit_cast(unsigned, __builtin_convertvector(p, hh));
+      else
+        r.v[e] = __builtin_bit_cast(unsigned, __builtin_convertvector(p, bb));
     }
     return r;
   }
@@ -102,15 +102,30 @@ struct FfnVec {
 
 // act(g) and its derivative. SiLU: g s(g), s(g) (1 + g (1 - s(g))), s the logistic
 // function; GELU: g P(g), P(g) + g phi(g), P and phi the normal distribution
-// function and its density.
+// function and its density. The tail Q(x) = 1 - P(x), x = |g|, is taken as exp(-x^2 /
+// 2) t R(t) with t = 1 / (1 + 3 x / 8): Q(x) exp(x^2 / 2) / t is smooth over 0 < t <= 1,
+// and R is the polynomial of degree 8 that fits it there by least squares, reweighted
+// towards the least largest relative error: 2.2e-7, in float32 5e-7, at any x. It
+// shares its exponential with the density. (The library's erfc cost 16 us of 101 in
+// the forward pass of 12800 x 384 x 1536.)
 __device__ __forceinline__ float ffn_act(float g, int act, float& slope) {
   if (act == GTR_ACT_SILU) {
     const float p = __builtin_amdgcn_rcpf(1.f + __expf(-g));
     slope = p * fmaf(g, 1.f - p, 1.f);
     return g * p;
   }
-  const float p = 0.5f * erfcf(g * -0.70710678118654752f);  // (1 + erf would lose the lower tail)
-  slope = fmaf(g * 0.39894228040143268f, __expf(-0.5f * g * g), p);
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.375f, 1.f)), e = __expf(-0.5f * g * g);
+  float r = -0.0329110212624073f;
+  r = fmaf(r, t, 0.13687977194786072f);
+  r = fmaf(r, t, -0.18652084469795227f);
+  r = fmaf(r, t, 0.050631992518901825f);
+  r = fmaf(r, t, 0.015628185123205185f);
+  r = fmaf(r, t, 0.08863813430070877f);
+  r = fmaf(r, t, 0.12844571471214294f);
+  r = fmaf(r, t, 0.14960458874702454f);
+  r = fmaf(r, t, 0.14960338175296783f);
+  const float q = e * t * r, p = g < 0.f ? q : 1.f - q;
+  slope = fmaf(g * 0.39894228040143268f, e, p);
   return g * p;
 }
 
