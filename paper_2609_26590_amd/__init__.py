@@ -624,6 +624,12 @@ def _is(t: Optional[torch.Tensor], shape, dtype, index: int) -> bool:
     return t is None or (t.shape == shape and t.dtype == dtype and t.get_device() == index and t.is_contiguous())
 
 
+def _vector(t: Optional[torch.Tensor], d: int, index: int) -> bool:
+    """_is for a float32 vector of d."""
+    return t is None or (t.numel() == d and t.dim() == 1 and t.dtype is torch.float32 and t.get_device() == index and
+                         t.is_contiguous())
+
+
 def _rows(name: str, t: torch.Tensor) -> None:
     _dev_contig(name, t)
     if t.dim() < 1 or t.dtype not in _DT:
@@ -644,26 +650,33 @@ def gtr_layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bi
     """Layer normalisation over the last dimension of x (float32, fp16 or bf16; any width up to 16384) that keeps the
     rows' statistics. weight, bias [d] float32. ``out`` may be x. Returns ``(y, mean, rstd)``, the statistics float32 of
     shape x.shape[:-1]."""
+    if stream is None and x.is_cuda and x.get_device() == torch._C._cuda_getDevice():
+        return _layernorm_fwd(x, weight, bias, eps, out, mean, rstd)
     _rows("x", x)
     return _on_stream(_layernorm_fwd, stream, (x, weight, bias, out, mean, rstd), (x, weight, bias, eps, out, mean, rstd))
 
 
 def _layernorm_fwd(x, weight, bias, eps, y, mu, rs):
-    shape, dev, dt = x.shape, x.device, x.dtype
+    shape, dev, dt, f32 = x.shape, x.device, x.dtype, torch.float32
+    code = _DT.get(dt)
+    if code is None or not shape or not x.is_contiguous():
+        _rows("x", x)
     d, rows, index = shape[-1], shape[:-1], dev.index
     if y is None:
         y = torch.empty_like(x)
     if mu is None:
-        mu = torch.empty(rows, dtype=torch.float32, device=dev)
+        mu = torch.empty(rows, dtype=f32, device=dev)
     if rs is None:
-        rs = torch.empty(rows, dtype=torch.float32, device=dev)
-    if not (_is(y, shape, dt, index) and _is(weight, (d,), torch.float32, index) and
-            _is(bias, (d,), torch.float32, index) and _is(mu, rows, torch.float32, index) and
-            _is(rs, rows, torch.float32, index)):
+        rs = torch.empty(rows, dtype=f32, device=dev)
+    # one expression for the call that is right (the checks one by one cost 2 us of 7); a wrong one is told by _check
+    if not (y.shape == shape and mu.shape == rows and rs.shape == rows and y.dtype is dt and mu.dtype is f32 and
+            rs.dtype is f32 and y.get_device() == index and mu.get_device() == index and rs.get_device() == index and
+            y.is_contiguous() and mu.is_contiguous() and rs.is_contiguous() and _vector(weight, d, index) and
+            _vector(bias, d, index)):
         _check("out", y, shape, (dt,), dev)
         for name, t, want in (("weight", weight, (d,)), ("bias", bias, (d,)), ("mean", mu, rows), ("rstd", rs, rows)):
-            _check(name, t, want, (torch.float32,), dev)
-    a = LayernormFwdArgs(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mu.data_ptr(), rs.data_ptr(), _DT[dt], d,
+            _check(name, t, want, (f32,), dev)
+    a = LayernormFwdArgs(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mu.data_ptr(), rs.data_ptr(), code, d,
                          x.numel() // d if d else 0, eps)
     st = load().gtr_layernorm_fwd(ctypes.byref(a), torch._C._cuda_getCurrentRawStream(index))
     if st:
@@ -679,19 +692,26 @@ def gtr_layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rst
     """Gradients of :func:`gtr_layernorm_fwd`: ``(dx, dw, db)``, dx in x's type, dw and db [d] float32 summed over the
     rows. ``dres`` (x's shape and type, a residual path's gradient) is added to dx. ``out`` (for dx) may be dy, x or
     dres. ``accumulate``: dw and db are added to what the given ``dw`` and ``db`` hold. What is not wanted is None."""
-    _rows("x", x)
     if accumulate and want_dw and (dw is None or db is None):
         raise ValueError("accumulate needs dw and db")
+    if stream is None and x.is_cuda and x.get_device() == torch._C._cuda_getDevice():
+        return _layernorm_bwd(dy, x, mean, rstd, weight, dres, want_dx, want_dw, out, dw, db, accumulate, workspace)
+    _rows("x", x)
     return _on_stream(_layernorm_bwd, stream, (x, dy, mean, rstd, weight, dres, out, dw, db),
                       (dy, x, mean, rstd, weight, dres, want_dx, want_dw, out, dw, db, accumulate, workspace))
 
 
 def _layernorm_bwd(dy, x, mean, rstd, weight, dres, want_dx, want_dw, dx, dw, db, accumulate, workspace):
-    shape, dev, dt = x.shape, x.device, x.dtype
-    d, rows, index, f32 = shape[-1], shape[:-1], dev.index, torch.float32
-    if not (_is(dy, shape, dt, index) and _is(dres, shape, dt, index) and _is(dx, shape, dt, index) and
-            _is(mean, rows, f32, index) and _is(rstd, rows, f32, index) and _is(weight, (d,), f32, index) and
-            _is(dw, (d,), f32, index) and _is(db, (d,), f32, index)):
+    shape, dev, dt, f32 = x.shape, x.device, x.dtype, torch.float32
+    code = _DT.get(dt)
+    if code is None or not shape or not x.is_contiguous():
+        _rows("x", x)
+    d, rows, index = shape[-1], shape[:-1], dev.index
+    if not (dy.shape == shape and dy.dtype is dt and dy.get_device() == index and dy.is_contiguous() and
+            mean.shape == rows and rstd.shape == rows and mean.dtype is f32 and rstd.dtype is f32 and
+            mean.get_device() == index and rstd.get_device() == index and mean.is_contiguous() and
+            rstd.is_contiguous() and _is(dres, shape, dt, index) and _is(dx, shape, dt, index) and
+            _vector(weight, d, index) and _vector(dw, d, index) and _vector(db, d, index)):
         for name, t in (("dy", dy), ("dres", dres), ("out", dx)):
             _check(name, t, shape, (dt,), dev)
         for name, t, want in (("mean", mean, rows), ("rstd", rstd, rows), ("weight", weight, (d,)), ("dw", dw, (d,)),
@@ -707,7 +727,7 @@ def _layernorm_bwd(dy, x, mean, rstd, weight, dres, want_dx, want_dw, dx, dw, db
         dw = torch.empty(d, dtype=f32, device=dev) if dw is None else dw
         db = torch.empty(d, dtype=f32, device=dev) if db is None else db
     a = LayernormBwdArgs(dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), _ptr(dres),
-                         _ptr(dx), _ptr(dw), _ptr(db), _DT[dt], d, x.numel() // d if d else 0, bool(accumulate))
+                         _ptr(dx), _ptr(dw), _ptr(db), code, d, x.numel() // d if d else 0, bool(accumulate))
     lib, ref = load(), ctypes.byref(a)
     need = lib.gtr_layernorm_bwd_workspace_size(ref) if want_dw else 0
     if need:
@@ -720,15 +740,20 @@ def _layernorm_bwd(dy, x, mean, rstd, weight, dres, want_dx, want_dw, dx, dw, db
 
 
 def _ffn_shape(x, w_gate, w_value, w_out) -> tuple:
-    dt, dev = x.dtype, x.device
-    if dt == torch.float32:
+    dt, shape, dev = x.dtype, x.shape, x.device
+    if dt not in _DT or not shape or not x.is_contiguous():
+        _rows("x", x)
+    if dt is torch.float32:
         raise ValueError("x must be float16 or bfloat16")
-    d, hidden, index = x.shape[-1], w_gate.shape[0], dev.index
-    if not (_is(w_gate, (hidden, d), dt, index) and _is(w_value, (hidden, d), dt, index) and
-            _is(w_out, (d, hidden), dt, index)):
-        _check("w_gate", w_gate, (hidden, d), (dt,), dev)
-        _check("w_value", w_value, (hidden, d), (dt,), dev)
-        _check("w_out", w_out, (d, hidden), (dt,), dev)
+    d, hidden, index = shape[-1], w_gate.shape[0], dev.index
+    up, down = (hidden, d), (d, hidden)
+    if not (w_gate.shape == up and w_value.shape == up and w_out.shape == down and w_gate.dtype is dt and
+            w_value.dtype is dt and w_out.dtype is dt and w_gate.get_device() == index and
+            w_value.get_device() == index and w_out.get_device() == index and w_gate.is_contiguous() and
+            w_value.is_contiguous() and w_out.is_contiguous()):
+        _check("w_gate", w_gate, up, (dt,), dev)
+        _check("w_value", w_value, up, (dt,), dev)
+        _check("w_out", w_out, down, (dt,), dev)
     return d, hidden, x.numel() // d if d else 0
 
 
@@ -747,6 +772,8 @@ def gtr_ffn_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Tensor, w_
     x [..., d] (fp16 or bf16), w_gate and w_value [hidden, d], w_out [d, hidden] (same type; d and hidden multiples of
     8), ``residual`` of x's shape and type (may be ``out``). ``act``: "silu" or "gelu". Returns ``(y, gate, value)``:
     the two projections [..., hidden] for :func:`gtr_ffn_bwd` with ``save`` (or where given), else None."""
+    if stream is None and x.is_cuda and x.get_device() == torch._C._cuda_getDevice():
+        return _ffn_fwd(x, w_gate, w_value, w_out, _act(act), residual, save, out, gate, value, workspace)
     _rows("x", x)
     return _on_stream(_ffn_fwd, stream, (x, w_gate, w_value, w_out, residual, out, gate, value),
                       (x, w_gate, w_value, w_out, _act(act), residual, save, out, gate, value, workspace))
@@ -790,9 +817,12 @@ def gtr_ffn_bwd(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_value
 
     The weights' gradients are in ``dw_dtype`` (x's type, the default, or float32) or in that of the tensors given;
     ``accumulate`` adds to what those hold. The residual's gradient is dy itself. What is not wanted is None."""
-    _rows("x", x)
     if accumulate and want_dw and (dw_gate is None or dw_value is None or dw_out is None):
         raise ValueError("accumulate needs dw_gate, dw_value and dw_out")
+    if stream is None and x.is_cuda and x.get_device() == torch._C._cuda_getDevice():
+        return _ffn_bwd(dy, x, w_gate, w_value, w_out, gate, value, _act(act), want_dx, want_dw, dw_dtype, out, dw_gate,
+                        dw_value, dw_out, accumulate, workspace)
+    _rows("x", x)
     return _on_stream(_ffn_bwd, stream, (x, dy, w_gate, w_value, w_out, gate, value, out, dw_gate, dw_value, dw_out),
                       (dy, x, w_gate, w_value, w_out, gate, value, _act(act), want_dx, want_dw, dw_dtype, out, dw_gate,
                        dw_value, dw_out, accumulate, workspace))
