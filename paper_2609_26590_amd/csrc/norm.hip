@@ -284,7 +284,7 @@ struct LnBwd {
 // cache, and the call is one launch.
 template <int DT, bool TINY>
 __device__ __forceinline__ void ln_columns(const LnBwd& g, int pair) {
-  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES, U = 4;
+  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES, U = 8;
   __shared__ float sums[kLnWaves][2][2 * VE];
   const LnCols<DT, TINY> k(2 * pair + (threadIdx.x & 1), g.d);
   const int lanes = blockDim.x / 2;  // rows at a time
@@ -513,12 +513,13 @@ static int64_t ln_bwd_groups(int64_t M, const LnShape& s) {
 }
 
 // Whether dw and db are summed by columns: where a batch is short, its second reading
-// comes from cache, and dx does not overwrite what is read. 1600 x 384 fp16, calls one
-// after the other: 11.2 us
-// against 12.9 with partial sums and their launch; 2000 x 1024 17.5 against 13.0.
+// comes from cache in one or two round trips, and dx does not overwrite what is read.
+// Calls one after the other against partial sums and their launch, us: 64 x 384 fp16
+// 8.4 / 12.8, 777 x 1001 float32 8.9 / 12.4, 1600 x 192 bf16 8.8 / 12.5, 1600 x 384
+// 12.3 / 12.6; but 2000 x 384 13.5 / 12.6.
 static bool ln_by_columns(const gtr_layernorm_bwd_args* a) {
-  return a->M <= 2048 && a->M * a->d * (int64_t)dtype_size(a->dtype) <= 3 << 20 &&
-         !(a->dx && (a->dx == a->dy || a->dx == a->x));
+  const int64_t bytes = a->M * a->d * (int64_t)dtype_size(a->dtype);
+  return a->M <= 2048 && bytes <= (a->M <= 1024 ? 12 << 18 : 5 << 18) && !(a->dx && (a->dx == a->dy || a->dx == a->x));
 }
 
 template <class P>
