@@ -240,16 +240,18 @@ constexpr int kFfnLds = 2 * (BM + BN) * 128;
 // whole step before it is read again: its transfer has three parts' time to
 // arrive.
 //
-// What the epilogue reads (a residual, the projections) is fetched before the
-// products where the registers have room for it (tiles under 256 x 256: short
-// products, whose epilogue would wait for it), else before the epilogue, half of it
-// at a time.
+// What the epilogue reads (a residual, the projections) is fetched before the first of
+// it is used, a half's rows at a time. (Fetched before the products, where the small
+// tiles have the registers, it came out the same: 1600 x 192 x 768 backward 23.2 us
+// against 23.0.)
 //
 // b: the work-group's number of T, in the order of dispatch. Work-group b runs on XCD
 // b % 8 (round-robin dispatch); each XCD takes a contiguous range of the tiles, in
-// groups of 8 row tiles, rows fastest: a patch of 8 x 4 tiles that share operands runs
-// on an XCD's 32 CUs at a time.
-template <int DT, int TA, int TB, int EPI, int BM, int BN, int WM, int WN>
+// groups of 4 row tiles, rows fastest: a patch of 4 x 8 tiles that share operands runs
+// on an XCD's 32 CUs at a time (8192 x 4096 x 11008 forward 1568 us; in groups of 8
+// 1591, of 16 some 3 % more).
+// MANY: the launch may have several products.
+template <int DT, int TA, int TB, int EPI, int BM, int BN, int WM, int WN, bool MANY>
 __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, int T) {
   typedef Operand<DT, DT> Op;
   constexpr int NW = WM * WN;
@@ -269,19 +271,23 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
   // work-group -> tile
   const int xcd = b & 7, slot = b >> 3;
   int jt = xcd * (T >> 3) + min(xcd, T & 7) + slot;
-  const int per = T / g.ksplit, bz = jt / per;
-  jt -= bz * per;
-  int pi = 0;
-  while (pi + 1 < g.nprod && jt >= g.p[pi].gx * g.p[pi].gy) jt -= g.p[pi].gx * g.p[pi].gy, ++pi;
+  int bz = 0, pi = 0;
+  if (EPI == kFfnStore && g.ksplit > 1) {
+    const int per = T / g.ksplit;
+    bz = jt / per;
+    jt -= bz * per;
+  }
+  if (MANY)
+    while (pi + 1 < g.nprod && jt >= g.p[pi].gx * g.p[pi].gy) jt -= g.p[pi].gx * g.p[pi].gy, ++pi;
   const FfnProd& p = g.p[pi];
-  constexpr int GM = 8;
+  constexpr int GM = 4;
   const int grp = jt / (GM * p.gy), first = grp * GM, gsz = min(p.gx - first, GM), in = jt - grp * GM * p.gy;
   const int bx = first + in % gsz, by = in / gsz;
   const int mb = bx * BM, nb = by * BC;
 
   // K steps of this slice; a segment has `sps` steps
   const int K = p.K, sps = (K + 63) / 64, all = sps * p.nseg;
-  const int s_per = (all + g.ksplit - 1) / g.ksplit;
+  const int s_per = EPI == kFfnStore && g.ksplit > 1 ? (all + g.ksplit - 1) / g.ksplit : all;
   const int s0 = bz * s_per, steps = max(0, min(s0 + s_per, all) - s0);
 
   unsigned va[2][LA::P], vb[2][LB::P];  // byte offsets of this lane's transfers
@@ -436,6 +442,29 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
   };
   static_assert(PL <= ROWS / 2 * DR, "a part's transfers are issued before its step's descriptors change");
 
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    next();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      unsigned l = half_at(k, h);
+#pragma unroll
+      for (int q = 0; q < PL; ++q) transfer(l, h, q);
+    }
+  }
+  next();
+  ring_wait<2 * PL>();
+#pragma unroll
+  for (int q = 0; q < 2 * TI; ++q) read_a(0, q);
+#pragma unroll
+  for (int q = 0; q < 2 * TJ; ++q) read_b(0, q);
+  ring_sync();
+  for (int k = 0; k < steps; ++k) {
+    part(0, k & 1);
+    part(1, k & 1);
+  }
+  ring_wait<0>();  // no transfer is in flight when the work-group ends
+
   // Lane (r16, kq) holds, of an MFMA tile of C, row r16 and columns 4 kq .. 4 kq + 3.
   // Two column tiles side by side exchange lane rows, so that it holds 8 consecutive
   // columns of one of them: 16 (kq % 2) + 8 (kq / 2) .. + 7 of the pair.
@@ -461,8 +490,7 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
   const auto rres = tile_of(EPI == kFfnStore && !cut ? p.res : nullptr);
   const auto rg = tile_of(g.gate), rl = tile_of(g.value), rdg = tile_of(g.dgate), rdl = tile_of(g.dvalue);
   const bool res32 = EPI == kFfnStore && p.res && !cut && cdt == GTR_F32, res16 = EPI == kFfnStore && p.res && !cut && cdt != GTR_F32;
-  constexpr bool EARLY = BM < 256;
-  FfnVec<CW> e0[EARLY ? 2 : 1][TI][2 * NQ], e1[EARLY ? 2 : 1][TI][2 * NQ];  // what the epilogue reads
+  FfnVec<CW> e0[TI][2 * NQ], e1[TI][2 * NQ];  // what the epilogue reads
   auto at = [&](int h, int i, int q) {
     return (unsigned)((h * HM + wm + 16 * i + r16) * (int)ldc) * es + col[DUAL ? 0 : q / NQ][q % NQ];
   };
@@ -474,46 +502,18 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
         for (int q = 0; q < 2 * NQ; ++q) {
           const unsigned o = at(h, i, q);
           if constexpr (EPI == kFfnGateGrad) {
-            e0[EARLY ? h : 0][i][q].load(rg, o);
-            e1[EARLY ? h : 0][i][q].load(rl, o);
+            e0[i][q].load(rg, o);
+            e1[i][q].load(rl, o);
           } else {
-            e0[EARLY ? h : 0][i][q].load(rres, o);
-            if (res32) e1[EARLY ? h : 0][i][q].load(rres, o + CW * 2);
+            e0[i][q].load(rres, o);
+            if (res32) e1[i][q].load(rres, o + CW * 2);
           }
         }
     }
   };
-  if (EARLY) {
-    fetch(0);
-    fetch(1);
-  }
-
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    next();
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      unsigned l = half_at(k, h);
-#pragma unroll
-      for (int q = 0; q < PL; ++q) transfer(l, h, q);
-    }
-  }
-  next();
-  ring_wait<2 * PL>();
-#pragma unroll
-  for (int q = 0; q < 2 * TI; ++q) read_a(0, q);
-#pragma unroll
-  for (int q = 0; q < 2 * TJ; ++q) read_b(0, q);
-  ring_sync();
-  for (int k = 0; k < steps; ++k) {
-    part(0, k & 1);
-    part(1, k & 1);
-  }
-  ring_wait<0>();  // no transfer is in flight when the work-group ends
-
 #pragma unroll
   for (int h = 0; h < 2; ++h) {  // the rows of A_h
-    if (!EARLY) fetch(h);
+    fetch(h);
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
       float x[2][NQ][CW];
@@ -547,8 +547,8 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
           const unsigned o = at(h, i, q);
           if constexpr (EPI == kFfnGateGrad) {
             float gt[CW], vl[CW], dg[CW], dv[CW], hh[CW];
-            e0[EARLY ? h : 0][i][q].template unpack<DT>(gt);
-            e1[EARLY ? h : 0][i][q].template unpack<DT>(vl);
+            e0[i][q].template unpack<DT>(gt);
+            e1[i][q].template unpack<DT>(vl);
 #pragma unroll
             for (int e = 0; e < CW; ++e) {
               float s;
@@ -563,13 +563,13 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
           } else {
             if (res16) {
               float r[CW];
-              e0[EARLY ? h : 0][i][q].template unpack<DT>(r);
+              e0[i][q].template unpack<DT>(r);
 #pragma unroll
               for (int e = 0; e < CW; ++e) v[e] += r[e];
             }
             if (res32) {
 #pragma unroll
-              for (int e = 0; e < CW; ++e) v[e] += e < CW / 2 ? e0[EARLY ? h : 0][i][q].f32(e) : e1[EARLY ? h : 0][i][q].f32(e - CW / 2);
+              for (int e = 0; e < CW; ++e) v[e] += e < CW / 2 ? e0[i][q].f32(e) : e1[i][q].f32(e - CW / 2);
             }
             if (cdt == GTR_F32) {
               FfnVec<CW>::bits(v).store(rc, o);
@@ -587,7 +587,7 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
 template <int DT, int TA, int TB, int EPI, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(2))) ffn_gemm_kernel(FfnGemm g) {
   __shared__ __attribute__((aligned(1024))) char ring[kFfnLds<BM, BN>];
-  ffn_tile<DT, TA, TB, EPI, BM, BN, WM, WN>(g, ring, blockIdx.x, gridDim.x);
+  ffn_tile<DT, TA, TB, EPI, BM, BN, WM, WN, false>(g, ring, blockIdx.x, gridDim.x);
 }
 
 // The gradients of the input and of the weights in one launch: neither needs the
@@ -603,9 +603,9 @@ ffn_grad_kernel(FfnGemm dx, FfnGemm dw, int nx, int nw, int x_first) {
   const int b = head ? blockIdx.x : blockIdx.x - r0;
   if (head && b >= n0) return;
   if (head == (x_first != 0))
-    ffn_tile<DT, 0, 1, kFfnStore, BM, BN, WM, WN>(dx, ring, b, nx);
+    ffn_tile<DT, 0, 1, kFfnStore, BM, BN, WM, WN, false>(dx, ring, b, nx);
   else
-    ffn_tile<DT, 1, 1, kFfnStore, BM, BN, WM, WN>(dw, ring, b, nw);
+    ffn_tile<DT, 1, 1, kFfnStore, BM, BN, WM, WN, true>(dw, ring, b, nw);
 }
 
 // C = the sum of the slices' partial sums (+ res), 8 elements per thread: of g, then
