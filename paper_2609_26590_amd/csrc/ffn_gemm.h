@@ -611,9 +611,16 @@ ffn_grad_kernel(FfnGemm dx, FfnGemm dw, int nx, int nw, int x_first) {
 // C = the sum of the slices' partial sums (+ res), 8 elements per thread: of g, then
 // of h.
 __device__ __forceinline__ void ffn_reduce(const FfnGemm& g, int64_t t) {
-  int pi = 0;
-  while (pi + 1 < g.nprod && t >= g.p[pi + 1].part_off) ++pi;
-  const FfnProd& p = g.p[pi];
+  char* c = g.p[0].c;
+  const char* res = g.p[0].res;
+  int64_t off = t;  // (C is contiguous)
+#pragma unroll
+  for (int i = 1; i < kFfnProds; ++i)
+    if (i < g.nprod && t >= g.p[i].part_off) {
+      c = g.p[i].c;
+      res = g.p[i].res;
+      off = t - g.p[i].part_off;
+    }
   float x[8];
   load8(g.part, GTR_F32, t, x);
 #pragma unroll 4
@@ -623,14 +630,13 @@ __device__ __forceinline__ void ffn_reduce(const FfnGemm& g, int64_t t) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] += y[e];
   }
-  const int64_t off = t - p.part_off;  // (C is contiguous)
-  if (p.res) {
+  if (res) {
     float y[8];
-    load8(p.res, g.cdt, off, y);
+    load8(res, g.cdt, off, y);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] += y[e];
   }
-  store_n<8>(p.c, g.cdt, off, x);
+  store_n<8>(c, g.cdt, off, x);
 }
 __global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g, FfnGemm h) {
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
