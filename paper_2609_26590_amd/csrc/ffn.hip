@@ -241,12 +241,9 @@ static gtr_status ffn_sizes(int64_t M, int32_t d, int32_t hidden, int dt, int ac
 // ---------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------
-// Tokens up to which the forward pass runs in ffn_few_kernel (at most 16). Kernel
-// times of both launches, in tiles against there: 1 x 1024 x 2816 17.0 against 13.8
-// us, 1 x 192 x 768 13.1 against 9.2; 16 x 1024 x 2816 17.0 against 18.1, where the
-// tokens' rows are as many loads as a weight's.
-constexpr int kFfnFew = 8;
-
+// Up to kFewTokens tokens the forward pass runs in ffn_few_kernel, which has columns
+// for no more. Kernel times of both launches, in tiles against there: 1 x 1024 x 2816
+// 17.0 against 9.7 us, 1 x 192 x 768 13.1 against 6.6.
 template <int DT>
 static gtr_status ffn_run_few(const gtr_ffn_fwd_args* a, hipStream_t stream) {
   FfnFew up = {}, down = {};
@@ -264,8 +261,8 @@ static gtr_status ffn_run_few(const gtr_ffn_fwd_args* a, hipStream_t stream) {
   down.w[0] = static_cast<const char*>(a->w_out);
   down.c = static_cast<char*>(a->y);
   down.res = static_cast<const char*>(a->residual);
-  hipLaunchKernelGGL((ffn_few_kernel<DT, 2>), dim3((up.N + 15) / 16), dim3(512), 0, stream, up);
-  hipLaunchKernelGGL((ffn_few_kernel<DT, 1>), dim3((down.N + 15) / 16), dim3(512), 0, stream, down);
+  hipLaunchKernelGGL((ffn_few_kernel<DT, 2>), dim3((up.N + 7) / 8), dim3(64 * few_waves(2)), 0, stream, up);
+  hipLaunchKernelGGL((ffn_few_kernel<DT, 1>), dim3((down.N + 7) / 8), dim3(64 * few_waves(1)), 0, stream, down);
   return hipGetLastError() == hipSuccess ? GTR_OK : GTR_ERR_HIP;
 }
 
@@ -283,7 +280,7 @@ static void ffn_fwd_plan(const gtr_ffn_fwd_args* a, FfnFwdPlan* f) {
   f->pu = ffn_plan(&f->up, 1, kRowRow, kFfnGate);
   f->pd = ffn_plan(&f->down, 1, kRowRow, kFfnStore);
   f->h_bytes = ffn_align((size_t)a->M * a->hidden * 2);
-  f->total = f->h_bytes + (a->M > kFfnFew && f->pd.ksplit > 1 ? ffn_align((size_t)f->pd.ksplit * a->M * a->d * 4) : 0);
+  f->total = f->h_bytes + (a->M > kFewTokens && f->pd.ksplit > 1 ? ffn_align((size_t)f->pd.ksplit * a->M * a->d * 4) : 0);
 }
 
 static gtr_status ffn_fwd_check(const gtr_ffn_fwd_args* a, const FfnFwdPlan& f) {
@@ -391,7 +388,7 @@ extern "C" gtr_status gtr_ffn_fwd(const gtr_ffn_fwd_args* a, hipStream_t stream)
   ffn_fwd_plan(a, &f);
   st = ffn_fwd_check(a, f);
   if (st != GTR_OK) return st;
-  if (a->M <= kFfnFew) return a->dtype == GTR_F16 ? ffn_run_few<GTR_F16>(a, stream) : ffn_run_few<GTR_BF16>(a, stream);
+  if (a->M <= kFewTokens) return a->dtype == GTR_F16 ? ffn_run_few<GTR_F16>(a, stream) : ffn_run_few<GTR_BF16>(a, stream);
   char* h = static_cast<char*>(a->workspace);
   FfnGemm g = {};
   g.nprod = 1;

@@ -648,12 +648,26 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g, FfnGemm h) {
 }
 
 // ---------------------------------------------------------------------------
-// A few tokens (up to 16): the weights' bytes are the work, each read once. A
-// work-group takes 16 columns of C; its waves take the 64-deep pieces of K in turn,
-// U of them in flight, and multiply a weight's 16 rows (one 16-byte load per lane and
-// 32 K elements, straight into the MFMA operand) with the tokens' rows, which stay in
-// cache. The waves' sums meet in LDS and are added in their order.
+// A few tokens (up to kFewTokens): the weights' bytes are the work, each read once,
+// and the time is how soon all of them are asked for. A work-group takes 8 columns of
+// C, half of what the matrix instruction has rows for, so that a narrow product still
+// covers the chip (1,024 columns: 128 work-groups instead of 64). The other 8 rows
+// take the same weights' next 32 K elements, and the other 8 of its columns the same
+// tokens' there: of the four 8x8 blocks of the result the two on the diagonal are
+// halves of the sum, the other two mean nothing. A lane's 16-byte load is its part of
+// the operand as it stands; a weight's row is read 128 bytes at a time. The waves take
+// the 64-deep pieces of K in turn, kFewFlight of them asked for at once, the tokens'
+// rows come from cache, and the waves' sums meet in LDS and are added in their order.
+// One token, bf16, gated and down product in us, against 16 columns each with eight
+// waves and four pieces in flight: 192 x 768 3.3 + 3.3 (was 4.3 + 4.7), 1024 x 2816
+// 5.3 + 4.4 (7.4 + 7.2), 2048 x 5632 10.7 + 5.7 (13.7 + 8.6), 4096 x 11008 37.9 +
+// 20.3 (44.3 + 22.8: 4.8 and 4.4 TB/s). Two weights with eight waves and one piece in
+// flight: 5.6 and 39.7 at the second and the last; with more in flight the registers
+// leave fewer work-groups on a CU.
 // ---------------------------------------------------------------------------
+constexpr int kFewTokens = 8;
+constexpr int few_waves(int nb) { return nb == 1 ? 8 : 4; }
+constexpr int kFewFlight = 2;
 struct FfnFew {
   const char* x;       // [M][K]
   const char* w[2];    // [N][K]: gate and value, or one weight
@@ -664,25 +678,25 @@ struct FfnFew {
 };
 
 template <int DT, int NB>
-__global__ void __launch_bounds__(512) ffn_few_kernel(FfnFew g) {
+__global__ void __launch_bounds__(64 * few_waves(NB)) ffn_few_kernel(FfnFew g) {
   typedef Operand<DT, DT> Op;
-  constexpr int U = 4, NW = 8;
+  constexpr int U = kFewFlight, NW = few_waves(NB);
   __shared__ f4 sums[NW][NB][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int r16 = lane & 15, kq = lane >> 4, n0 = blockIdx.x * 16;
+  const int r8 = lane & 7, half = (lane >> 3) & 1, kq = lane >> 4, n0 = blockIdx.x * 8;
   const int K = g.K, pieces = (K + 63) / 64;
   // this lane's rows; past the last one the last one again, which is not stored
-  const char *wr[NB], *xr = g.x + (int64_t)min(r16, g.M - 1) * K * 2;
+  const char *wr[NB], *xr = g.x + (int64_t)min(r8, g.M - 1) * K * 2;
 #pragma unroll
-  for (int b = 0; b < NB; ++b) wr[b] = g.w[b] + (int64_t)min(n0 + r16, g.N - 1) * K * 2;
+  for (int b = 0; b < NB; ++b) wr[b] = g.w[b] + (int64_t)min(n0 + r8, g.N - 1) * K * 2;
   f4 acc[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) acc[b] = f4{0.f, 0.f, 0.f, 0.f};
   for (int p = wave; p < pieces; p += NW * U) {
-    w4 fw[2 * U][NB], fx[2 * U];
+    w4 fw[U][NB], fx[U];
 #pragma unroll
-    for (int u = 0; u < 2 * U; ++u) {
-      const int k = 64 * (p + NW * (u >> 1)) + 32 * (u & 1) + 8 * kq;
+    for (int u = 0; u < U; ++u) {
+      const int k = 64 * (p + NW * u) + 32 * half + 8 * kq;
       const bool in = k < K;  // (K is a multiple of 8)
       const int64_t o = 2 * (int64_t)(in ? k : 0);
 #pragma unroll
@@ -694,21 +708,21 @@ __global__ void __launch_bounds__(512) ffn_few_kernel(FfnFew g) {
       if (!in) fx[u] = w4{0, 0, 0, 0};
     }
 #pragma unroll
-    for (int u = 0; u < 2 * U; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int b = 0; b < NB; ++b) acc[b] = mfma(Op::get(fw[u][b]), Op::get(fx[u]), acc[b]);
   }
 #pragma unroll
   for (int b = 0; b < NB; ++b) sums[wave][b][lane] = acc[b];
   __syncthreads();
-  const int m = r16, n = n0 + 4 * kq;  // columns n .. n + 3 of token m
-  if (threadIdx.x >= 64 || m >= g.M || n >= g.N) return;
+  const int m = r8, n = n0 + 4 * kq;  // columns n .. n + 3 of token m
+  if (threadIdx.x >= 32 || half || m >= g.M || n >= g.N) return;
   float s[NB][4];
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
-    f4 v = sums[0][b][lane];
+    f4 v = sums[0][b][lane] + sums[0][b][lane + 40];
 #pragma unroll
-    for (int i = 1; i < NW; ++i) v += sums[i][b][lane];
+    for (int i = 1; i < NW; ++i) v += sums[i][b][lane] + sums[i][b][lane + 40];
 #pragma unroll
     for (int e = 0; e < 4; ++e) s[b][e] = v[e];
   }

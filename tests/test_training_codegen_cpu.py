@@ -280,9 +280,9 @@ def test_ffn_few_addresses(M, K, N, two, dt):
     c, r, g, v = new("c", M * N * 2, "w"), new("res", M * N * 2, "r"), new("gate", M * N * 2, "w"), new("value", M * N * 2, "w")
     kern = struct.pack("<QQQQQQQiiii", x, w0, w1 if two else 0, c, 0 if two else r, g if two else 0, v if two else 0, M, N,
                        K, 1) + bytes(100)
-    blocks = -(-N // 16)
+    blocks = -(-N // 8)
     check_kernel(text, kernel_named(text, f"ffn_few_kernelILi{dt}ELi{2 if two else 1}E"), kern, new.regions,
-                 sorted({(0, 0, 0), (blocks - 1, 0, 0)}), 8)
+                 sorted({(0, 0, 0), (blocks - 1, 0, 0)}), 4 if two else 8)
 
 
 def bodies(text, sub):
