@@ -47,28 +47,19 @@ enum { kFfnStore = 0, kFfnGate = 1, kFfnGateGrad = 2 };
 // reads (12800 x 384 x 1536 fp16, both launches: 57.6 + 37.2 us -> 52.2 + 32.5).
 constexpr int kFfnLater = 2;
 
-// N (4 or 8) 16-bit elements, or N / 2 float32: what one load or store of a lane moves.
-template <int N>
+// What one load or store of a lane moves: 8 16-bit elements, or 4 float32.
 struct FfnVec {
-  typedef unsigned V __attribute__((ext_vector_type(N / 2)));
+  typedef unsigned V __attribute__((ext_vector_type(4)));
   V v;
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, unsigned off) {
-    if constexpr (N == 8)
-      v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
-    else
-      v = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
-  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, unsigned off) { v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0); }
   template <int AUX = 0>
   __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, unsigned off) const {
-    if constexpr (N == 8)
-      __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, AUX);
-    else
-      __builtin_amdgcn_raw_buffer_store_b64(v, r, off, 0, AUX);
+    __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, AUX);
   }
   template <int DT>
-  __device__ __forceinline__ void unpack(float (&x)[N]) const {
+  __device__ __forceinline__ void unpack(float (&x)[8]) const {
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) {
+    for (int e = 0; e < 4; ++e) {
       const unsigned u = v[e];
       if constexpr (DT == GTR_F16) {
         x[2 * e] = (float)__builtin_bit_cast(_Float16, (unsigned short)(u & 0xffffu));
@@ -84,12 +75,12 @@ struct FfnVec {
     return __builtin_bit_cast(float, u);
   }
   template <int DT>
-  static __device__ __forceinline__ FfnVec pack(const float (&x)[N]) {
+  static __device__ __forceinline__ FfnVec pack(const float (&x)[8]) {
     typedef _Float16 hh __attribute__((ext_vector_type(2)));
     typedef __bf16 bb __attribute__((ext_vector_type(2)));
     FfnVec r;
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) {  // pairs, which convert in one instruction
+    for (int e = 0; e < 4; ++e) {  // pairs, which convert in one instruction
       const f2 p = {x[2 * e], x[2 * e + 1]};
       if constexpr (DT == GTR_F16)
         r.v[e] = __builtin_bit_cast(unsigned, __builtin_convertvector(p, hh));
@@ -101,7 +92,7 @@ struct FfnVec {
   static __device__ __forceinline__ FfnVec bits(const float* x) {
     FfnVec r;
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) r.v[e] = __builtin_bit_cast(unsigned, x[e]);
+    for (int e = 0; e < 4; ++e) r.v[e] = __builtin_bit_cast(unsigned, x[e]);
     return r;
   }
 };
@@ -184,13 +175,15 @@ struct FfnTile {
     return BT == 128 ? m | q << 2 : BT == 64 ? m >> 1 | q << 1 : q;
   }
   // byte offset of this lane's piece of transfer c (0 .. BT / 8 - 1), and its first K element
+  // (MIX: of a half that is every second 16 of the tile's rows or columns)
+  template <bool MIX>
   static __device__ __forceinline__ unsigned voff(int c, int lane, int64_t ld) {
     if constexpr (T == 0) {
-      const int row = 8 * c + (lane >> 3);
-      return (unsigned)(row * (int)ld * 2) + 16u * ((lane & 7) ^ row_swz(row));
+      const int row = 8 * c + (lane >> 3), at = MIX ? row + (row & ~15) : row;
+      return (unsigned)(at * (int)ld * 2) + 16u * ((lane & 7) ^ row_swz(row));
     } else {
       const int k = RPC * c + lane / (BT / 8), p = lane % (BT / 8);
-      return (unsigned)(k * (int)ld * 2) + 32u * ((p >> 1) ^ unit_swz(k)) + 16u * (p & 1);
+      return (unsigned)(k * (int)ld * 2) + (MIX ? 64u : 32u) * ((p >> 1) ^ unit_swz(k)) + 16u * (p & 1);
     }
   }
   static __device__ __forceinline__ int piece_k(int c, int lane) {  // T = 0: K elements before this lane's piece
@@ -263,6 +256,8 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
   static_assert(2 * STAGE == kFfnLds<BM, BN>, "two stages");
   constexpr bool DUAL = EPI == kFfnGate;
   constexpr int BC = DUAL ? HN : BN;  // columns of C of a tile
+  constexpr bool MIX = TJ == 1 && !DUAL, PAIR = TJ == 1 && DUAL;
+  static_assert(TJ == 1 || TJ % 2 == 0, "MFMA tiles of C in pairs");
   static_assert(!DUAL || TB == 0, "the gated epilogue reads linear-layer weights");
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -295,10 +290,10 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
   for (int h = 0; h < 2; ++h) {
 #pragma unroll
     for (int q = 0; q < LA::P; ++q)
-      va[h][q] = LA::voff(wave + NW * q, lane, p.lda) + h * HM * 2 * (TA ? 1 : (unsigned)p.lda);
+      va[h][q] = LA::template voff<false>(wave + NW * q, lane, p.lda) + h * HM * 2 * (TA ? 1 : (unsigned)p.lda);
 #pragma unroll
     for (int q = 0; q < LB::P; ++q)
-      vb[h][q] = LB::voff(wave + NW * q, lane, p.ldb) + (DUAL ? 0 : h * HN * 2 * (TB ? 1 : (unsigned)p.ldb));
+      vb[h][q] = LB::template voff<MIX>(wave + NW * q, lane, p.ldb) + (DUAL ? 0 : h * (MIX ? 16 : HN) * 2 * (TB ? 1 : (unsigned)p.ldb));
   }
 
   // Descriptors of a step's operands: they end where the tile's rows do (rows along
@@ -466,12 +461,20 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
   ring_wait<0>();  // no transfer is in flight when the work-group ends
 
   // Lane (r16, kq) holds, of an MFMA tile of C, row r16 and columns 4 kq .. 4 kq + 3.
-  // Two column tiles side by side exchange lane rows, so that it holds 8 consecutive
-  // columns of one of them: 16 (kq % 2) + 8 (kq / 2) .. + 7 of the pair.
+  // Two tiles exchange lane rows, so that it holds 8 consecutive columns of one of them,
+  // 8 (kq / 2) .. + 7 of tile kq % 2. The two are side by side: column tiles of a half;
+  // where a wave has one of those, its tiles of the two halves (MIX: the halves take the
+  // tile's columns 16 by 16 in turn); and for the gated epilogue, where the halves are
+  // the two projections, the tiles of A0's and A1's rows (PAIR). (1600 x 192 x 768 with
+  // 4 columns per lane: gated product 7.8 us, now 7.0; gradients of the projections 12.4,
+  // now 11.0; 4150 rows 16.3, now 12.5. Halves that alternate in the larger tiles too, 32
+  // columns at a time, cost their transfers more than the stores gain: 12800 x 384 x
+  // 1536 gradients of the projections 63.8 us -> 67.9.)
   // Loads and stores go through descriptors of the tile's rows, columns past the last
   // out of range.
-  constexpr int CW = TJ % 2 ? 4 : 8, NQ = TJ * 4 / CW;  // consecutive columns of a lane, and how often in a half
-  const int cofs = CW == 8 ? 16 * (kq & 1) + 8 * (kq >> 1) : 4 * kq;
+  constexpr int NQ = TJ == 1 ? 1 : TJ / 2;       // times 8 columns of a lane in a half
+  constexpr int NC = DUAL || MIX ? NQ : 2 * NQ;  // and in the tile
+  const int cofs = 8 * (kq >> 1) + (PAIR ? 0 : 16 * (kq & 1)), rofs = r16 + (PAIR ? HM * (kq & 1) : 0);
   const int rows = min(BM, p.M - mb);
   const bool cut = EPI == kFfnStore && g.ksplit > 1;
   const int cdt = cut ? (int)GTR_F32 : EPI == kFfnStore ? g.cdt : DT;
@@ -480,102 +483,99 @@ __device__ __forceinline__ void ffn_tile(const FfnGemm& g, char* ring, int b, in
   const int64_t first_at = ((int64_t)mb * ldc + nb) * es;  // the tile's first element
   const int range = (int)((rows * ldc - nb) * es);
   auto tile_of = [&](const char* c) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(c) + first_at, 0, c ? range : 0, 0x00020000); };
-  unsigned col[DUAL ? 1 : 2][NQ];  // a lane's columns, in bytes from the tile's first
+  unsigned col[NC];  // a lane's columns, in bytes from the tile's first
 #pragma unroll
-  for (int q = 0; q < (DUAL ? NQ : 2 * NQ); ++q) {
-    const int c = q / NQ * HN + wn + 4 * CW * (q % NQ) + cofs;
-    col[q / NQ][q % NQ] = nb + c < p.N ? c * es : 0x80000000u;
+  for (int q = 0; q < NC; ++q) {
+    const int c = q / NQ * HN + (MIX ? 2 : 1) * wn + 32 * (q % NQ) + cofs;
+    col[q] = nb + c < p.N ? c * es : 0x80000000u;
   }
   const auto rc = tile_of(cut ? reinterpret_cast<const char*>(g.part + bz * g.part_slice + p.part_off) : p.c);
   const auto rres = tile_of(EPI == kFfnStore && !cut ? p.res : nullptr);
   const auto rg = tile_of(g.gate), rl = tile_of(g.value), rdg = tile_of(g.dgate), rdl = tile_of(g.dvalue);
   const bool res32 = EPI == kFfnStore && p.res && !cut && cdt == GTR_F32, res16 = EPI == kFfnStore && p.res && !cut && cdt != GTR_F32;
-  FfnVec<CW> e0[TI][2 * NQ], e1[TI][2 * NQ];  // what the epilogue reads
+  FfnVec e0[TI][NC], e1[TI][NC];  // what the epilogue reads
   auto at = [&](int h, int i, int q) {
-    return (unsigned)((h * HM + wm + 16 * i + r16) * (int)ldc) * es + col[DUAL ? 0 : q / NQ][q % NQ];
+    return (unsigned)((h * HM + wm + 16 * i + rofs) * (int)ldc) * es + col[q];
   };
   auto fetch = [&](int h) {
     if (EPI == kFfnGateGrad || res16 || res32) {
 #pragma unroll
       for (int i = 0; i < TI; ++i)
 #pragma unroll
-        for (int q = 0; q < 2 * NQ; ++q) {
+        for (int q = 0; q < NC; ++q) {
           const unsigned o = at(h, i, q);
           if constexpr (EPI == kFfnGateGrad) {
             e0[i][q].load(rg, o);
             e1[i][q].load(rl, o);
           } else {
             e0[i][q].load(rres, o);
-            if (res32) e1[i][q].load(rres, o + CW * 2);
+            if (res32) e1[i][q].load(rres, o + 16);
           }
         }
     }
   };
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {  // the rows of A_h
+  for (int h = 0; h < (PAIR ? 1 : 2); ++h) {  // the rows of A_h
     fetch(h);
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
-      float x[2][NQ][CW];
+      float x[2][NQ][8];
 #pragma unroll
-      for (int q = 0; q < 2 * NQ; ++q)
+      for (int q = 0; q < (MIX ? 1 : 2 * NQ); ++q)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if constexpr (CW == 8) {
-            x[q / NQ][q % NQ][e] = acc[h][q / NQ][i][2 * (q % NQ)][e];
-            x[q / NQ][q % NQ][4 + e] = acc[h][q / NQ][i][2 * (q % NQ) + 1][e];
-            swap_rows(x[q / NQ][q % NQ][e], x[q / NQ][q % NQ][4 + e]);
-          } else {
-            x[q / NQ][q % NQ][e] = acc[h][q / NQ][i][q % NQ][e];
-          }
+          float(&v)[8] = x[q / NQ][q % NQ];
+          v[e] = acc[h][q / NQ][i][TJ == 1 ? 0 : 2 * (q % NQ)][e];
+          v[4 + e] = MIX ? acc[h][1][i][0][e] : PAIR ? acc[1][q][i][0][e] : acc[h][q / NQ][i][TJ == 1 ? 0 : 2 * (q % NQ) + 1][e];
+          swap_rows(v[e], v[4 + e]);
         }
       if constexpr (DUAL) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
           const unsigned o = at(h, i, q);
-          if (g.gate) FfnVec<CW>::template pack<DT>(x[0][q]).template store<kFfnLater>(rg, o);
-          if (g.value) FfnVec<CW>::template pack<DT>(x[1][q]).template store<kFfnLater>(rl, o);
-          float y[CW], s;
+          if (g.gate) FfnVec::pack<DT>(x[0][q]).template store<kFfnLater>(rg, o);
+          if (g.value) FfnVec::pack<DT>(x[1][q]).template store<kFfnLater>(rl, o);
+          float y[8], s;
 #pragma unroll
-          for (int e = 0; e < CW; ++e) y[e] = ffn_act(x[0][q][e], g.act, s) * x[1][q][e];
-          FfnVec<CW>::template pack<DT>(y).store(rc, o);
+          for (int e = 0; e < 8; ++e) y[e] = ffn_act(x[0][q][e], g.act, s) * x[1][q][e];
+          FfnVec::pack<DT>(y).store(rc, o);
         }
       } else {
 #pragma unroll
-        for (int q = 0; q < 2 * NQ; ++q) {
-          float(&v)[CW] = x[q / NQ][q % NQ];
+        for (int q = 0; q < NC; ++q) {
+          float(&v)[8] = x[q / NQ][q % NQ];
           const unsigned o = at(h, i, q);
           if constexpr (EPI == kFfnGateGrad) {
-            float gt[CW], vl[CW], dg[CW], dv[CW], hh[CW];
+            float gt[8], vl[8], dg[8], dv[8], hh[8];
             e0[i][q].template unpack<DT>(gt);
             e1[i][q].template unpack<DT>(vl);
 #pragma unroll
-            for (int e = 0; e < CW; ++e) {
+            for (int e = 0; e < 8; ++e) {
               float s;
               const float a = ffn_act(gt[e], g.act, s);
               dg[e] = v[e] * vl[e] * s;
               dv[e] = v[e] * a;
               hh[e] = a * vl[e];
             }
-            FfnVec<CW>::template pack<DT>(dg).store(rdg, o);
-            FfnVec<CW>::template pack<DT>(dv).store(rdl, o);
-            if (p.c) FfnVec<CW>::template pack<DT>(hh).store(rc, o);
+            FfnVec::pack<DT>(dg).store(rdg, o);
+            FfnVec::pack<DT>(dv).store(rdl, o);
+            if (p.c) FfnVec::pack<DT>(hh).store(rc, o);
           } else {
             if (res16) {
-              float r[CW];
+              float r[8];
               e0[i][q].template unpack<DT>(r);
 #pragma unroll
-              for (int e = 0; e < CW; ++e) v[e] += r[e];
+              for (int e = 0; e < 8; ++e) v[e] += r[e];
             }
             if (res32) {
 #pragma unroll
-              for (int e = 0; e < CW; ++e) v[e] += e < CW / 2 ? e0[i][q].f32(e) : e1[i][q].f32(e - CW / 2);
+              for (int e = 0; e < 8; ++e) v[e] += e < 4 ? e0[i][q].f32(e) : e1[i][q].f32(e - 4);
             }
             if (cdt == GTR_F32) {
-              FfnVec<CW>::bits(v).store(rc, o);
-              FfnVec<CW>::bits(v + CW / 2).store(rc, o + CW * 2);
+              FfnVec::bits(v).store(rc, o);
+              FfnVec::bits(v + 4).store(rc, o + 16);
             } else {
-              FfnVec<CW>::template pack<DT>(v).store(rc, o);
+              FfnVec::pack<DT>(v).store(rc, o);
             }
           }
         }
