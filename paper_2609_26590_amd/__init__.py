@@ -745,7 +745,7 @@ def _ffn_shape(x, w_gate, w_value, w_out) -> tuple:
         _rows("x", x)
     if dt is torch.float32:
         raise ValueError("x must be float16 or bfloat16")
-    d, hidden, index = shape[-1], w_gate.shape[0], dev.index
+    d, hidden, index = shape[-1], w_gate.shape[0] if w_gate.dim() else 0, dev.index
     up, down = (hidden, d), (d, hidden)
     if not (w_gate.shape == up and w_value.shape == up and w_out.shape == down and w_gate.dtype is dt and
             w_value.dtype is dt and w_out.dtype is dt and w_gate.get_device() == index and

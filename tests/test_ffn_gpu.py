@@ -312,7 +312,8 @@ def test_the_binding_refuses(gtr):
             fwd(x.float(), *w), fwd(x, s["wg"].bfloat16(), *w[1:]), fwd(x, s["wg"], s["wv"][:64], s["wo"]),
             fwd(x, s["wg"], s["wv"], s["wo"].t()), fwd(x[:, :32], *w), fwd(x.t(), *w), fwd(x, *w, act="relu"),
             fwd(x, *w, residual=x[:12]), fwd(x, *w, gate=g[:, :64]), fwd(x, *w, out=dy.float()), fwd(x.cpu(), *w),
-            fwd(x, s["wg"].cpu(), *w[1:]), bwd(dy[:12], x, *w, g, v), bwd(dy, x, *w, g.t(), v), bwd(dy, x, *w, g, v[:12]),
+            fwd(x, s["wg"].cpu(), *w[1:]), fwd(x, s["wg"][0, 0], *w[1:]),
+            bwd(dy[:12], x, *w, g, v), bwd(dy, x, *w, g.t(), v), bwd(dy, x, *w, g, v[:12]),
             bwd(dy, x, *w, g, v, dw_dtype=torch.bfloat16), bwd(dy, x, *w, g, v, accumulate=True),
             bwd(dy, x, *w, g, v, dw_gate=torch.zeros_like(s["wo"])), bwd(dy, x, *w, g, v, act="none"),
             lnf(x.double()), lnf(x.t()), lnf(x, m), lnf(x, torch.ones(64, device="cuda").half()), lnf(x, mean=m[:3]),
