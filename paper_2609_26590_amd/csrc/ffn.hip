@@ -33,17 +33,22 @@ struct FfnPlan {
 };
 
 // Estimates in us, from timings of each tile on its own: a step with `o` work-groups
-// on the CU, and what a work-group takes besides its steps, `fill` being the share of
-// the chip's places that are taken (the gradients' epilogue moves 10 bytes per element
-// of C, which bound it once many do so together).
-static float ffn_step(int tile, int lay, int o) {
-  static const float one[3][3] = {{1.0f, 1.0f, 1.1f}, {0.38f, 0.42f, 0.45f}, {0.24f, 0.25f, 0.3f}};
+// on the CU (its matrix cores are shared late: the second costs less than the fourth),
+// and what a work-group takes besides its steps, `fill` being the share of the chip's
+// places that are taken (the gradients' epilogue moves 10 bytes per element of C, which
+// bound it once many do so together). Rows along K that do not start on 128 bytes
+// (`skew`) spread each transfer over twice the lines.
+static float ffn_step(int tile, int lay, int o, bool skew) {
+  static const float one[3][3] = {{1.0f, 1.0f, 1.1f}, {0.41f, 0.42f, 0.45f}, {0.24f, 0.25f, 0.3f}};
   static const float full[3][3] = {{1.42f, 1.45f, 1.35f}, {0.97f, 1.05f, 1.15f}, {0.82f, 1.19f, 1.46f}};
-  const int n = kFfnPerCu[tile];
-  return n == 1 ? full[tile][lay] : one[tile][lay] + (full[tile][lay] - one[tile][lay]) * (float)(o - 1) / (float)(n - 1);
+  static const float shared[5] = {0.f, 0.f, 0.19f, 0.54f, 1.f};  // tile 2: ((o - 1) / 3)^1.5
+  const float by = skew ? tile == 2 ? 1.5f : 1.4f : 1.f;
+  return by * (tile == 0   ? full[0][lay]
+               : tile == 1 ? (o > 1 ? full : one)[1][lay]
+                           : one[2][lay] + (full[2][lay] - one[2][lay]) * shared[o]);
 }
 static float ffn_fixed(int tile, int epi, float fill) {
-  static const float us[3][3] = {{9.f, 5.f, 4.f}, {9.f, 4.6f, 2.5f}, {8.f, 5.f, 4.f}}, more[3] = {26.f, 12.f, 3.5f};
+  static const float us[3][3] = {{9.f, 5.f, 4.f}, {9.f, 4.6f, 2.5f}, {8.f, 8.5f, 6.f}}, more[3] = {26.f, 8.5f, 1.5f};
   return us[epi][tile] + (epi == kFfnGateGrad ? more[tile] * (fill < 1.f ? fill : 1.f) : 0.f);
 }
 static int64_t ffn_tiles(const FfnProd* p, int nprod, int tile, int epi) {
@@ -67,6 +72,7 @@ static FfnPlan ffn_plan(const FfnProd* p, int nprod, int lay, int epi) {
   float least = 0.f;
   const int steps = ffn_steps(p[0]);
   const int64_t elems = ffn_elems(p, nprod);
+  const bool skew = lay == kRowRow && (p[0].lda % 64 || p[0].ldb % 64);
   for (int c = 0; c < 3; ++c) {
     const int64_t tiles = ffn_tiles(p, nprod, c, epi), slots = (int64_t)kFfnCus * kFfnPerCu[c];
     const int most = epi == kFfnStore && steps >= 8 ? (steps / 4 < 32 ? steps / 4 : 32) : 1;
@@ -74,10 +80,10 @@ static FfnPlan ffn_plan(const FfnProd* p, int nprod, int lay, int epi) {
       const int per = (steps + ks - 1) / ks;
       if (ks > 1 && (steps + per - 1) / per != ks) continue;  // a slice would be empty
       const int64_t n = tiles * ks;
-      const float tile_us = per * ffn_step(c, lay, kFfnPerCu[c]) + ffn_fixed(c, epi, 1.f);
+      const float tile_us = per * ffn_step(c, lay, kFfnPerCu[c], skew) + ffn_fixed(c, epi, 1.f);
       float us;
       if (n <= slots)
-        us = per * ffn_step(c, lay, (int)((n + kFfnCus - 1) / kFfnCus)) + ffn_fixed(c, epi, (float)n / (float)slots);
+        us = per * ffn_step(c, lay, (int)((n + kFfnCus - 1) / kFfnCus), skew) + ffn_fixed(c, epi, (float)n / (float)slots);
       else if (kFfnPerCu[c] == 1)
         us = (float)((n + slots - 1) / slots) * tile_us;
       else  // a CU's work-groups do not start and end together: no whole rounds
@@ -113,7 +119,7 @@ static void ffn_plan_grads(const FfnProd* x, int nx, const FfnProd* w, int nw, F
         const int64_t n = tx * kx + tw * kw;
         const int o = n >= slots ? kFfnPerCu[c] : (int)((n + kFfnCus - 1) / kFfnCus);
         const float fixed = ffn_fixed(c, kFfnStore, 1.f);
-        const float ux = nx ? perx * ffn_step(c, kRowCol, o) + fixed : 0.f, uw = nw ? perw * ffn_step(c, kColCol, o) + fixed : 0.f;
+        const float ux = nx ? perx * ffn_step(c, kRowCol, o, false) + fixed : 0.f, uw = nw ? perw * ffn_step(c, kColCol, o, false) + fixed : 0.f;
         const float longest = ux > uw ? ux : uw, shortest = ux < uw && nx ? ux : nw ? uw : ux;
         float us = ((float)(tx * kx) * ux + (float)(tw * kw) * uw) / (float)(kFfnCus * o);
         us = n > slots ? us + 0.5f * shortest : us;
