@@ -173,7 +173,8 @@ typedef enum {
  *        any call's workspace overlaps, and every completed call leaves them
  *        zeroed again, so one workspace (large enough for each) serves any
  *        number of calls of any shapes on one stream. Calls that overlap in
- *        time (two streams, for instance) must not share a workspace.
+ *        time (two streams, for instance) must not share a workspace, nor may
+ *        a call of another operator use it, which would overwrite those words.
  * spin_limit : polls a one-launch work-group makes while it waits for the
  *        chunks before it, before it gives up (0: the library default, about a
  *        second). A work-group that gives up sets bit 0 of the fault word and
@@ -299,7 +300,8 @@ int gtr_gla_segment_chunks(const gtr_gla_args* args);
  * workspace : caller-owned, 256-byte aligned, gtr_spatial_swiglu_workspace_size
  *           bytes (B*H*W*hidden*2 for the activations plus the float32 partial
  *           products of a K-split output product, rounded up); no
- *           initialisation needed.
+ *           initialisation needed. It is left with any contents, so it is never
+ *           a gtr_gla_fwd workspace, whose words must stay zeroed.
  * Errors as for gtr_gla_fwd; every check runs before any launch.
  */
 typedef struct {
@@ -445,7 +447,9 @@ gtr_status gtr_layernorm_fwd(const gtr_layernorm_fwd_args* args, hipStream_t str
  *          they hold
  * workspace : for dw and db, where gtr_layernorm_bwd_workspace_size(args) is not
  *          0: 256-byte aligned, at least that many bytes, no initialisation
- *          needed; calls that overlap in time must not share one.
+ *          needed; calls that overlap in time must not share one. It is left
+ *          with any contents: never a gtr_gla_fwd workspace, whose words must
+ *          stay zeroed.
  * Sizes and types as for gtr_layernorm_fwd.
  */
 typedef struct {
@@ -492,6 +496,8 @@ typedef enum { GTR_ACT_SILU = 0, GTR_ACT_GELU = 1 } gtr_act;
  * workspace : 256-byte aligned, at least gtr_ffn_fwd_workspace_size(args) bytes
  *            (M * hidden * 2 and the partial sums of products cut along K), no
  *            initialisation needed; calls that overlap in time must not share one.
+ *            It is left with any contents: never a gtr_gla_fwd workspace, whose
+ *            words must stay zeroed.
  */
 typedef struct {
   const void* x;

@@ -20,7 +20,7 @@ Entry points (same names as the C ABI in ``include/gtr.h``):
 * :func:`gtr_ffn_fwd`, :func:`gtr_ffn_bwd` - the gated feed-forward
   ``[act(x W_gate^T) * (x W_value^T)] W_out^T`` and its gradients.
 
-:class:`Workspace` keeps a caller-owned, zero-initialised workspace buffer.
+:class:`Workspace` keeps caller-owned workspace memory; one serves all of the calls above on one stream.
 """
 from __future__ import annotations
 
@@ -275,25 +275,40 @@ def gtr_gla_workspace_fault(ws: torch.Tensor) -> int:
 
 
 class Workspace:
-    """A growable, zero-initialised device workspace for :func:`gtr_gla_fwd`,
-    used on one stream: it is allocated and zero-filled on that stream, so
-    the caching allocator never hands its memory to another stream while a
-    call on this one may still use it."""
+    """Growable device memory for the calls that take a ``workspace``, used on
+    one stream: it is allocated on that stream, so the caching allocator never
+    hands its memory to another stream while a call on this one may still use it.
+
+    It holds two buffers: a zero-initialised one for :func:`gtr_gla_fwd`, which
+    finds its synchronisation words zeroed and leaves them so, and one for the
+    other calls, which leave any contents behind and would overwrite those words."""
 
     def __init__(self, device=None, stream=None):
         self.device = torch.device("cuda") if device is None else torch.device(device)
         self.stream = stream
         self.buf: Optional[torch.Tensor] = None
+        self.plain: Optional[torch.Tensor] = None
 
     def get(self, nbytes: int, stream=None) -> torch.Tensor:
-        if self.buf is None or self.buf.numel() < nbytes:
+        """At least nbytes of zero-initialised memory, whose words a completed gtr_gla_fwd leaves zeroed."""
+        self.buf = self._grown(self.buf, nbytes, stream, True)
+        return self.buf
+
+    def scratch(self, nbytes: int, stream=None) -> torch.Tensor:
+        """At least nbytes of memory of any contents."""
+        self.plain = self._grown(self.plain, nbytes, stream, False)
+        return self.plain
+
+    def _grown(self, buf: Optional[torch.Tensor], nbytes: int, stream, zeroed: bool) -> torch.Tensor:
+        if buf is None or buf.numel() < nbytes:
             s = stream if stream is not None else (self.stream or torch.cuda.current_stream(self.device))
             n = max(256, (nbytes + 255) // 256 * 256)
             with torch.cuda.stream(s):
                 # 256-byte aligned: torch's caching allocator hands out 512-byte aligned blocks
-                self.buf = torch.empty(n, dtype=torch.uint8, device=self.device)
-                gtr_gla_workspace_init(self.buf, s)
-        return self.buf
+                buf = torch.empty(n, dtype=torch.uint8, device=self.device)
+                if zeroed:
+                    gtr_gla_workspace_init(buf, s)
+        return buf
 
 
 # default workspaces, one per (device, stream): calls on different streams
@@ -475,7 +490,7 @@ def gtr_spatial_swiglu(x: torch.Tensor, w_gate: torch.Tensor, w_value: torch.Ten
         raise GtrError("gtr_spatial_swiglu_workspace_size", 2)
     if workspace is None:
         workspace = _default_workspace("swiglu", x.device, stream)
-    buf = workspace.get(need, stream)
+    buf = workspace.scratch(need, stream)
     a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel()
     st = lib.gtr_spatial_swiglu(ctypes.byref(a), _stream_ptr(stream))
     if st:
@@ -640,7 +655,7 @@ def _scratch(need: int, dev: torch.device, workspace: Optional["Workspace"]) -> 
     """Scratch memory of a call on the current stream. Without a ``workspace`` it is the caching allocator's: it belongs
     to this stream (and, in a graph capture, to the graph), so that no two calls in flight share it."""
     if workspace is not None:
-        return workspace.get(need, torch.cuda.current_stream(dev))
+        return workspace.scratch(need, torch.cuda.current_stream(dev))
     return torch.empty(need, dtype=torch.uint8, device=dev)
 
 
