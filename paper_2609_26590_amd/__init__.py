@@ -281,13 +281,16 @@ class Workspace:
 
     It holds two buffers: a zero-initialised one for :func:`gtr_gla_fwd`, which
     finds its synchronisation words zeroed and leaves them so, and one for the
-    other calls, which leave any contents behind and would overwrite those words."""
+    other calls, which leave any contents behind and would overwrite those words.
+    A buffer that a graph capture was given is kept when a larger one takes its
+    place: the graph's replays go on using it."""
 
     def __init__(self, device=None, stream=None):
         self.device = torch.device("cuda") if device is None else torch.device(device)
         self.stream = stream
         self.buf: Optional[torch.Tensor] = None
         self.plain: Optional[torch.Tensor] = None
+        self._captured: list = []
 
     def get(self, nbytes: int, stream=None) -> torch.Tensor:
         """At least nbytes of zero-initialised memory, whose words a completed gtr_gla_fwd leaves zeroed."""
@@ -308,6 +311,8 @@ class Workspace:
                 buf = torch.empty(n, dtype=torch.uint8, device=self.device)
                 if zeroed:
                     gtr_gla_workspace_init(buf, s)
+        if torch._C._cuda_isCurrentStreamCapturing() and not any(t is buf for t in self._captured):
+            self._captured.append(buf)
         return buf
 
 

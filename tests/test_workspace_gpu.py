@@ -38,3 +38,26 @@ def test_one_workspace_for_every_call(gtr, dtype):
         got = calls(gtr, data, ws)
         assert gtr.gtr_gla_workspace_fault(ws.buf) == 0
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_graph_outlives_its_workspaces_growth(gtr):
+    """Calls recorded with a Workspace that larger eager calls make grow afterwards: the replays keep their memory."""
+    small, ws = inputs(torch.float16, 2), gtr.Workspace()
+    want = calls(gtr, small, None)
+    calls(gtr, small, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = calls(gtr, small, ws)
+    for k in range(3):
+        sizes = ws.buf.numel(), ws.plain.numel()
+        x, wg, wo = (torch.randn(s, device="cuda").half() for s in ((3000 + 1000 * k, 384), (1536, 384), (384, 1536)))
+        gtr.gtr_ffn_fwd(x, wg, wg, wo, workspace=ws)
+        q = torch.randn(2 + k, 6, 400, 64, device="cuda").half()
+        gtr.gtr_gla_fwd(q, q, q, -q.abs(), H=20, W=20, workspace=ws)
+        assert ws.buf.numel() > sizes[0] and ws.plain.numel() > sizes[1]
+        others = [torch.full((n,), 0x5A, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all((t == 0x5A).all() for t in others)
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
