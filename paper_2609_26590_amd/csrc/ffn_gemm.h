@@ -6,6 +6,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "ffn_plan.h"
 #include "gemm.h"
 #include "gtr.h"
 #include "gtr_device.h"
@@ -14,17 +15,6 @@ namespace gtr {
 
 typedef int i4 __attribute__((ext_vector_type(4)));
 typedef short s16v4 __attribute__((ext_vector_type(4)));
-
-// One product of a launch: C[M][N] = sum over nseg segments of A_s B_s, K deep each.
-struct FfnProd {
-  const char *a[2], *b[2];  // the segments' operands (gate epilogue: b = the two weights, nseg 1)
-  char* c;
-  const char* res;  // [M][N] in C's type, added (a residual, or C itself to accumulate), or null
-  int64_t lda, ldb, ldc;
-  int M, N, K, nseg;
-  int gx, gy;  // row and column tiles
-  int64_t part_off;  // where its partial sums start within a slice
-};
 
 constexpr int kFfnProds = 3;
 struct FfnGemm {
@@ -38,9 +28,6 @@ struct FfnGemm {
   // backward: read), and in the backward pass their gradients
   char *gate, *value, *dgate, *dvalue;
 };
-
-// What an epilogue does with the product.
-enum { kFfnStore = 0, kFfnGate = 1, kFfnGateGrad = 2 };
 
 // Cache policy of stores that nothing reads soon (non-temporal): the projections kept
 // for the backward pass leave the caches to the activations that the next product
@@ -665,7 +652,6 @@ __global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g, FfnGemm h) {
 // flight: 5.6 and 39.7 at the second and the last; with more in flight the registers
 // leave fewer work-groups on a CU.
 // ---------------------------------------------------------------------------
-constexpr int kFewTokens = 8;
 constexpr int few_waves(int nb) { return nb == 1 ? 8 : 4; }
 constexpr int kFewFlight = 2;
 struct FfnFew {
