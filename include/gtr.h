@@ -488,8 +488,9 @@ typedef enum { GTR_ACT_SILU = 0, GTR_ACT_GELU = 1 } gtr_act;
  * residual : [M, d] dtype or NULL; may be y (in place)
  * gate, value : [M, hidden] dtype, receive g and v for gtr_ffn_bwd; either may
  *            be NULL
- * M >= 1 (one token upwards); d and hidden multiples of 8; every pointer
- * 16-byte aligned; an output overlaps nothing else.
+ * 1 <= M <= 2^30 (one token upwards); d and hidden multiples of 8, at most 2^20;
+ * M d and M hidden at most 2^37, d hidden at most 2^36; every pointer 16-byte
+ * aligned; an output overlaps nothing else.
  * Both projections, the activation and their product are one launch. The
  * products accumulate in float32; act(g) v is formed in float32 and rounded to
  * dtype for the output product (in fp16 it must stay in range).

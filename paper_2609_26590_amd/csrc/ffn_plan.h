@@ -32,6 +32,9 @@ constexpr int kFfnCus = 256;
 // Tiles a product can run in: 256 x 256 with one work-group of 8 waves per CU,
 // 128 x 128 with two of 4 waves, 64 x 64 with four of 4 waves.
 constexpr int kFfnTile[3] = {256, 128, 64}, kFfnPerCu[3] = {1, 2, 4};
+// A launch takes less than 2^32 threads: of n work-groups of a tile size (small tiles of
+// a billion rows are more).
+inline bool ffn_fits(int64_t n, int tile) { return n * (tile == 0 ? 512 : 256) < (int64_t)1 << 32; }
 enum { kRowRow = 0, kRowCol = 1, kColCol = 2 };  // operands: both along K, A alone, none
 
 struct FfnPlan {
@@ -88,6 +91,7 @@ inline FfnPlan ffn_plan(const FfnProd* p, int nprod, int lay, int epi) {
       const int per = (steps + ks - 1) / ks;
       if (ks > 1 && (steps + per - 1) / per != ks) continue;  // a slice would be empty
       const int64_t n = tiles * ks;
+      if (!ffn_fits(n, c)) break;
       const float tile_us = per * ffn_step(c, lay, kFfnPerCu[c], skew) + ffn_fixed(c, epi, 1.f);
       float us;
       if (n <= slots)
@@ -125,6 +129,7 @@ inline void ffn_plan_grads(const FfnProd* x, int nx, const FfnProd* w, int nw, F
         if (kw > 1 && (sw + perw - 1) / perw != kw) continue;
         if (kw > 1 && tw * (kw - 1) >= slots) break;
         const int64_t n = tx * kx + tw * kw;
+        if (!ffn_fits(n + 7, c)) break;
         const int o = n >= slots ? kFfnPerCu[c] : (int)((n + kFfnCus - 1) / kFfnCus);
         const float fixed = ffn_fixed(c, kFfnStore, 1.f);
         const float ux = nx ? perx * ffn_step(c, kRowCol, o, false) + fixed : 0.f, uw = nw ? perw * ffn_step(c, kColCol, o, false) + fixed : 0.f;
@@ -166,9 +171,10 @@ inline gtr_status ffn_sizes(int64_t M, int32_t d, int32_t hidden, int dt, int ac
   if (d % 8 || hidden % 8 || d > kFfnMaxWidth || hidden > kFfnMaxWidth || (dt != GTR_F16 && dt != GTR_BF16) ||
       (act != GTR_ACT_SILU && act != GTR_ACT_GELU))
     return GTR_ERR_UNSUPPORTED;
-  // rows and work-groups count in 32 bits
+  // Rows count in 32 bits, and the largest tiles' launches hold every work-group
+  // (activations and weights of 256 and 128 GiB: past what the memory holds).
   const int64_t w = d > hidden ? d : hidden;
-  if (M > ((int64_t)1 << 30) || M * w > ((int64_t)1 << 38)) return GTR_ERR_SHAPE;
+  if (M > ((int64_t)1 << 30) || M * w > ((int64_t)1 << 37) || (int64_t)d * hidden > ((int64_t)1 << 36)) return GTR_ERR_SHAPE;
   return GTR_OK;
 }
 
