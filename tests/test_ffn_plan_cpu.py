@@ -2,6 +2,8 @@
 import pytest
 
 import ffn_plans as plans
+from test_ffn_gpu import SHAPES
+from test_ffn_tiles_gpu import CUT, LARGE
 
 SHAPE, UNSUP = 2, 3
 MOST_ROWS, MOST_WIDTH, MOST_ACTIVATIONS, MOST_WEIGHTS = 1 << 30, 1 << 20, 1 << 37, 1 << 36  # (gtr.h)
@@ -44,3 +46,26 @@ def test_sizes_past_the_limits_are_refused():
     assert plans.forward(64, 1 << 20, 1 << 16) != SHAPE and plans.forward(64, 1 << 20, (1 << 16) + 8) == SHAPE
     assert plans.backward(64, 1 << 18, 1 << 18) != SHAPE and plans.backward(64, (1 << 18) + 8, 1 << 18) == SHAPE
     assert plans.forward(1, MOST_WIDTH + 8, 8) == UNSUP and plans.forward(1, 8, MOST_WIDTH) != UNSUP
+
+
+def test_the_gpu_tests_reach_every_tile_and_cut():
+    """The shapes that the GPU tests check values at, by what they plan: each product in each tile size, with K steps
+    behind the first, and cut along K and not."""
+    for shape in LARGE:
+        up, down = plans.forward(*shape)
+        dh, dx, dw = plans.backward(*shape)
+        assert {p["tile"] for p in (up, down, dh, dx, dw)} == {256}, shape
+        M, d, hidden = shape
+        assert M % 256 and d % 256 and hidden % 256 and d > 4 * 64 and hidden > 4 * 64
+    cuts = [plans.backward(*shape)[1:] for shape in CUT]
+    assert all(dw["ksplit"] > 1 for _, dw in cuts)
+    assert any(dx["ksplit"] > 1 for dx, _ in cuts) and any(dx["ksplit"] == 1 for dx, _ in cuts)
+    alone = [plans.backward(*shape, want=14)[2] for shape in CUT]
+    assert {dw["tile"] for _, dw in cuts} | {dw["tile"] for dw in alone if dw["ksplit"] > 1} == {256, 128, 64}
+    seen = [set(), set(), set(), set(), set()]  # tile and whether it is cut, of each product
+    for shape in SHAPES + LARGE + CUT:
+        for s, p in zip(seen, plans.forward(*shape) + plans.backward(*shape)):
+            s.add((p["tile"], p["ksplit"] > 1))
+    assert seen[0] == seen[2] == {(256, False), (128, False), (64, False)}
+    for s in (seen[1], seen[3], seen[4]):
+        assert {t for t, _ in s} == {256, 128, 64} and {c for _, c in s} == {False, True}, seen
