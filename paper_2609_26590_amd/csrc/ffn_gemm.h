@@ -89,9 +89,11 @@ struct FfnVec {
 // function and its density. The tail Q(x) = 1 - P(x), x = |g|, is taken as exp(-x^2 /
 // 2) t R(t) with t = 1 / (1 + 3 x / 8): Q(x) exp(x^2 / 2) / t is smooth over 0 < t <= 1,
 // and R is the polynomial of degree 8 that fits it there by least squares, reweighted
-// towards the least largest relative error: 2.2e-7, in float32 5e-7, at any x. It
-// shares its exponential with the density. (The library's erfc cost 16 us of 101 in
-// the forward pass of 12800 x 384 x 1536.)
+// towards the least largest relative error, 2.6e-7 at any x. In float32 the rounding of
+// the exponential's argument comes to it, which grows with x^2: Q is off by at most 1e-6
+// + 1.25 x^2 2^-24 of itself (5.3e-7 up to x = 2, 3.8e-6 up to 9, 7.7e-6 up to 13), where a
+// 16-bit type's rounding is 4.9e-4 or more. Q shares its exponential with the density.
+// (The library's erfc cost 16 us of 101 in the forward pass of 12800 x 384 x 1536.)
 __device__ __forceinline__ float ffn_act(float g, int act, float& slope) {
   if (act == GTR_ACT_SILU) {
     const float p = __builtin_amdgcn_rcpf(1.f + __expf(-g));
