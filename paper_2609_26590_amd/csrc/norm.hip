@@ -512,14 +512,32 @@ static int64_t ln_bwd_groups(int64_t M, const LnShape& s) {
   return g < all ? g : all;
 }
 
-// Whether dw and db are summed by columns: where a batch is short, its second reading
-// comes from cache in one or two round trips, and dx does not overwrite what is read.
-// Calls one after the other against partial sums and their launch, us: 64 x 384 fp16
-// 8.4 / 12.8, 777 x 1001 float32 8.9 / 12.4, 1600 x 192 bf16 8.8 / 12.5, 1600 x 384
-// 12.3 / 12.6; but 2000 x 384 13.5 / 12.6.
-static bool ln_by_columns(const gtr_layernorm_bwd_args* a) {
-  const int64_t bytes = a->M * a->d * (int64_t)dtype_size(a->dtype);
-  return a->M <= 2048 && bytes <= (a->M <= 1024 ? 12 << 18 : 5 << 18) && !(a->dx && (a->dx == a->dy || a->dx == a->x));
+// Work-groups that take the columns: two vectors each.
+static int ln_column_groups(int d, int dt) {
+  const int VE = dt == GTR_F32 ? 4 : 8;
+  return (d + 2 * VE - 1) / (2 * VE);
+}
+// Whether dw and db are summed by columns: where that is sooner for calls one after the
+// other, which are paced by the host, by one launch or two (8.3 and 12.3 us), and dx does
+// not overwrite what is read. Work-groups that share the columns read every row, so it
+// takes longer with the rows (a round of loads per 8) and with the elements: measured at
+// 12 widths of three types, from 0.4 to 1.6 times the limit, the two are even at M (d +
+// 540) = 1.2 to 2.2 million, and at half of that where a work-group of more than 512
+// threads has a CU for itself; and where those are more than three rounds of the chip
+// (float32 past 6144 columns, 16 bits past 12288) by columns was not sooner at any M.
+// Us by columns / by partial sums: float16 1372 x 72 8.8 / 13.0, 3660 x 72 14.7 / 13.6;
+// 1333 x 300 11.8 / 13.2, 1833 x 300 13.8 / 12.9; 777 x 900 9.6 / 12.9, 1555 x 900
+// 14.6 / 12.8; 549 x 1500 9.4 / 12.8, 1098 x 1500 13.7 / 12.9; 92 x 6000 10.7 / 13.3;
+// float32 1583 x 300 10.7 / 13.0, 2666 x 300 14.5 / 12.9; 923 x 900 9.4 / 12.9, 1555 x 900
+// 13.4 / 13.0; 432 x 2048 10.7 / 12.9, 703 x 2048 15.0 / 13.1; 82 x 4096 10.2 / 12.9, 220
+// x 4096 14.8 / 13.1; 1 x 8192 14.0 / 12.2. For unaligned rows of 16 bits they are even at
+// 1.2 million (501 columns: 1075 rows 11.9 / 13.0, 1277 rows 14.3 / 12.9). Recorded into a
+// graph, where no host paces them, two launches are ahead from about 0.8 million on
+// (float16 1333 x 300 11.8 / 8.2, 777 x 900 9.6 / 10.9).
+static bool ln_by_columns(const gtr_layernorm_bwd_args* a, const LnShape& s) {
+  const bool wide = s.threads > 512;
+  if (wide && ln_column_groups(a->d, a->dtype) > 3 * 256) return false;
+  return a->M * (a->d + 540) <= (wide ? 640000 : 1400000) && !(a->dx && (a->dx == a->dy || a->dx == a->x));
 }
 
 template <class P>
@@ -586,7 +604,7 @@ static gtr_status ln_bwd_check(const gtr_layernorm_bwd_args* a, bool pointers, s
   if (st != GTR_OK) return st;
   const LnShape s = ln_shape(a->d, a->dtype);
   *need = ((size_t)ln_bwd_groups(a->M, s) * 2 * a->d * 4 + 255) & ~(size_t)255;
-  if (ln_by_columns(a)) *need = 0;
+  if (ln_by_columns(a, s)) *need = 0;
   if (!pointers) return GTR_OK;
   if (!a->dy || !a->x || !a->mean || !a->rstd || (!a->dx && !a->dw && !a->db)) return GTR_ERR_NULL;
   const size_t es = dtype_size(a->dtype), bytes = (size_t)a->M * a->d * es;
@@ -648,16 +666,15 @@ extern "C" gtr_status gtr_layernorm_bwd(const gtr_layernorm_bwd_args* a, hipStre
   if (st != GTR_OK) return st;
   const LnShape s = ln_shape(a->d, a->dtype);
   const int64_t G = ln_bwd_groups(a->M, s);
-  const bool sums = a->dw || a->db, columns = sums && ln_by_columns(a);
+  const bool sums = a->dw || a->db, columns = sums && ln_by_columns(a, s);
   LnBwd p = {static_cast<const char*>(a->dy), static_cast<const char*>(a->x), a->mean, a->rstd, a->w,
              static_cast<const char*>(a->dres), static_cast<char*>(a->dx),
              sums && !columns ? static_cast<float*>(a->workspace) : nullptr, a->M, a->d, 0, a->dw, a->db, a->accumulate};
   int64_t grid = G;
   if (columns) {
-    const int VE = a->dtype == GTR_F32 ? 4 : 8;
     // (without dx the rows have nothing to do, but a launch has a work-group for them)
     p.rows = a->dx ? (int)G : 1;
-    grid = p.rows + (a->d + 2 * VE - 1) / (2 * VE);
+    grid = p.rows + ln_column_groups(a->d, a->dtype);
   }
   const gtr_status run = ln_launch(a->dtype, LnLaunch<LnBwd>{p, s, (unsigned)grid, stream});
   if (run != GTR_OK || !sums || columns) return run;

@@ -1,0 +1,55 @@
+"""How gtr_layernorm_bwd sums dw and db, as its workspace tells on the CPU (none: by columns, one launch), at sizes where
+one way was measured to be at least 7 % sooner than the other; and that the choice has one border per width."""
+import ctypes
+
+import pytest
+
+import paper_2609_26590_amd as gtr
+
+
+def columns(M, d, dtype, **kw):
+    a = gtr.LayernormBwdArgs(dtype=dtype, d=d, M=M, **kw)
+    return gtr.load().gtr_layernorm_bwd_workspace_size(ctypes.byref(a)) == 0
+
+
+# us of calls one after the other, by columns and by partial sums
+MEASURED = [
+    (gtr.F16, 72, 915, 8.6, 13.0), (gtr.F16, 72, 2173, 10.4, 13.0), (gtr.F16, 72, 3660, 14.7, 13.6),
+    (gtr.F16, 136, 1967, 9.7, 13.1), (gtr.F16, 136, 2692, 14.5, 13.0), (gtr.F16, 300, 1333, 11.8, 13.2),
+    (gtr.F16, 300, 1833, 13.8, 12.9), (gtr.F16, 501, 806, 9.4, 13.0), (gtr.F16, 501, 1479, 14.7, 13.0),
+    (gtr.F16, 900, 923, 10.5, 12.9), (gtr.F16, 900, 1555, 14.6, 12.8), (gtr.F16, 1500, 651, 9.9, 12.8),
+    (gtr.F16, 2048, 513, 9.8, 13.0), (gtr.F16, 4096, 286, 10.1, 15.1), (gtr.F16, 6000, 92, 10.7, 13.3),
+    (gtr.F16, 12288, 25, 17.5, 20.9), (gtr.BF16, 72, 2173, 10.4, 13.1), (gtr.BF16, 900, 923, 10.4, 12.9),
+    (gtr.BF16, 900, 1555, 14.6, 12.8), (gtr.BF16, 300, 2666, 18.4, 12.9), (gtr.F32, 72, 2173, 8.6, 13.0),
+    (gtr.F32, 72, 3660, 14.4, 13.1), (gtr.F32, 300, 1583, 10.7, 13.0), (gtr.F32, 300, 2666, 14.5, 12.9),
+    (gtr.F32, 501, 1277, 10.6, 12.9), (gtr.F32, 501, 2151, 14.2, 13.0), (gtr.F32, 900, 923, 9.4, 12.9),
+    (gtr.F32, 1500, 651, 10.6, 13.1), (gtr.F32, 1500, 1098, 15.3, 12.8), (gtr.F32, 2048, 432, 10.7, 12.9),
+    (gtr.F32, 2048, 703, 15.0, 13.1), (gtr.F32, 4096, 131, 11.8, 12.9), (gtr.F32, 4096, 220, 14.8, 13.1),
+    (gtr.F32, 6000, 25, 10.1, 12.3), (gtr.F32, 6000, 156, 15.4, 14.0), (gtr.F32, 8192, 1, 14.0, 12.2),
+    (gtr.F32, 8192, 29, 15.3, 13.1), (gtr.F32, 16384, 15, 27.2, 21.9),
+]
+
+
+@pytest.mark.parametrize("dtype,d,M,by_columns,by_partial_sums", MEASURED)
+def test_the_sooner_way(dtype, d, M, by_columns, by_partial_sums):
+    assert columns(M, d, dtype) == (by_columns < by_partial_sums)
+
+
+@pytest.mark.parametrize("dtype", [gtr.F32, gtr.F16, gtr.BF16])
+def test_one_border_per_width(dtype):
+    """With more rows, and up to the widths whose work-groups have a CU for themselves with more columns, the choice
+    changes once, and by at most the step in the width."""
+    last = None
+    for d in range(8, 2049, 68):
+        ways = [columns(M, d, dtype) for M in range(1, 4000, 3)]
+        border = sum(ways)
+        assert ways == [True] * border + [False] * (len(ways) - border)
+        assert last is None or 0.8 * last <= border <= last
+        last = border
+
+
+def test_a_dx_over_its_inputs_is_summed_by_partial_sums():
+    at = 1 << 44
+    assert columns(100, 384, gtr.F16, dx=at, dy=at + (1 << 30), x=at + (1 << 31), dres=at)
+    assert not columns(100, 384, gtr.F16, dx=at, dy=at, x=at + (1 << 31))
+    assert not columns(100, 384, gtr.F16, dx=at, dy=at + (1 << 30), x=at)
