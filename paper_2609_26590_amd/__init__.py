@@ -656,6 +656,12 @@ def _rows(name: str, t: torch.Tensor) -> None:
         raise ValueError(f"{name} must be [..., d] of float32, float16 or bfloat16")
 
 
+def _i32(n: int) -> int:
+    """n as the ABI's 32-bit integers hold it; a larger one, which ctypes would cut to its lower bits, as the largest,
+    which the library refuses."""
+    return n if n < 0x7fffffff else 0x7fffffff
+
+
 def _scratch(need: int, dev: torch.device, workspace: Optional["Workspace"]) -> torch.Tensor:
     """Scratch memory of a call on the current stream. Without a ``workspace`` it is the caching allocator's: it belongs
     to this stream (and, in a graph capture, to the graph), so that no two calls in flight share it."""
@@ -696,8 +702,8 @@ def _layernorm_fwd(x, weight, bias, eps, y, mu, rs):
         _check("out", y, shape, (dt,), dev)
         for name, t, want in (("weight", weight, (d,)), ("bias", bias, (d,)), ("mean", mu, rows), ("rstd", rs, rows)):
             _check(name, t, want, (f32,), dev)
-    a = LayernormFwdArgs(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mu.data_ptr(), rs.data_ptr(), code, d,
-                         x.numel() // d if d else 0, eps)
+    a = LayernormFwdArgs(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mu.data_ptr(), rs.data_ptr(), code,
+                         _i32(d), x.numel() // d if d else 0, eps)
     st = load().gtr_layernorm_fwd(ctypes.byref(a), torch._C._cuda_getCurrentRawStream(index))
     if st:
         raise GtrError("gtr_layernorm_fwd", st)
@@ -747,7 +753,7 @@ def _layernorm_bwd(dy, x, mean, rstd, weight, dres, want_dx, want_dw, dx, dw, db
         dw = torch.empty(d, dtype=f32, device=dev) if dw is None else dw
         db = torch.empty(d, dtype=f32, device=dev) if db is None else db
     a = LayernormBwdArgs(dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), _ptr(dres),
-                         _ptr(dx), _ptr(dw), _ptr(db), code, d, x.numel() // d if d else 0, bool(accumulate))
+                         _ptr(dx), _ptr(dw), _ptr(db), code, _i32(d), x.numel() // d if d else 0, bool(accumulate))
     lib, ref = load(), ctypes.byref(a)
     need = lib.gtr_layernorm_bwd_workspace_size(ref) if want_dw else 0
     if need:
@@ -815,7 +821,7 @@ def _ffn_fwd(x, w_gate, w_value, w_out, act, residual, save, y, gate, value, wor
                               ("value", value, kept)):
             _check(name, t, want, (dt,), dev)
     a = FfnFwdArgs(x.data_ptr(), w_gate.data_ptr(), w_value.data_ptr(), w_out.data_ptr(), _ptr(residual), y.data_ptr(),
-                   _ptr(gate), _ptr(value), _DT[dt], act, M, d, hidden)
+                   _ptr(gate), _ptr(value), _DT[dt], act, M, _i32(d), _i32(hidden))
     lib, ref = load(), ctypes.byref(a)
     need = lib.gtr_ffn_fwd_workspace_size(ref)
     if need:
@@ -876,8 +882,8 @@ def _ffn_bwd(dy, x, w_gate, w_value, w_out, gate, value, act, want_dx, want_dw, 
         dwv = torch.empty((hidden, d), dtype=wt, device=dev) if dwv is None else dwv
         dwo = torch.empty((d, hidden), dtype=wt, device=dev) if dwo is None else dwo
     a = FfnBwdArgs(dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_value.data_ptr(), w_out.data_ptr(), _ptr(gate),
-                   _ptr(value), _ptr(dx), _ptr(dwg), _ptr(dwv), _ptr(dwo), _DT[dt], _DT[wt], act, bool(accumulate), M, d,
-                   hidden)
+                   _ptr(value), _ptr(dx), _ptr(dwg), _ptr(dwv), _ptr(dwo), _DT[dt], _DT[wt], act, bool(accumulate), M,
+                   _i32(d), _i32(hidden))
     lib, ref = load(), ctypes.byref(a)
     need = lib.gtr_ffn_bwd_workspace_size(ref)
     if need:
