@@ -90,14 +90,6 @@ static gtr_status ffn_run_grads(FfnGemm& x, FfnGemm& w, int dt, const FfnPlan& p
   return ffn_add_slices(x, w, stream);
 }
 
-struct FfnRange {
-  const void* p;
-  size_t n;
-};
-static bool ffn_overlap(const FfnRange& a, const FfnRange& b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return a.p && b.p && x < y + b.n && y < x + a.n;
-}
 static bool ffn_misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
 // ---------------------------------------------------------------------------
@@ -136,13 +128,13 @@ static gtr_status ffn_fwd_check(const gtr_ffn_fwd_args* a, const FfnFwdPlan& f) 
   if (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 255u) || a->workspace_bytes < f.total)
     return GTR_ERR_WORKSPACE;
   const size_t rows = (size_t)a->M * a->d * 2, kept = (size_t)a->M * a->hidden * 2, w = (size_t)a->d * a->hidden * 2;
-  const FfnRange ins[] = {{a->x, rows}, {a->w_gate, w}, {a->w_value, w}, {a->w_out, w}, {a->residual, rows}};
-  const FfnRange outs[] = {{a->y, rows}, {a->gate, kept}, {a->value, kept}, {a->workspace, f.total}};
+  const Bytes ins[] = {{a->x, rows}, {a->w_gate, w}, {a->w_value, w}, {a->w_out, w}, {a->residual, rows}};
+  const Bytes outs[] = {{a->y, rows}, {a->gate, kept}, {a->value, kept}, {a->workspace, f.total}};
   for (int i = 0; i < 4; ++i) {
     for (int j = 0; j < 5; ++j)
-      if (ffn_overlap(outs[i], ins[j]) && !(i == 0 && j == 4 && a->y == a->residual)) return GTR_ERR_ALIAS;
+      if (bytes_meet(outs[i], ins[j]) && !(i == 0 && j == 4 && a->y == a->residual)) return GTR_ERR_ALIAS;
     for (int j = 0; j < i; ++j)
-      if (ffn_overlap(outs[i], outs[j])) return GTR_ERR_ALIAS;
+      if (bytes_meet(outs[i], outs[j])) return GTR_ERR_ALIAS;
   }
   return GTR_OK;
 }
@@ -161,13 +153,13 @@ static gtr_status ffn_bwd_check(const gtr_ffn_bwd_args* a, const FfnBwdPlan& f) 
     return GTR_ERR_WORKSPACE;
   const size_t rows = (size_t)a->M * a->d * 2, kept = (size_t)a->M * a->hidden * 2, w = (size_t)a->d * a->hidden * 2;
   const size_t dw = (size_t)a->d * a->hidden * dtype_size(a->dw_dtype);
-  const FfnRange ins[] = {{a->dy, rows}, {a->x, rows}, {a->w_gate, w}, {a->w_value, w}, {a->w_out, w}, {a->gate, kept}, {a->value, kept}};
-  const FfnRange outs[] = {{a->dx, rows}, {a->dw_gate, dw}, {a->dw_value, dw}, {a->dw_out, dw}, {a->workspace, f.total}};
+  const Bytes ins[] = {{a->dy, rows}, {a->x, rows}, {a->w_gate, w}, {a->w_value, w}, {a->w_out, w}, {a->gate, kept}, {a->value, kept}};
+  const Bytes outs[] = {{a->dx, rows}, {a->dw_gate, dw}, {a->dw_value, dw}, {a->dw_out, dw}, {a->workspace, f.total}};
   for (int i = 0; i < 5; ++i) {
     for (int j = 0; j < 7; ++j)
-      if (ffn_overlap(outs[i], ins[j])) return GTR_ERR_ALIAS;
+      if (bytes_meet(outs[i], ins[j])) return GTR_ERR_ALIAS;
     for (int j = 0; j < i; ++j)
-      if (ffn_overlap(outs[i], outs[j])) return GTR_ERR_ALIAS;
+      if (bytes_meet(outs[i], outs[j])) return GTR_ERR_ALIAS;
   }
   return GTR_OK;
 }

@@ -43,4 +43,14 @@ WorkspaceLayout gla_workspace_layout(const GlaShape& s);
 
 size_t dtype_size(int dt);
 
+// n bytes from p on (none if p is null), and whether two such have a byte in common.
+struct Bytes {
+  const void* p;
+  size_t n;
+};
+inline bool bytes_meet(const Bytes& a, const Bytes& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && x < y + b.n && y < x + a.n;
+}
+
 }  // namespace gtr

@@ -476,7 +476,8 @@ __global__ void __launch_bounds__(1024) ln_reduce_kernel(const float* __restrict
 }
 
 // How a row is shared: by the fewest lanes of a wave that hold it with one vector each,
-// a wave with two (no barrier: 25,600 x 768 bf16 backward 26.5 us against 39.2 as two waves), the fewest waves of a work-group, or all 16 with more vectors.
+// a wave with two (no barrier: 25,600 x 768 bf16 backward 26.5 us against 39.2 as two
+// waves), the fewest waves of a work-group, or all 16 with more vectors.
 constexpr int kLnMaxWidth = 16384;
 struct LnShape {
   int T, threads, NV;  // template arguments T and NV, the work-group's size
@@ -579,15 +580,6 @@ static gtr_status ln_launch(int dt, const L& a) {
   return hipGetLastError() == hipSuccess ? GTR_OK : GTR_ERR_HIP;
 }
 
-struct LnRange {
-  const void* p;
-  size_t n;
-};
-static bool ln_overlap(const LnRange& a, const LnRange& b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return a.p && b.p && x < y + b.n && y < x + a.n;
-}
-
 // The checks that both passes share: sizes, type.
 static gtr_status ln_sizes(int64_t M, int32_t d, int dt) {
   if (M <= 0 || d <= 0) return GTR_ERR_SHAPE;
@@ -615,15 +607,15 @@ static gtr_status ln_bwd_check(const gtr_layernorm_bwd_args* a, bool pointers, s
   const bool sums = a->dw || a->db;
   if (sums && *need && (!a->workspace || ln_misaligned(a->workspace, 256) || a->workspace_bytes < *need))
     return GTR_ERR_WORKSPACE;
-  const LnRange ins[] = {{a->dy, bytes}, {a->x, bytes}, {a->dres, bytes}, {a->mean, (size_t)a->M * 4},
+  const Bytes ins[] = {{a->dy, bytes}, {a->x, bytes}, {a->dres, bytes}, {a->mean, (size_t)a->M * 4},
                          {a->rstd, (size_t)a->M * 4}, {a->w, (size_t)a->d * 4}};
-  const LnRange outs[] = {{a->dx, bytes}, {a->dw, (size_t)a->d * 4}, {a->db, (size_t)a->d * 4},
+  const Bytes outs[] = {{a->dx, bytes}, {a->dw, (size_t)a->d * 4}, {a->db, (size_t)a->d * 4},
                           {sums && *need ? a->workspace : nullptr, *need}};
   for (int i = 0; i < 4; ++i) {
     for (int j = 0; j < 6; ++j)
-      if (ln_overlap(outs[i], ins[j]) && !(i == 0 && j < 3 && outs[i].p == ins[j].p)) return GTR_ERR_ALIAS;
+      if (bytes_meet(outs[i], ins[j]) && !(i == 0 && j < 3 && outs[i].p == ins[j].p)) return GTR_ERR_ALIAS;
     for (int j = 0; j < i; ++j)
-      if (ln_overlap(outs[i], outs[j])) return GTR_ERR_ALIAS;
+      if (bytes_meet(outs[i], outs[j])) return GTR_ERR_ALIAS;
   }
   return GTR_OK;
 }
@@ -642,13 +634,13 @@ extern "C" gtr_status gtr_layernorm_fwd(const gtr_layernorm_fwd_args* a, hipStre
   if (ln_misaligned(a->x, es) || ln_misaligned(a->y, es) || ln_misaligned(a->w, 4) || ln_misaligned(a->b, 4) ||
       ln_misaligned(a->mean, 4) || ln_misaligned(a->rstd, 4))
     return GTR_ERR_UNSUPPORTED;
-  const LnRange ins[] = {{a->x, bytes}, {a->w, (size_t)a->d * 4}, {a->b, (size_t)a->d * 4}};
-  const LnRange outs[] = {{a->y, bytes}, {a->mean, (size_t)a->M * 4}, {a->rstd, (size_t)a->M * 4}};
+  const Bytes ins[] = {{a->x, bytes}, {a->w, (size_t)a->d * 4}, {a->b, (size_t)a->d * 4}};
+  const Bytes outs[] = {{a->y, bytes}, {a->mean, (size_t)a->M * 4}, {a->rstd, (size_t)a->M * 4}};
   for (int i = 0; i < 3; ++i) {
     for (int j = 0; j < 3; ++j)
-      if (ln_overlap(outs[i], ins[j]) && !(i == 0 && j == 0 && a->x == a->y)) return GTR_ERR_ALIAS;
+      if (bytes_meet(outs[i], ins[j]) && !(i == 0 && j == 0 && a->x == a->y)) return GTR_ERR_ALIAS;
     for (int j = 0; j < i; ++j)
-      if (ln_overlap(outs[i], outs[j])) return GTR_ERR_ALIAS;
+      if (bytes_meet(outs[i], outs[j])) return GTR_ERR_ALIAS;
   }
   const LnShape s = ln_shape(a->d, a->dtype);
   const LnFwd p = {static_cast<const char*>(a->x), a->w, a->b, static_cast<char*>(a->y), a->mean, a->rstd, a->M, a->d, a->eps};
