@@ -486,8 +486,8 @@ typedef enum { GTR_ACT_SILU = 0, GTR_ACT_GELU = 1 } gtr_act;
  * x, y     : [M, d] dtype (GTR_F16 or GTR_BF16)
  * w_gate, w_value : [hidden, d], w_out : [d, hidden] dtype (output features first)
  * residual : [M, d] dtype or NULL; may be y (in place)
- * gate, value : [M, hidden] dtype, receive g and v for gtr_ffn_bwd; either may
- *            be NULL
+ * gate, value : [M, hidden] dtype, receive g and v for gtr_ffn_bwd (rounded to
+ *            dtype; in fp16 they must stay in range); either may be NULL
  * 1 <= M <= 2^30 (one token upwards); d and hidden multiples of 8, at most 2^20;
  * M d and M hidden at most 2^37, d hidden at most 2^36; every pointer 16-byte
  * aligned; an output overlaps nothing else.

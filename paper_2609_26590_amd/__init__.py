@@ -20,6 +20,10 @@ Entry points (same names as the C ABI in ``include/gtr.h``):
 * :func:`gtr_ffn_fwd`, :func:`gtr_ffn_bwd` - the gated feed-forward
   ``[act(x W_gate^T) * (x W_value^T)] W_out^T`` and its gradients.
 
+No call takes part in torch's automatic differentiation: results never require
+a gradient, whatever the arguments do. A training step calls the ``_bwd``
+functions itself (:mod:`paper_2609_26590_amd.mixer` shows the order).
+
 :class:`Workspace` keeps caller-owned workspace memory; one serves all of the calls above on one stream.
 """
 from __future__ import annotations

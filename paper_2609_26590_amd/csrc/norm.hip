@@ -8,9 +8,10 @@
 //             dx = rstd (t - sum t / d - xh sum (t xh) / d) (+ dres)
 //             dw = sum over the rows of dy xh,  db = sum over the rows of dy
 //
-// What bounds both is memory: each reads its rows once and writes them once (32768 x
-// 4096 bf16 forward 101.6 us, 5.3 TB/s; 16384 x 4096 bf16 backward with a residual 97
-// us, 5.5 TB/s; a large copy reaches 5.1), and for short batches the launches. A
+// What bounds both is memory: each reads its rows once and writes them once (calls one
+// after the other, of new inputs: 32768 x 4096 bf16 forward 103 us, 5.2 TB/s; 16384 x
+// 4096 bf16 backward with a residual 98 us, 5.5 TB/s; a large copy reaches 5.1), and for
+// short batches the launches. A
 // row lives in the registers of the lanes that share it (so the forward pass
 // takes the squares about the mean, with no second read), in 16-byte vectors at
 // whatever address the row starts: the vector loads and stores of this machine
@@ -190,8 +191,8 @@ struct LnFwd {
 
 // NV vectors per lane. A work-group takes the rows r = its index, + the grid, ..
 // (256 / T of them at a time, one if T is 0), keeps the affine weights in registers
-// (read for every row they are four times its bytes) and has the next row on its way
-// while it works on one (AHEAD: where that fits the registers).
+// between its rows (for each row they are four times its bytes, from cache) and has the
+// next row on its way while it works on one (AHEAD: where that fits the registers).
 // One vector per lane takes at most 64 registers: two work-groups of 16 waves per CU
 // (8192 x 8192 bf16: 64.5 us, with one 80.5).
 template <int DT, int T, int NV, bool TINY>
@@ -493,8 +494,13 @@ static LnShape ln_shape(int d, int dt) {
 }
 static int ln_rows(const LnShape& s) { return s.T ? 256 / s.T : 1; }  // of a work-group at a time
 
-// Work-groups of the forward pass: up to 32 waves' per CU four times over (32768 x 4096
-// bf16: 101.6 us; with those of one time 128, with one row each 173).
+// Work-groups of the forward pass: up to 32 waves' per CU four times over. So a batch of
+// up to 32768 rows of a wave each has one row per wave, and longer ones share the weights.
+// Us of launches one after the other, with these, half, a quarter, an eighth of them:
+// 12800 x 384 fp16 6.9, 7.0, 6.9, 7.4; 40000 x 384 fp16 17.7, 17.3, 18.1, 19.6; 30000 x
+// 1000 float32 47.4, 48.7, 49.0, 53.9; 32768 x 4096 bf16 103, 108, 112, 118 (with one row
+// each 173); but wider rows take less with fewer: 8192 x 8192 bf16 66, 60, 56, 73; 4096 x
+// 16384 bf16 74, 66, 62, 60.
 static int64_t ln_fwd_groups(int64_t M, const LnShape& s) {
   const int R = ln_rows(s);
   const int64_t all = (M + R - 1) / R, most = 256 * 8192 / s.threads;

@@ -10,7 +10,8 @@ libgtr calls, and its gradients:
 
 ``p`` holds ln_w, ln_b ([d] float32), w_gate, w_value ([hidden, d]) and w_out ([d,
 hidden], all in x's type). The calls allocate what they return and may be recorded
-into a HIP graph.
+into a HIP graph. Gradients come from ``backward`` alone: nothing is recorded for
+torch's automatic differentiation, also where x or p require a gradient.
 """
 from __future__ import annotations
 
