@@ -525,26 +525,32 @@ static int ln_column_groups(int d, int dt) {
   return (d + 2 * VE - 1) / (2 * VE);
 }
 // Whether dw and db are summed by columns: where that is sooner for calls one after the
-// other, which are paced by the host, by one launch or two (8.3 and 12.3 us), and dx does
+// other, which are paced by the host, by one launch or two (8.5 and 12.9 us), and dx does
 // not overwrite what is read. Work-groups that share the columns read every row, so it
-// takes longer with the rows (a round of loads per 8) and with the elements: measured at
-// 12 widths of three types, from 0.4 to 1.6 times the limit, the two are even at M (d +
-// 540) = 1.2 to 2.2 million, and at half of that where a work-group of more than 512
-// threads has a CU for itself; and where those are more than three rounds of the chip
-// (float32 past 6144 columns, 16 bits past 12288) by columns was not sooner at any M.
-// Us by columns / by partial sums: float16 1372 x 72 8.8 / 13.0, 3660 x 72 14.7 / 13.6;
-// 1333 x 300 11.8 / 13.2, 1833 x 300 13.8 / 12.9; 777 x 900 9.6 / 12.9, 1555 x 900
-// 14.6 / 12.8; 549 x 1500 9.4 / 12.8, 1098 x 1500 13.7 / 12.9; 92 x 6000 10.7 / 13.3;
-// float32 1583 x 300 10.7 / 13.0, 2666 x 300 14.5 / 12.9; 923 x 900 9.4 / 12.9, 1555 x 900
-// 13.4 / 13.0; 432 x 2048 10.7 / 12.9, 703 x 2048 15.0 / 13.1; 82 x 4096 10.2 / 12.9, 220
-// x 4096 14.8 / 13.1; 1 x 8192 14.0 / 12.2. For unaligned rows of 16 bits they are even at
-// 1.2 million (501 columns: 1075 rows 11.9 / 13.0, 1277 rows 14.3 / 12.9). Recorded into a
-// graph, where no host paces them, two launches are ahead from about 0.8 million on
-// (float16 1333 x 300 11.8 / 8.2, 777 x 900 9.6 / 10.9).
+// takes longer with the rows (a round of loads per 8) and with the elements: M (d + 540).
+// Measured at 32 widths of two types (and 12 of the third, bf16, like fp16) on both sides,
+// the two ways are even, in millions of that, at
+//   rows of a wave, one vector per lane   fp16 1.2 (unaligned rows) to 2.1, float32 1.8 to 2.0
+//   rows of a wave, two vectors           fp16 1.6 to 1.8, float32 1.8 to 1.9
+//   rows of a work-group                  fp16 1.75 up to 1536 columns, 2.3 to 3.3 beyond;
+//     float32 1.5 to 2.3, and of more than 512 threads (a CU holds one such) 0.65 to 1.0
+// and never, or within 3 %, where the columns are more than three rounds of work-groups that
+// have a CU for themselves (float32 past 6144 columns, 16 bits past 12288). Us by columns /
+// by partial sums below and above the limits taken: fp16 1333 x 300 11.8 / 13.2, 1833 x 300
+// 13.8 / 12.9; 923 x 900 10.5 / 12.9, 1555 x 900 14.6 / 12.8; 772 x 2048 11.5 / 12.9, 1159 x
+// 2048 15.8 / 13.7; 305 x 6000 17.4 / 19.9, 458 x 6000 21.5 / 20.1; float32 649 x 1000 8.6 /
+// 13.0, 1948 x 1000 15.8 / 13.2; 482 x 2048 11.6 / 12.9, 676 x 2048 14.6 / 12.9; 161 x 4096
+// 12.7 / 13.0, 215 x 4096 14.9 / 13.2; 1 x 8192 14.0 / 12.2. Recorded into a graph, where no
+// host paces them, two launches are ahead from about 0.8 million on (fp16 1333 x 300 11.8 /
+// 8.2, 777 x 900 9.6 / 10.9).
+static int64_t ln_columns_limit(const LnShape& s, int dt) {
+  if (s.T && s.NV == 1) return 1400000;
+  if (!s.T && dt != GTR_F32) return 2000000;
+  return s.threads > 512 ? 700000 : 1600000;
+}
 static bool ln_by_columns(const gtr_layernorm_bwd_args* a, const LnShape& s) {
-  const bool wide = s.threads > 512;
-  if (wide && ln_column_groups(a->d, a->dtype) > 3 * 256) return false;
-  return a->M * (a->d + 540) <= (wide ? 640000 : 1400000) && !(a->dx && (a->dx == a->dy || a->dx == a->x));
+  if (s.threads > 512 && ln_column_groups(a->d, a->dtype) > 3 * 256) return false;
+  return a->M * (a->d + 540) <= ln_columns_limit(s, a->dtype) && !(a->dx && (a->dx == a->dy || a->dx == a->x));
 }
 
 template <class P>
