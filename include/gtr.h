@@ -561,6 +561,100 @@ size_t gtr_ffn_bwd_workspace_size(const gtr_ffn_bwd_args* args);
 gtr_status gtr_ffn_bwd(const gtr_ffn_bwd_args* args, hipStream_t stream);
 
 /*
+ * The gated linear recurrence with a diagonal state (one number per channel where
+ * gtr_gla_fwd's state is dk numbers per value), trained and served: statuses,
+ * streams, checks, graphs and repeatable results as for the training calls above.
+ *
+ * gtr_recurrence_fwd: for every sequence and channel, visiting the tokens of the
+ * H x W grid in the order of `scan`,
+ *   h_t = a_t h_{t-1} + b_t,  b_t = x_t, or with complement (1 - a_t) x_t
+ * a_t = exp(g_t) with g_kind GTR_GATE_LOG_DECAY (-inf forgets all that was before),
+ * sigmoid(g_t)^(1 / gate_tau) with GTR_GATE_LOGITS (any g_t, infinities among them);
+ * an a_t below 2^-126 is 0.
+ * x, h  : [B, H*W, d] dtype (GTR_F32, GTR_F16 or GTR_BF16), tokens in SPATIAL order;
+ *         h may be x (in place, with the same row stride)
+ * g     : [B, H*W, d] g_dtype (dtype or GTR_F32)
+ * x_ld, g_ld : elements from row to row of x and g (0: d; at least d), the same
+ *         between sequences: the halves of one projection are read in place
+ * h0    : [B, d] float32, the state before the first token in scan order; NULL is 0
+ * h_final : [B, d] float32, receives the state after the last one, or NULL; may be
+ *         h0 itself, so one call of H = W = 1 is a server's step in place
+ * Any d >= 1 and H*W < 2^31 (one token upwards; a 1-D sequence is H = 1), no
+ * alignment beyond an element's; a launch's threads stay below 2^32, which passes
+ * over B d H W of about 2^40 / 4. Gates and states are float32, h is rounded once.
+ * workspace : where gtr_recurrence_fwd_workspace_size(args) is not 0 (sequences of
+ *         more tokens than a work-group takes): 256-byte aligned, at least that many
+ *         bytes, no initialisation needed; calls that overlap in time must not share
+ *         one. It is left with any contents: never a gtr_gla_fwd workspace.
+ * spin_limit : polls of a wait between a sequence's work-groups before it gives up
+ *         and the states become NaN from there on (0: the library's default, seconds;
+ *         no wait depends on work that has not started). A small one is for tests.
+ */
+typedef struct {
+  const void* x;
+  const void* g;
+  void* h;
+  const float* h0;
+  float* h_final;
+  gtr_dtype dtype;
+  gtr_dtype g_dtype;
+  gtr_gate_kind g_kind;
+  float gate_tau;
+  int32_t complement;
+  int32_t B, H, W, d;
+  gtr_scan scan;
+  int64_t x_ld, g_ld;
+  void* workspace;
+  size_t workspace_bytes;
+  uint32_t spin_limit;
+} gtr_recurrence_fwd_args;
+
+size_t gtr_recurrence_fwd_workspace_size(const gtr_recurrence_fwd_args* args);
+gtr_status gtr_recurrence_fwd(const gtr_recurrence_fwd_args* args, hipStream_t stream);
+
+/*
+ * gtr_recurrence_bwd: the gradients of gtr_recurrence_fwd. With
+ * D_t = dh_t + a_{t+1} D_{t+1} (dh_final in place of the product behind the last
+ * token):
+ *   dx_t = D_t, or with complement (1 - a_t) D_t
+ *   d log a_t = a_t D_t (h_{t-1} [- x_t]);  dg_t = d log a_t, or with logits
+ *   d log a_t sigmoid(-g_t) / gate_tau
+ *   dh0 = a_1 D_1
+ * dh, h : [B, H*W, d] dtype, contiguous; h as gtr_recurrence_fwd left it (h_{t-1} is
+ *          read from it, rounded to dtype as it is; h0 before the first token)
+ * x      : needed with complement only
+ * dx, dg : in dtype and g_dtype, rows dx_ld and dg_ld elements apart (0: d); either may
+ *          be NULL. Each may lie where dh, g or x does, row on row (so may not h).
+ * dh_final, dh0 : [B, d] float32 or NULL; dh0 may be dh_final
+ * Sizes, strides, workspace and spin_limit as for gtr_recurrence_fwd.
+ */
+typedef struct {
+  const void* dh;
+  const void* g;
+  const void* h;
+  const void* x;
+  const float* h0;
+  const float* dh_final;
+  void* dx;
+  void* dg;
+  float* dh0;
+  gtr_dtype dtype;
+  gtr_dtype g_dtype;
+  gtr_gate_kind g_kind;
+  float gate_tau;
+  int32_t complement;
+  int32_t B, H, W, d;
+  gtr_scan scan;
+  int64_t x_ld, g_ld, dx_ld, dg_ld;
+  void* workspace;
+  size_t workspace_bytes;
+  uint32_t spin_limit;
+} gtr_recurrence_bwd_args;
+
+size_t gtr_recurrence_bwd_workspace_size(const gtr_recurrence_bwd_args* args);
+gtr_status gtr_recurrence_bwd(const gtr_recurrence_bwd_args* args, hipStream_t stream);
+
+/*
  * gtr_gla_fwd_noalloc - gtr_gla_fwd for callers that cannot allocate device
  * memory (code under HIP graph capture, serving loops, harnesses that forbid
  * hipMalloc). Same arguments, results and schedules as gtr_gla_fwd, except

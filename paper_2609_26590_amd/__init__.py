@@ -19,6 +19,9 @@ Entry points (same names as the C ABI in ``include/gtr.h``):
   for training, with the gradients of input, weight and bias.
 * :func:`gtr_ffn_fwd`, :func:`gtr_ffn_bwd` - the gated feed-forward
   ``[act(x W_gate^T) * (x W_value^T)] W_out^T`` and its gradients.
+* :func:`gtr_recurrence_fwd`, :func:`gtr_recurrence_bwd` - the gated linear
+  recurrence with a diagonal state, ``h_t = a_t h_{t-1} + b_t`` along the four
+  scan orders, from single tokens to long sequences, and its gradients.
 
 No call takes part in torch's automatic differentiation: results never require
 a gradient, whatever the arguments do. A training step calls the ``_bwd``
@@ -51,7 +54,8 @@ EXPORTS = ("gtr_scan_permute", "gtr_gla_workspace_size", "gtr_gla_workspace_init
            "gtr_gla_schedule", "gtr_gla_value_parts", "gtr_gla_segment_chunks", "gtr_gla_workspace_fault", "gtr_status_string", "gtr_spatial_swiglu_workspace_size",
            "gtr_spatial_swiglu", "gtr_gemm", "gtr_layernorm", "gtr_heads_split", "gtr_heads_merge", "gtr_add",
            "gtr_layernorm_fwd", "gtr_layernorm_bwd_workspace_size", "gtr_layernorm_bwd", "gtr_ffn_fwd_workspace_size",
-           "gtr_ffn_fwd", "gtr_ffn_bwd_workspace_size", "gtr_ffn_bwd")
+           "gtr_ffn_fwd", "gtr_ffn_bwd_workspace_size", "gtr_ffn_bwd", "gtr_recurrence_fwd_workspace_size",
+           "gtr_recurrence_fwd", "gtr_recurrence_bwd_workspace_size", "gtr_recurrence_bwd")
 
 
 class GtrError(RuntimeError):
@@ -142,6 +146,31 @@ class FfnBwdArgs(ctypes.Structure):
     ]
 
 
+class RecurrenceFwdArgs(ctypes.Structure):
+    """Mirror of ``gtr_recurrence_fwd_args`` (include/gtr.h)."""
+    _fields_ = [
+        ("x", ctypes.c_void_p), ("g", ctypes.c_void_p), ("h", ctypes.c_void_p), ("h0", ctypes.c_void_p),
+        ("h_final", ctypes.c_void_p), ("dtype", ctypes.c_int), ("g_dtype", ctypes.c_int), ("g_kind", ctypes.c_int),
+        ("gate_tau", ctypes.c_float), ("complement", ctypes.c_int32), ("B", ctypes.c_int32), ("H", ctypes.c_int32),
+        ("W", ctypes.c_int32), ("d", ctypes.c_int32), ("scan", ctypes.c_int), ("x_ld", ctypes.c_int64),
+        ("g_ld", ctypes.c_int64), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("spin_limit", ctypes.c_uint32),
+    ]
+
+
+class RecurrenceBwdArgs(ctypes.Structure):
+    """Mirror of ``gtr_recurrence_bwd_args`` (include/gtr.h)."""
+    _fields_ = [
+        ("dh", ctypes.c_void_p), ("g", ctypes.c_void_p), ("h", ctypes.c_void_p), ("x", ctypes.c_void_p),
+        ("h0", ctypes.c_void_p), ("dh_final", ctypes.c_void_p), ("dx", ctypes.c_void_p), ("dg", ctypes.c_void_p),
+        ("dh0", ctypes.c_void_p), ("dtype", ctypes.c_int), ("g_dtype", ctypes.c_int), ("g_kind", ctypes.c_int),
+        ("gate_tau", ctypes.c_float), ("complement", ctypes.c_int32), ("B", ctypes.c_int32), ("H", ctypes.c_int32),
+        ("W", ctypes.c_int32), ("d", ctypes.c_int32), ("scan", ctypes.c_int), ("x_ld", ctypes.c_int64),
+        ("g_ld", ctypes.c_int64), ("dx_ld", ctypes.c_int64), ("dg_ld", ctypes.c_int64), ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t), ("spin_limit", ctypes.c_uint32),
+    ]
+
+
 _lib = None
 
 
@@ -191,7 +220,8 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.gtr_add.argtypes = [P, P, P, I64, ctypes.c_int, P]
     lib.gtr_add.restype = ctypes.c_int
     for name, args in (("gtr_layernorm_fwd", LayernormFwdArgs), ("gtr_layernorm_bwd", LayernormBwdArgs),
-                       ("gtr_ffn_fwd", FfnFwdArgs), ("gtr_ffn_bwd", FfnBwdArgs)):
+                       ("gtr_ffn_fwd", FfnFwdArgs), ("gtr_ffn_bwd", FfnBwdArgs),
+                       ("gtr_recurrence_fwd", RecurrenceFwdArgs), ("gtr_recurrence_bwd", RecurrenceBwdArgs)):
         getattr(lib, name).argtypes = [ctypes.POINTER(args), P]
         getattr(lib, name).restype = ctypes.c_int
         if args is not LayernormFwdArgs:
@@ -897,3 +927,143 @@ def _ffn_bwd(dy, x, w_gate, w_value, w_out, gate, value, act, want_dx, want_dw, 
     if st:
         raise GtrError("gtr_ffn_bwd", st)
     return dx, dwg, dwv, dwo
+
+
+# ---------------------------------------------------------------------------
+# a token mixer with a diagonal state: gtr_recurrence_fwd / gtr_recurrence_bwd
+# ---------------------------------------------------------------------------
+def _row_stride(name: str, t: torch.Tensor, shape, dtypes, dev: torch.device) -> int:
+    """Elements from row to row of t [B, L, d], which may be a part of wider rows (0: contiguous)."""
+    if t.shape == shape and t.dtype in dtypes and t.device == dev:
+        if t.is_contiguous():
+            return 0
+        B, L, d = shape
+        ld = t.stride(1) if L > 1 else t.stride(0)
+        if (d == 1 or t.stride(2) == 1) and (B == 1 or t.stride(0) == L * ld) and ld >= d:
+            return ld
+        raise ValueError(f"{name} must be rows of a last dimension without gaps, evenly spaced over its tokens")
+    if t.device != dev:
+        raise ValueError(f"{name} must be on {dev}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    raise ValueError(f"{name} has dtype {t.dtype}, expected one of {list(dtypes)}")
+
+
+def _rec_shape(name, t, H, W, scan, gate_tau) -> torch.Size:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dim() != 3 or t.dtype not in _DT or t.shape[1] != H * W:
+        raise ValueError(f"{name} must be [B, H*W, d] of float32, float16 or bfloat16 with H*W = {H * W}")
+    if scan not in SCANS:
+        raise ValueError(f"scan must be one of {sorted(SCANS)}")
+    if gate_tau is not None and not gate_tau > 0:
+        raise ValueError("gate_tau must be positive")
+    return t.shape
+
+
+def gtr_recurrence_fwd(x: torch.Tensor, g: torch.Tensor, *, H: int, W: int, scan: str = "row",
+                       gate_tau: Optional[float] = None, complement: bool = False, h0: Optional[torch.Tensor] = None,
+                       want_final: bool = False, out: Optional[torch.Tensor] = None,
+                       h_final: Optional[torch.Tensor] = None, workspace: Optional["Workspace"] = None, stream=None,
+                       spin_limit: int = 0):
+    """The gated linear recurrence h_t = a_t h_{t-1} + b_t, channel by channel, over the tokens of x [B, H*W, d]
+    (float32, fp16 or bf16, spatial order; a 1-D sequence is H = 1) in the order of ``scan``.
+
+    a_t = exp(g_t), or with ``gate_tau`` sigmoid(g_t)^(1 / gate_tau); b_t = x_t, or with ``complement`` (1 - a_t) x_t.
+    g is of x's shape, in its type or float32. x and g may be parts of wider rows (the halves of one projection).
+    ``h0`` [B, d] float32: the state before the first token (zeros). ``out`` may be x. ``h_final`` [B, d] float32 (made
+    with ``want_final``) receives the state after the last token and may be h0: a server's step is one call with
+    H = W = 1 that keeps its state in place. Returns ``(h, h_final)``."""
+    _rec_shape("x", x, H, W, scan, gate_tau)
+    if stream is None and x.get_device() == torch._C._cuda_getDevice():
+        return _recurrence_fwd(x, g, H, W, scan, gate_tau, complement, h0, want_final, out, h_final, workspace, spin_limit)
+    return _on_stream(_recurrence_fwd, stream, (x, g, h0, out, h_final),
+                      (x, g, H, W, scan, gate_tau, complement, h0, want_final, out, h_final, workspace, spin_limit))
+
+
+def _recurrence_fwd(x, g, H, W, scan, gate_tau, complement, h0, want_final, h, last, workspace, spin):
+    shape, dev, dt, f32 = x.shape, x.device, x.dtype, torch.float32
+    x_ld = _row_stride("x", x, shape, (dt,), dev)
+    g_ld = _row_stride("g", g, shape, (dt, f32), dev)
+    state, index = (shape[0], shape[2]), dev.index
+    if h is None:
+        h = torch.empty(shape, dtype=dt, device=dev)
+    if last is None and want_final:
+        last = torch.empty(state, dtype=f32, device=dev)
+    if not (_is(h, shape, dt, index) and _is(h0, state, f32, index) and _is(last, state, f32, index)):
+        _check("out", h, shape, (dt,), dev)
+        _check("h0", h0, state, (f32,), dev)
+        _check("h_final", last, state, (f32,), dev)
+    a = RecurrenceFwdArgs(x.data_ptr(), g.data_ptr(), h.data_ptr(), _ptr(h0), _ptr(last), _DT[dt], _DT[g.dtype],
+                          GATE_LOG_DECAY if gate_tau is None else GATE_LOGITS, 0.0 if gate_tau is None else gate_tau,
+                          bool(complement), _i32(shape[0]), _i32(H), _i32(W), _i32(shape[2]), SCANS[scan], x_ld, g_ld,
+                          None, 0, spin)
+    lib, ref = load(), ctypes.byref(a)
+    need = lib.gtr_recurrence_fwd_workspace_size(ref)
+    if need:
+        buf = _scratch(need, dev, workspace)
+        a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel()
+    st = lib.gtr_recurrence_fwd(ref, torch._C._cuda_getCurrentRawStream(index))
+    if st:
+        raise GtrError("gtr_recurrence_fwd", st)
+    return h, last
+
+
+def gtr_recurrence_bwd(dh: torch.Tensor, g: torch.Tensor, h: torch.Tensor, x: Optional[torch.Tensor] = None, *, H: int,
+                       W: int, scan: str = "row", gate_tau: Optional[float] = None, complement: bool = False,
+                       h0: Optional[torch.Tensor] = None, dh_final: Optional[torch.Tensor] = None, want_dx: bool = True,
+                       want_dg: bool = True, want_dh0: bool = False, out: Optional[torch.Tensor] = None,
+                       dg: Optional[torch.Tensor] = None, dh0: Optional[torch.Tensor] = None,
+                       workspace: Optional["Workspace"] = None, stream=None, spin_limit: int = 0):
+    """Gradients of :func:`gtr_recurrence_fwd`: ``(dx, dg, dh0)``, from the h that it returned.
+
+    ``dh`` [B, H*W, d] is h's gradient, ``dh_final`` [B, d] float32 that of the last state; x is needed with
+    ``complement`` only. dx is in dh's type, dg in g's, dh0 [B, d] float32 (made with ``want_dh0``, or where given).
+    ``out`` (for dx) and ``dg`` may be parts of wider rows, and may lie where dh, g or x does. What is not wanted is
+    None."""
+    if complement and x is None:
+        raise ValueError("complement needs x")
+    _rec_shape("dh", dh, H, W, scan, gate_tau)
+    args = (dh, g, h, x if complement else None, H, W, scan, gate_tau, complement, h0, dh_final, want_dx, want_dg,
+            want_dh0, out, dg, dh0, workspace, spin_limit)
+    if stream is None and dh.get_device() == torch._C._cuda_getDevice():
+        return _recurrence_bwd(*args)
+    return _on_stream(_recurrence_bwd, stream, (dh, g, h, x, h0, dh_final, out, dg, dh0), args)
+
+
+def _recurrence_bwd(dh, g, h, x, H, W, scan, gate_tau, complement, h0, dlast, want_dx, want_dg, want_dh0, dx, dg, dh0,
+                    workspace, spin):
+    shape, dev, dt, f32 = dh.shape, dh.device, dh.dtype, torch.float32
+    state, index = (shape[0], shape[2]), dev.index
+    if not (_is(dh, shape, dt, index) and h is not None and _is(h, shape, dt, index) and _is(h0, state, f32, index) and
+            _is(dlast, state, f32, index) and _is(dh0, state, f32, index)):
+        for name, t, want, of in (("dh", dh, shape, dt), ("h", h, shape, dt), ("h0", h0, state, f32),
+                                  ("dh_final", dlast, state, f32), ("dh0", dh0, state, f32)):
+            _check(name, t, want, (of,), dev)
+    g_ld = _row_stride("g", g, shape, (dt, f32), dev)
+    x_ld = 0 if x is None else _row_stride("x", x, shape, (dt,), dev)
+    if not want_dx:
+        dx = None
+    elif dx is None:
+        dx = torch.empty(shape, dtype=dt, device=dev)
+    if not want_dg:
+        dg = None
+    elif dg is None:
+        dg = torch.empty(shape, dtype=g.dtype, device=dev)
+    if dh0 is None and want_dh0:
+        dh0 = torch.empty(state, dtype=f32, device=dev)
+    dx_ld = 0 if dx is None else _row_stride("out", dx, shape, (dt,), dev)
+    dg_ld = 0 if dg is None else _row_stride("dg", dg, shape, (g.dtype,), dev)
+    a = RecurrenceBwdArgs(dh.data_ptr(), g.data_ptr(), h.data_ptr(), _ptr(x), _ptr(h0), _ptr(dlast), _ptr(dx), _ptr(dg),
+                          _ptr(dh0), _DT[dt], _DT[g.dtype], GATE_LOG_DECAY if gate_tau is None else GATE_LOGITS,
+                          0.0 if gate_tau is None else gate_tau, bool(complement), _i32(shape[0]), _i32(H), _i32(W),
+                          _i32(shape[2]), SCANS[scan], x_ld, g_ld, dx_ld, dg_ld, None, 0, spin)
+    lib, ref = load(), ctypes.byref(a)
+    need = lib.gtr_recurrence_bwd_workspace_size(ref)
+    if need:
+        buf = _scratch(need, dev, workspace)
+        a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel()
+    st = lib.gtr_recurrence_bwd(ref, torch._C._cuda_getCurrentRawStream(index))
+    if st:
+        raise GtrError("gtr_recurrence_bwd", st)
+    return dx, dg, dh0

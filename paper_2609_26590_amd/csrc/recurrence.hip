@@ -1,0 +1,790 @@
+// The gated linear recurrence with a diagonal state, channel by channel along one of the
+// four scan orders, and its gradients, in float32:
+//
+//   la_t = g_t, or logsigmoid(g_t) / tau;   a_t = exp(la_t)
+//   h_t = a_t h_{t-1} + b_t,   b_t = x_t, or (1 - a_t) x_t
+//
+//   Y_t = a_t D_t,  D_t = dh_t + Y_{t+1}   (Y behind the last token: the last state's gradient)
+//   dx_t = D_t, or (1 - a_t) D_t;   dla_t = Y_t (h_{t-1} [- x_t]);   dg_t = dla_t, or
+//   dla_t sigmoid(-g_t) / tau;   dh_0 = Y_1
+//
+// Both are a scan of affine maps s -> P s + E, which compose; the backward one runs in
+// the reversed order. What bounds them is memory: every array once (scan_tile).
+#include <hip/hip_runtime.h>
+
+#include "gtr.h"
+#include "gtr_device.h"
+#include "gtr_internal.h"
+
+namespace gtr {
+
+// ---------------------------------------------------------------------------
+// rows
+// ---------------------------------------------------------------------------
+// V consecutive elements of a row, at any element address (the machine's vector loads and
+// stores need no alignment beyond an element's), in whole words.
+template <int BYTES>
+struct __attribute__((packed, aligned(2))) RecRaw {
+  unsigned u[BYTES / 4];
+};
+template <>
+struct RecRaw<2> {
+  unsigned short u[1];
+};
+template <int DT, int V>
+struct RecVec {
+  static constexpr int ES = DT == GTR_F32 ? 4 : 2;
+  RecRaw<V * ES> r;
+  __device__ __forceinline__ void load(const char* p) { r = *reinterpret_cast<const RecRaw<V * ES>*>(p); }
+  __device__ __forceinline__ void store(char* p) const { *reinterpret_cast<RecRaw<V * ES>*>(p) = r; }
+  __device__ __forceinline__ unsigned short half(int v) const {
+    return (unsigned short)(v & 1 ? r.u[v / 2] >> 16 : r.u[v / 2] & 0xffffu);
+  }
+  __device__ __forceinline__ float get(int v) const {
+    if constexpr (DT == GTR_F32)
+      return __builtin_bit_cast(float, r.u[v]);
+    else if constexpr (DT == GTR_F16)
+      return (float)__builtin_bit_cast(_Float16, half(v));
+    else
+      return bf16_bits_to_f32(half(v));
+  }
+  __device__ __forceinline__ void set(const float (&x)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if constexpr (DT == GTR_F32) {
+        r.u[v] = __builtin_bit_cast(unsigned, x[v]);
+      } else {
+        unsigned short b;
+        if constexpr (DT == GTR_F16)
+          b = __builtin_bit_cast(unsigned short, (_Float16)x[v]);
+        else
+          b = __builtin_bit_cast(unsigned short, (__bf16)x[v]);
+        r.u[v / 2] = v & 1 ? r.u[v / 2] | (unsigned)b << 16 : b;
+      }
+    }
+  }
+  __device__ __forceinline__ void store1(char* p, int v) const {
+    if constexpr (DT == GTR_F32)
+      *reinterpret_cast<unsigned*>(p + 4 * v) = r.u[v];
+    else
+      *reinterpret_cast<unsigned short*>(p + 2 * v) = half(v);
+  }
+};
+
+// The rows that a scan visits one after the other, from step s on. Uniform over a wave.
+struct RecWalk {
+  int64_t row;         // spatial index of the present step
+  int64_t step, wrap;  // to the next one, within a grid column and behind its end
+  int left, run;       // steps to that end; steps of a whole column less one
+  __device__ __forceinline__ RecWalk(int64_t s, int64_t L, int H, int W, int dir) {
+    const bool back = dir == GTR_SCAN_ROW_REV || dir == GTR_SCAN_COL_REV;
+    const unsigned at = (unsigned)(back ? L - 1 - s : s);  // (L is below 2^31)
+    if (dir == GTR_SCAN_ROW || dir == GTR_SCAN_ROW_REV) {
+      row = at;
+      step = wrap = back ? -1 : 1;
+      left = run = 0x7fffffff;
+    } else {
+      const unsigned j = at / (unsigned)H, i = at - j * (unsigned)H;
+      const int64_t to_top = (int64_t)(H - 1) * W - 1;
+      row = (int64_t)i * W + j;
+      step = back ? -W : W;
+      wrap = back ? to_top : -to_top;
+      left = back ? (int)i : H - 1 - (int)i;
+      run = H - 1;
+    }
+  }
+  __device__ __forceinline__ void next() {
+    const bool end = left == 0;
+    row += end ? wrap : step;
+    left = end ? run : left - 1;
+  }
+};
+
+// ---------------------------------------------------------------------------
+// gates
+// ---------------------------------------------------------------------------
+// log(1 + u) for 0 <= u <= 1 as log(w) u / (w - 1), w = 1 + u as rounded: the quotient
+// takes back the rounding of w, so that small u keep their relative accuracy.
+__device__ __forceinline__ float log1p_unit(float u) {
+  const float w = 1.f + u, m = w - 1.f;
+  const float r = __builtin_amdgcn_logf(w) * 0.693147180559945309f * u * __builtin_amdgcn_rcpf(m);
+  return m == 0.f ? u : r;
+}
+// 1 - exp(la), of which a = exp(la): as the exponential's series about 0 up to 1/2
+// (what is left out is under 2^-26 of it), else as it stands.
+__device__ __forceinline__ float one_minus_exp(float la, float a) {
+  float s = 1.f / 40320.f;
+  s = fmaf(s, la, 1.f / 5040.f);
+  s = fmaf(s, la, 1.f / 720.f);
+  s = fmaf(s, la, 1.f / 120.f);
+  s = fmaf(s, la, 1.f / 24.f);
+  s = fmaf(s, la, 1.f / 6.f);
+  s = fmaf(s, la, 0.5f);
+  s = fmaf(s, la, 1.f);
+  return fabsf(la) < 0.5f ? -la * s : 1.f - a;
+}
+// a, 1 - a where KEEP, and d la / d g where SLOPE.
+template <bool LOGITS, bool KEEP, bool SLOPE>
+__device__ __forceinline__ void rec_gate(float g, float inv_tau, float& a, float& keep, float& slope) {
+  float la = g;
+  if constexpr (LOGITS) {
+    const float u = __builtin_amdgcn_exp2f(-fabsf(g) * 1.44269504088896341f);
+    la = (fminf(g, 0.f) - log1p_unit(u)) * inv_tau;
+    if constexpr (SLOPE) slope = (g < 0.f ? 1.f : u) * __builtin_amdgcn_rcpf(1.f + u) * inv_tau;
+  }
+  a = __builtin_amdgcn_exp2f(la * 1.44269504088896341f);
+  if constexpr (KEEP) keep = one_minus_exp(la, a);
+}
+
+// ---------------------------------------------------------------------------
+// the scan of a tile
+// ---------------------------------------------------------------------------
+// A work-group takes a tile: the channels of a block (V per lane), T steps per wave. Each
+// wave composes its own steps (P, E), the waves' maps meet in LDS, and the state before
+// the tile comes from the tiles before it in one launch, by look-back:
+//
+//   - every tile hands on its map, in one 64-bit word per channel that is its own flag:
+//     zero until it is written (~P in the low half, which no P leaves zero). Words travel by
+//     device-scope atomic loads and stores, so no cache is written back or dropped for them;
+//   - tiles are in groups. The last tile of a group hands on the state behind the group,
+//     for which it waits for that of the group before. A tile composes the maps of the tiles
+//     before it in its group, shared out over its waves, and applies them to that state.
+//
+// So a sequence of n tiles has a chain of n / group hand-overs, and the composition is the
+// same whatever the order in which work-groups run: results do not depend on it. Tiles are
+// numbered by a counter as their work-groups start, the first steps of all sequences first:
+// what a tile waits for has started before it, and a map is handed on before anything is
+// waited for, so every wait ends on any number of compute units. (Waits are bounded all the
+// same: one that runs out makes the states NaN from there on.)
+struct RecTiles {
+  unsigned long long* maps;    // [sequences][tiles][64 V]
+  unsigned long long* states;  // [sequences][groups][64 V]
+  unsigned* counter;           // the next tile; null where a sequence is one tile
+  int tiles, group, groups, blocks;
+  unsigned spin;
+};
+
+constexpr int kRecWaves = 16;
+
+__device__ __forceinline__ unsigned long long rec_word(float P, float E) {
+  unsigned lo = ~__builtin_bit_cast(unsigned, P);
+  lo = lo ? lo : ~0x7fc00000u;  // (a NaN with every bit set becomes another one)
+  return (unsigned long long)__builtin_bit_cast(unsigned, E) << 32 | lo;
+}
+__device__ __forceinline__ float rec_map(unsigned long long w) { return __builtin_bit_cast(float, ~(unsigned)w); }
+__device__ __forceinline__ float rec_add(unsigned long long w) { return __builtin_bit_cast(float, (unsigned)(w >> 32)); }
+
+// N lanes' words of this lane's V channels, once all lanes have all of theirs.
+template <int V, int N>
+__device__ __forceinline__ void rec_wait(unsigned long long (&w)[N][V], const unsigned long long* const (&at)[N],
+                                         unsigned spin) {
+  for (unsigned n = 0;; ++n) {
+    bool all = true;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        w[i][v] = __hip_atomic_load(at[i] + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        all &= (unsigned)w[i][v] != 0u;
+      }
+    if (__all(all)) return;
+    if (n >= spin) break;
+    __builtin_amdgcn_s_sleep(1);
+  }
+  const float nan = __builtin_bit_cast(float, 0x7fc00000u);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int v = 0; v < V; ++v) w[i][v] = rec_word(nan, nan);
+}
+
+struct RecWhere {
+  int tile, seq, b, block;  // uniform
+};
+// Which tile this work-group takes.
+__device__ __forceinline__ RecWhere rec_where(const RecTiles& t, unsigned sequences) {
+  unsigned id = blockIdx.x;
+  if (t.counter) {
+    __shared__ unsigned mine;
+    if (threadIdx.x == 0) mine = atomicAdd(t.counter, 1u);
+    __syncthreads();
+    id = (unsigned)__builtin_amdgcn_readfirstlane((int)mine);
+  }
+  RecWhere w;
+  w.tile = (int)(id / sequences);
+  w.seq = (int)(id % sequences);
+  w.b = w.seq / t.blocks;
+  w.block = w.seq % t.blocks;
+  return w;
+}
+
+// The state s before this wave's steps, of which (P, E) is the map. The first wave of a
+// sequence comes with the state before the sequence as s and with the map that leads to its
+// last state from anywhere (P = 0), so that nobody else reads the first state: a caller's
+// may lie where the last state goes.
+template <int V>
+__device__ __forceinline__ void rec_carry(const RecTiles& t, const RecWhere& at, int wave, int lane, const float (&P)[V],
+                                          const float (&E)[V], float (&s)[V]) {
+  constexpr int CB = 64 * V;
+  __shared__ float own[kRecWaves][2][CB], before[kRecWaves][2][CB], behind[CB];
+  const int waves = blockDim.x >> 6, c = lane * V;
+  if (waves == 1 && t.tiles == 1) return;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    own[wave][0][c + v] = P[v];
+    own[wave][1][c + v] = E[v];
+  }
+  __syncthreads();
+  const int group = at.tile / t.group, k = at.tile % t.group;  // k tiles before it in its group
+  const bool hands_state = k == t.group - 1, last = at.tile == t.tiles - 1;
+  float tP[V], tE[V];
+  if (wave == 0 && !last) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      tP[v] = 1.f;
+      tE[v] = 0.f;
+    }
+    for (int w = 0; w < waves; ++w)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float p = own[w][0][c + v];
+        tE[v] = fmaf(p, tE[v], own[w][1][c + v]);
+        tP[v] *= p;
+      }
+    if (!hands_state) {
+      unsigned long long* m = t.maps + ((int64_t)at.seq * t.tiles + at.tile) * CB + c;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        __hip_atomic_store(m + v, rec_word(tP[v], tE[v]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+  if (at.tile > 0) {
+    const int per = (k + waves - 1) / waves, j0 = wave * per, j1 = min(k, j0 + per);
+    float bP[V], bE[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      bP[v] = 1.f;
+      bE[v] = 0.f;
+    }
+    constexpr int U = 4;
+    const unsigned long long* m = t.maps + ((int64_t)at.seq * t.tiles + (int64_t)group * t.group) * CB + c;
+    for (int j = j0; j < j1; j += U) {
+      unsigned long long w[U][V];
+      const unsigned long long* p[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) p[u] = m + (int64_t)min(j + u, j1 - 1) * CB;
+      rec_wait<V, U>(w, p, t.spin);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (j + u >= j1) break;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          bE[v] = fmaf(rec_map(w[u][v]), bE[v], rec_add(w[u][v]));
+          bP[v] *= rec_map(w[u][v]);
+        }
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      before[wave][0][c + v] = bP[v];
+      before[wave][1][c + v] = bE[v];
+    }
+    if (wave == waves - 1) {  // (the wave with the fewest maps)
+      float g[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) g[v] = 0.f;
+      if (group > 0) {
+        unsigned long long w[1][V];
+        const unsigned long long* p[1] = {t.states + ((int64_t)at.seq * t.groups + group - 1) * CB + c};
+        rec_wait<V, 1>(w, p, t.spin);
+#pragma unroll
+        for (int v = 0; v < V; ++v) g[v] = rec_add(w[0][v]);
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) behind[c + v] = g[v];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[v] = behind[c + v];
+    const int used = min(waves, per ? (k + per - 1) / per : 0);
+    for (int w = 0; w < used; ++w)
+#pragma unroll
+      for (int v = 0; v < V; ++v) s[v] = fmaf(before[w][0][c + v], s[v], before[w][1][c + v]);
+  }
+  if (wave == 0 && hands_state && !last) {
+    unsigned long long* m = t.states + ((int64_t)at.seq * t.groups + group) * CB + c;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      __hip_atomic_store(m + v, rec_word(0.f, fmaf(tP[v], s[v], tE[v])), __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+  }
+  for (int w = 0; w < wave; ++w)
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[v] = fmaf(own[w][0][c + v], s[v], own[w][1][c + v]);
+}
+
+struct RecFwd {
+  RecTiles t;
+  const char *x, *g;
+  char* h;
+  const float* h0;
+  float* h_final;
+  int64_t x_ld, g_ld;  // bytes from row to row
+  int64_t L;
+  int H, W, d, dir;
+  unsigned sequences;
+  float inv_tau;
+};
+
+// A lane's V channels from c on: the last lane of an odd width starts early and leaves
+// the `skip` channels that are another lane's to it; lanes past the width repeat the last
+// one's and store nothing.
+template <int V>
+struct RecCols {
+  int c, skip;
+  __device__ __forceinline__ RecCols(int block, int lane, int d) {
+    const int at = (block * 64 + lane) * V;
+    c = min(at, d - V);
+    skip = min(V, at - c);
+  }
+};
+template <int DT, int V>
+__device__ __forceinline__ void rec_store(const RecVec<DT, V>& r, char* p, int skip) {
+  if (skip == 0) {
+    r.store(p);
+  } else {
+#pragma unroll
+    for (int v = 1; v < V; ++v)
+      if (v >= skip) r.store1(p, v);
+  }
+}
+
+template <int DT, int GT, int V, int T, bool LOGITS, bool COMPLEMENT>
+__global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_fwd_kernel(RecFwd p) {
+  constexpr int ES = RecVec<DT, V>::ES, GS = RecVec<GT, V>::ES;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const RecWhere at = rec_where(p.t, p.sequences);
+  const RecCols<V> k(at.block, lane, p.d);
+  const int64_t s0 = ((int64_t)at.tile * waves + wave) * T;
+  const int n = (int)min((int64_t)T, p.L - s0);  // this wave's steps (none: 0 or less)
+  const bool first = s0 == 0;
+  float s[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) s[v] = first && p.h0 ? p.h0[(int64_t)at.b * p.d + k.c + v] : 0.f;
+  const char* x = p.x + at.b * p.L * p.x_ld + (int64_t)k.c * ES;
+  const char* g = p.g + at.b * p.L * p.g_ld + (int64_t)k.c * GS;
+  RecVec<DT, V> rx[T];
+  RecVec<GT, V> rg[T];
+  float a[T][V], b[T][V], P[V], E[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    P[v] = first ? 0.f : 1.f;
+    E[v] = s[v];
+  }
+  if (n > 0) {
+    RecWalk w(s0, p.L, p.H, p.W, p.dir);
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      rx[t].load(x + w.row * p.x_ld);
+      rg[t].load(g + w.row * p.g_ld);
+      if (t + 1 < n) w.next();  // (steps past the end read the last row again)
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float keep = 0.f, slope;
+        rec_gate<LOGITS, COMPLEMENT, false>(rg[t].get(v), p.inv_tau, a[t][v], keep, slope);
+        b[t][v] = COMPLEMENT ? keep * rx[t].get(v) : rx[t].get(v);
+        if (T > 1 && t >= n) {
+          a[t][v] = 1.f;
+          b[t][v] = 0.f;
+        }
+        E[v] = fmaf(a[t][v], E[v], b[t][v]);
+        P[v] *= a[t][v];
+      }
+  }
+  if constexpr (T > 1) rec_carry<V>(p.t, at, wave, lane, P, E, s);
+  if (n <= 0) return;
+  char* h = p.h + (at.b * p.L * p.d + k.c) * ES;
+  RecWalk w(s0, p.L, p.H, p.W, p.dir);
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    RecVec<DT, V> r;
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[v] = fmaf(a[t][v], s[v], b[t][v]);
+    r.set(s);
+    if (t < n) rec_store(r, h + w.row * p.d * ES, k.skip);
+    w.next();
+  }
+  if (p.h_final && s0 + n == p.L) {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (v >= k.skip) p.h_final[(int64_t)at.b * p.d + k.c + v] = s[v];
+  }
+}
+
+struct RecBwd {
+  RecTiles t;
+  const char *dh, *g, *h, *x;
+  const float *h0, *dh_final;
+  char *dx, *dg;
+  float* dh0;
+  int64_t x_ld, g_ld, dx_ld, dg_ld;
+  int64_t L;
+  int H, W, d, dir;  // dir: the reversed order
+  unsigned sequences;
+  float inv_tau;
+};
+
+// As the forward pass, in the reversed order: the state is Y, a step's map Y -> a (dh + Y).
+template <int DT, int GT, int V, int T, bool LOGITS, bool COMPLEMENT>
+__global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_bwd_kernel(RecBwd p) {
+  constexpr int ES = RecVec<DT, V>::ES, GS = RecVec<GT, V>::ES;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const RecWhere at = rec_where(p.t, p.sequences);
+  const RecCols<V> k(at.block, lane, p.d);
+  const int64_t s0 = ((int64_t)at.tile * waves + wave) * T, state = (int64_t)at.b * p.d + k.c;
+  const int n = (int)min((int64_t)T, p.L - s0);
+  const bool first = s0 == 0;
+  float y[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) y[v] = first && p.dh_final ? p.dh_final[state + v] : 0.f;
+  const char* dh = p.dh + (at.b * p.L * p.d + k.c) * ES;
+  const char* h = p.h + (at.b * p.L * p.d + k.c) * ES;
+  const char* g = p.g + at.b * p.L * p.g_ld + (int64_t)k.c * GS;
+  const char* x = COMPLEMENT ? p.x + at.b * p.L * p.x_ld + (int64_t)k.c * ES : nullptr;
+  RecVec<DT, V> rd[T], rh[T], rx[T];
+  RecVec<GT, V> rg[T];
+  float a[T][V], keep[T][V], slope[T][V], P[V], E[V], h0[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    P[v] = first ? 0.f : 1.f;
+    E[v] = y[v];
+    h0[v] = 0.f;
+  }
+  if (n > 0) {
+    const bool to_start = s0 + n == p.L;  // this wave has the scan's first token, before which the state is h0
+    RecWalk w(s0, p.L, p.H, p.W, p.dir);
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      rd[t].load(dh + w.row * p.d * ES);
+      rg[t].load(g + w.row * p.g_ld);
+      if constexpr (COMPLEMENT) rx[t].load(x + w.row * p.x_ld);
+      if (t + 1 < n || (t + 1 == n && !to_start)) w.next();
+      rh[t].load(h + w.row * p.d * ES);  // (of the scan's first token: not used)
+    }
+    if (to_start && p.h0) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) h0[v] = p.h0[state + v];
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        rec_gate<LOGITS, COMPLEMENT, true>(rg[t].get(v), p.inv_tau, a[t][v], keep[t][v], slope[t][v]);
+        const bool mine = T == 1 || t < n;
+        E[v] = mine ? a[t][v] * (rd[t].get(v) + E[v]) : E[v];
+        P[v] = mine ? a[t][v] * P[v] : P[v];
+      }
+  }
+  if constexpr (T > 1) rec_carry<V>(p.t, at, wave, lane, P, E, y);
+  if (n <= 0) return;
+  char* dx = p.dx ? p.dx + at.b * p.L * p.dx_ld + (int64_t)k.c * ES : nullptr;
+  char* dg = p.dg ? p.dg + at.b * p.L * p.dg_ld + (int64_t)k.c * GS : nullptr;
+  const bool to_start = s0 + n == p.L;
+  RecWalk w(s0, p.L, p.H, p.W, p.dir);
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    if (T > 1 && t >= n) break;
+    RecVec<DT, V> rdx;
+    RecVec<GT, V> rdg;
+    float ox[V], og[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float D = rd[t].get(v) + y[v];
+      y[v] = a[t][v] * D;
+      ox[v] = COMPLEMENT ? keep[t][v] * D : D;
+      float before = to_start && t == n - 1 ? h0[v] : rh[t].get(v);
+      if constexpr (COMPLEMENT) before -= rx[t].get(v);
+      og[v] = y[v] * before;
+      if constexpr (LOGITS) og[v] *= slope[t][v];
+    }
+    rdx.set(ox);
+    rdg.set(og);
+    if (dx) rec_store(rdx, dx + w.row * p.dx_ld, k.skip);
+    if (dg) rec_store(rdg, dg + w.row * p.dg_ld, k.skip);
+    w.next();
+  }
+  if (p.dh0 && to_start) {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (v >= k.skip) p.dh0[state + v] = y[v];
+  }
+}
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+__global__ void __launch_bounds__(256) rec_clear_kernel(u32x4* p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = u32x4{0, 0, 0, 0};
+}
+
+}  // namespace gtr
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+namespace gtr {
+
+constexpr int kRecFwdSteps = 16, kRecBwdSteps = 8;  // per wave
+constexpr unsigned kRecSpin = 1u << 22;             // polls of a wait, of a microsecond or less each
+
+struct RecPlan {
+  int V, T, waves;
+  RecTiles t;
+  int64_t sequences, grid;
+  size_t need, clear;  // bytes of workspace, of which those that are cleared
+};
+
+static gtr_status rec_plan(int32_t B, int32_t H, int32_t W, int32_t d, int steps, RecPlan* r) {
+  if (B <= 0 || H <= 0 || W <= 0 || d <= 0) return GTR_ERR_SHAPE;
+  const int64_t L = (int64_t)H * W;
+  if (L >= (int64_t)1 << 31) return GTR_ERR_SHAPE;
+  r->V = d == 1 ? 1 : 2;
+  r->T = L == 1 ? 1 : steps;
+  const int64_t waves = (L + r->T - 1) / r->T;
+  r->waves = (int)(waves < kRecWaves ? waves : kRecWaves);
+  const int64_t tiles = (waves + r->waves - 1) / r->waves;
+  r->t = RecTiles{};
+  r->t.tiles = (int)tiles;
+  r->t.blocks = (d + 64 * r->V - 1) / (64 * r->V);
+  r->t.group = 4;
+  while ((int64_t)r->t.group * r->t.group < tiles && r->t.group < 64) r->t.group *= 2;
+  r->t.groups = (int)((tiles + r->t.group - 1) / r->t.group);
+  r->t.spin = kRecSpin;
+  r->sequences = (int64_t)B * r->t.blocks;
+  r->grid = r->sequences * tiles;  // (below 2^62)
+  // a launch's threads stay below 2^32
+  if (r->grid > (((int64_t)1 << 32) - 1) / (64 * r->waves)) return GTR_ERR_SHAPE;
+  r->need = r->clear = 0;
+  if (tiles > 1) {
+    const size_t words = (size_t)r->sequences * (size_t)(tiles + r->t.groups) * 64 * r->V;
+    r->clear = r->need = 256 + words * 8;
+  }
+  return GTR_OK;
+}
+
+static gtr_status rec_types(int dtype, int g_dtype, int g_kind, float tau, int scan) {
+  if (dtype != GTR_F32 && dtype != GTR_F16 && dtype != GTR_BF16) return GTR_ERR_UNSUPPORTED;
+  if (g_dtype != dtype && g_dtype != GTR_F32) return GTR_ERR_UNSUPPORTED;
+  if (scan < GTR_SCAN_ROW || scan > GTR_SCAN_COL_REV) return GTR_ERR_UNSUPPORTED;
+  if (g_kind != GTR_GATE_LOG_DECAY && g_kind != GTR_GATE_LOGITS) return GTR_ERR_UNSUPPORTED;
+  if (g_kind == GTR_GATE_LOGITS && !(tau > 0.f && 1.f / tau <= 3.0e38f && tau <= 3.0e38f)) return GTR_ERR_UNSUPPORTED;
+  return GTR_OK;
+}
+
+// The rows of an operand: n rows of `width` bytes, `ld` bytes apart.
+struct RecRows {
+  const void* p;
+  int64_t n, ld, width;
+};
+static bool rec_rows(const void* p, int64_t n, int64_t ld, int32_t d, int es, RecRows* r) {
+  if (ld == 0) ld = d;
+  int64_t bytes;
+  if (ld < d || __builtin_mul_overflow(ld, (int64_t)es, &bytes) || __builtin_mul_overflow(bytes, n, &bytes) ||
+      bytes > (int64_t)1 << 62)
+    return false;
+  *r = RecRows{p, n, ld * es, (int64_t)d * es};
+  return true;
+}
+static Bytes rec_bytes(const RecRows& r) { return {r.p, (size_t)((r.n - 1) * r.ld + r.width)}; }
+// Rows that lie between each other's (two halves of one matrix) do not meet.
+static bool rows_meet(const RecRows& a, const RecRows& b) {
+  if (!bytes_meet(rec_bytes(a), rec_bytes(b))) return false;
+  if (a.ld != b.ld) return true;
+  const RecRows &lo = a.p <= b.p ? a : b, &hi = a.p <= b.p ? b : a;
+  const int64_t off = (int64_t)((reinterpret_cast<uintptr_t>(hi.p) - reinterpret_cast<uintptr_t>(lo.p)) % (uint64_t)a.ld);
+  return off < lo.width || off + hi.width > a.ld;
+}
+static bool same_rows(const RecRows& a, const RecRows& b) { return a.p == b.p && a.ld == b.ld && a.width == b.width; }
+static RecRows flat_rows(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
+static bool rec_misaligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
+
+static gtr_status rec_workspace(const RecPlan& r, const void* ws, size_t bytes) {
+  if (r.need && (!ws || rec_misaligned(ws, 256) || bytes < r.need)) return GTR_ERR_WORKSPACE;
+  return GTR_OK;
+}
+
+// Lays the tiles' words out and clears them (with a kernel: the call may be captured).
+static void rec_words(RecPlan* r, void* ws, uint32_t spin, hipStream_t stream) {
+  if (spin) r->t.spin = spin;
+  if (!r->need) return;
+  r->t.counter = static_cast<unsigned*>(ws);
+  r->t.maps = reinterpret_cast<unsigned long long*>(static_cast<char*>(ws) + 256);
+  r->t.states = r->t.maps + r->sequences * r->t.tiles * 64 * r->V;
+  const int64_t n = (int64_t)(r->clear / 16), blocks = (n + 255) / 256;
+  hipLaunchKernelGGL(rec_clear_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, stream,
+                     static_cast<u32x4*>(ws), n);
+}
+
+template <class P>
+struct RecLaunch {
+  P p;
+  const RecPlan& r;
+  hipStream_t stream;
+};
+template <int DT, int GT, int V, int T, bool LOGITS, bool COMPLEMENT>
+static void rec_go(const RecLaunch<RecFwd>& a) {
+  hipLaunchKernelGGL((rec_fwd_kernel<DT, GT, V, T, LOGITS, COMPLEMENT>), dim3((unsigned)a.r.grid), dim3(64 * a.r.waves), 0,
+                     a.stream, a.p);
+}
+template <int DT, int GT, int V, int T, bool LOGITS, bool COMPLEMENT>
+static void rec_go(const RecLaunch<RecBwd>& a) {
+  hipLaunchKernelGGL((rec_bwd_kernel<DT, GT, V, T, LOGITS, COMPLEMENT>), dim3((unsigned)a.r.grid), dim3(64 * a.r.waves), 0,
+                     a.stream, a.p);
+}
+template <int STEPS, int DT, int GT, bool LOGITS, bool COMPLEMENT, class P>
+static void rec_sized(const RecLaunch<P>& a) {
+  if (a.r.V == 1) return a.r.T == 1 ? rec_go<DT, GT, 1, 1, LOGITS, COMPLEMENT>(a) : rec_go<DT, GT, 1, STEPS, LOGITS, COMPLEMENT>(a);
+  a.r.T == 1 ? rec_go<DT, GT, 2, 1, LOGITS, COMPLEMENT>(a) : rec_go<DT, GT, 2, STEPS, LOGITS, COMPLEMENT>(a);
+}
+template <int STEPS, int DT, int GT, class P>
+static void rec_kind(const RecLaunch<P>& a, bool logits, bool complement) {
+  if (logits)
+    complement ? rec_sized<STEPS, DT, GT, true, true>(a) : rec_sized<STEPS, DT, GT, true, false>(a);
+  else
+    complement ? rec_sized<STEPS, DT, GT, false, true>(a) : rec_sized<STEPS, DT, GT, false, false>(a);
+}
+template <int STEPS, class P>
+static gtr_status rec_launch(const RecLaunch<P>& a, int dt, int gt, bool logits, bool complement) {
+  if (dt == GTR_F32)
+    rec_kind<STEPS, GTR_F32, GTR_F32>(a, logits, complement);
+  else if (dt == GTR_F16)
+    gt == dt ? rec_kind<STEPS, GTR_F16, GTR_F16>(a, logits, complement) : rec_kind<STEPS, GTR_F16, GTR_F32>(a, logits, complement);
+  else
+    gt == dt ? rec_kind<STEPS, GTR_BF16, GTR_BF16>(a, logits, complement) : rec_kind<STEPS, GTR_BF16, GTR_F32>(a, logits, complement);
+  return hipGetLastError() == hipSuccess ? GTR_OK : GTR_ERR_HIP;
+}
+
+static gtr_status rec_fwd_plan(const gtr_recurrence_fwd_args* a, RecPlan* r) {
+  if (!a) return GTR_ERR_NULL;
+  const gtr_status st = rec_plan(a->B, a->H, a->W, a->d, kRecFwdSteps, r);
+  return st != GTR_OK ? st : rec_types(a->dtype, a->g_dtype, a->g_kind, a->gate_tau, a->scan);
+}
+static gtr_status rec_bwd_plan(const gtr_recurrence_bwd_args* a, RecPlan* r) {
+  if (!a) return GTR_ERR_NULL;
+  const gtr_status st = rec_plan(a->B, a->H, a->W, a->d, kRecBwdSteps, r);
+  return st != GTR_OK ? st : rec_types(a->dtype, a->g_dtype, a->g_kind, a->gate_tau, a->scan);
+}
+
+}  // namespace gtr
+
+using namespace gtr;
+
+extern "C" size_t gtr_recurrence_fwd_workspace_size(const gtr_recurrence_fwd_args* a) {
+  RecPlan r;
+  return rec_fwd_plan(a, &r) == GTR_OK ? r.need : 0;
+}
+
+extern "C" gtr_status gtr_recurrence_fwd(const gtr_recurrence_fwd_args* a, hipStream_t stream) {
+  RecPlan r;
+  gtr_status st = rec_fwd_plan(a, &r);
+  if (st != GTR_OK) return st;
+  if (!a->x || !a->g || !a->h) return GTR_ERR_NULL;
+  const int es = (int)dtype_size(a->dtype), gs = (int)dtype_size(a->g_dtype);
+  const int64_t L = (int64_t)a->H * a->W, n = a->B * L, state = (int64_t)a->B * a->d * 4;
+  RecRows x, g, h;
+  if (!rec_rows(a->x, n, a->x_ld, a->d, es, &x) || !rec_rows(a->g, n, a->g_ld, a->d, gs, &g) ||
+      !rec_rows(a->h, n, 0, a->d, es, &h))
+    return GTR_ERR_SHAPE;
+  if (rec_misaligned(a->x, es) || rec_misaligned(a->g, gs) || rec_misaligned(a->h, es) || rec_misaligned(a->h0, 4) ||
+      rec_misaligned(a->h_final, 4))
+    return GTR_ERR_UNSUPPORTED;
+  st = rec_workspace(r, a->workspace, a->workspace_bytes);
+  if (st != GTR_OK) return st;
+  const RecRows h0 = flat_rows(a->h0, state), last = flat_rows(a->h_final, state),
+                ws = flat_rows(r.need ? a->workspace : nullptr, (int64_t)r.need);
+  if ((rows_meet(h, x) && !same_rows(h, x)) || rows_meet(h, g) || rows_meet(h, h0) || rows_meet(h, last) || rows_meet(h, ws) ||
+      rows_meet(last, x) || rows_meet(last, g) || (rows_meet(last, h0) && last.p != h0.p) || rows_meet(last, ws) ||
+      rows_meet(ws, x) || rows_meet(ws, g) || rows_meet(ws, h0))
+    return GTR_ERR_ALIAS;
+  rec_words(&r, a->workspace, a->spin_limit, stream);
+  RecFwd p = {};
+  p.t = r.t;
+  p.x = static_cast<const char*>(a->x);
+  p.g = static_cast<const char*>(a->g);
+  p.h = static_cast<char*>(a->h);
+  p.h0 = a->h0;
+  p.h_final = a->h_final;
+  p.x_ld = x.ld;
+  p.g_ld = g.ld;
+  p.L = L;
+  p.H = a->H;
+  p.W = a->W;
+  p.d = a->d;
+  p.dir = a->scan;
+  p.sequences = (unsigned)r.sequences;
+  p.inv_tau = a->g_kind == GTR_GATE_LOGITS ? 1.f / a->gate_tau : 1.f;
+  return rec_launch<kRecFwdSteps>(RecLaunch<RecFwd>{p, r, stream}, a->dtype, a->g_dtype, a->g_kind == GTR_GATE_LOGITS,
+                                  a->complement != 0);
+}
+
+extern "C" size_t gtr_recurrence_bwd_workspace_size(const gtr_recurrence_bwd_args* a) {
+  RecPlan r;
+  return rec_bwd_plan(a, &r) == GTR_OK ? r.need : 0;
+}
+
+extern "C" gtr_status gtr_recurrence_bwd(const gtr_recurrence_bwd_args* a, hipStream_t stream) {
+  RecPlan r;
+  gtr_status st = rec_bwd_plan(a, &r);
+  if (st != GTR_OK) return st;
+  if (!a->dh || !a->g || !a->h || (a->complement && !a->x) || (!a->dx && !a->dg && !a->dh0)) return GTR_ERR_NULL;
+  const int es = (int)dtype_size(a->dtype), gs = (int)dtype_size(a->g_dtype);
+  const int64_t L = (int64_t)a->H * a->W, n = a->B * L, state = (int64_t)a->B * a->d * 4;
+  RecRows dh, g, h, x, dx, dg;
+  if (!rec_rows(a->dh, n, 0, a->d, es, &dh) || !rec_rows(a->g, n, a->g_ld, a->d, gs, &g) ||
+      !rec_rows(a->h, n, 0, a->d, es, &h) || !rec_rows(a->complement ? a->x : nullptr, n, a->x_ld, a->d, es, &x) ||
+      !rec_rows(a->dx, n, a->dx_ld, a->d, es, &dx) || !rec_rows(a->dg, n, a->dg_ld, a->d, gs, &dg))
+    return GTR_ERR_SHAPE;
+  if (rec_misaligned(a->dh, es) || rec_misaligned(a->g, gs) || rec_misaligned(a->h, es) || rec_misaligned(x.p, es) ||
+      rec_misaligned(a->dx, es) || rec_misaligned(a->dg, gs) || rec_misaligned(a->h0, 4) ||
+      rec_misaligned(a->dh_final, 4) || rec_misaligned(a->dh0, 4))
+    return GTR_ERR_UNSUPPORTED;
+  st = rec_workspace(r, a->workspace, a->workspace_bytes);
+  if (st != GTR_OK) return st;
+  const RecRows ins[] = {dh, g, x, h, flat_rows(a->h0, state), flat_rows(a->dh_final, state)};
+  const RecRows outs[] = {dx, dg, flat_rows(a->dh0, state), flat_rows(r.need ? a->workspace : nullptr, (int64_t)r.need)};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < 6; ++j) {
+      // a row's gradients may lie where that row of dh, g or x was, and the first state's where the last one's was
+      const bool over = (i < 2 && j < 3 && same_rows(outs[i], ins[j])) || (i == 2 && j == 5 && outs[i].p == ins[j].p);
+      if (rows_meet(outs[i], ins[j]) && !over) return GTR_ERR_ALIAS;
+    }
+    for (int j = 0; j < i; ++j)
+      if (rows_meet(outs[i], outs[j])) return GTR_ERR_ALIAS;
+  }
+  rec_words(&r, a->workspace, a->spin_limit, stream);
+  RecBwd p = {};
+  p.t = r.t;
+  p.dh = static_cast<const char*>(a->dh);
+  p.g = static_cast<const char*>(a->g);
+  p.h = static_cast<const char*>(a->h);
+  p.x = static_cast<const char*>(a->x);
+  p.h0 = a->h0;
+  p.dh_final = a->dh_final;
+  p.dx = static_cast<char*>(a->dx);
+  p.dg = static_cast<char*>(a->dg);
+  p.dh0 = a->dh0;
+  p.x_ld = x.ld;
+  p.g_ld = g.ld;
+  p.dx_ld = dx.ld;
+  p.dg_ld = dg.ld;
+  p.L = L;
+  p.H = a->H;
+  p.W = a->W;
+  p.d = a->d;
+  p.dir = a->scan ^ 2;  // ROW <-> ROW_REV, COL <-> COL_REV
+  p.sequences = (unsigned)r.sequences;
+  p.inv_tau = a->g_kind == GTR_GATE_LOGITS ? 1.f / a->gate_tau : 1.f;
+  return rec_launch<kRecBwdSteps>(RecLaunch<RecBwd>{p, r, stream}, a->dtype, a->g_dtype, a->g_kind == GTR_GATE_LOGITS,
+                                  a->complement != 0);
+}
