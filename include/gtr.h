@@ -654,6 +654,81 @@ typedef struct {
 size_t gtr_recurrence_bwd_workspace_size(const gtr_recurrence_bwd_args* args);
 gtr_status gtr_recurrence_bwd(const gtr_recurrence_bwd_args* args, hipStream_t stream);
 
+/* No activation, for gtr_groupnorm_fwd / _bwd (the feed-forward has always one). */
+enum { GTR_ACT_NONE = 2 };
+
+/*
+ * gtr_groupnorm_fwd: group normalisation with an activation over token grids, channels
+ * last (gtr_layernorm_fwd's manner; its rows are tokens, here the statistics are an
+ * image's). For image b and group j of C / groups consecutive channels, over all L
+ * tokens and the group's channels, in float32,
+ *   mean, var (biased), rstd = (var + eps)^(-1/2),
+ *   y = act((x - mean) rstd w + b)
+ * x, y : [B, L, C] dtype (GTR_F32, GTR_F16 or GTR_BF16); y may be x (in place)
+ * w, b : [C] float32; NULL stands for ones / zeros
+ * mean, rstd : [B, groups] float32, for gtr_groupnorm_bwd, or NULL
+ * act  : GTR_ACT_NONE, GTR_ACT_SILU or GTR_ACT_GELU
+ * C a multiple of groups and at most 16384, 1 <= L < 2^31, B L < 2^40; no alignment
+ * beyond an element's. 0 <= eps < 1e30 (a group of equal values with eps 0 gives NaN).
+ * workspace : where gtr_groupnorm_fwd_workspace_size(args) is not 0, 256-byte
+ *        aligned, at least that many bytes, no initialisation needed; calls that
+ *        overlap in time must not share one. It is left with any contents: never a
+ *        gtr_gla_fwd workspace.
+ */
+typedef struct {
+  const void* x;
+  const float* w;
+  const float* b;
+  void* y;
+  float* mean;
+  float* rstd;
+  gtr_dtype dtype;
+  int32_t act;
+  int64_t L;
+  int32_t B, C, groups;
+  float eps;
+  void* workspace;
+  size_t workspace_bytes;
+} gtr_groupnorm_fwd_args;
+
+size_t gtr_groupnorm_fwd_workspace_size(const gtr_groupnorm_fwd_args* args);
+gtr_status gtr_groupnorm_fwd(const gtr_groupnorm_fwd_args* args, hipStream_t stream);
+
+/*
+ * gtr_groupnorm_bwd: the gradients of gtr_groupnorm_fwd. With h = (x - mean) rstd,
+ * du = dy act'(h w + b), t = du w and the means over a group's tokens and channels:
+ *   dx = rstd (t - mean(t) - h mean(t h)) (+ dres)
+ *   dw = sum over images and tokens of du h,  db = that of du
+ * dy, x, dres, dx : [B, L, C] dtype. dres (a gradient that reaches x another way) may
+ *          be NULL. dx may be NULL (not wanted) or be dy, x or dres itself.
+ * mean, rstd : as gtr_groupnorm_fwd left them; w, b, act as there
+ * dw, db : [C] float32, or NULL where not wanted; accumulate 1: added to what they hold
+ * Sizes, types and the workspace as for gtr_groupnorm_fwd; which outputs are wanted
+ * changes its size.
+ */
+typedef struct {
+  const void* dy;
+  const void* x;
+  const float* mean;
+  const float* rstd;
+  const float* w;
+  const float* b;
+  const void* dres;
+  void* dx;
+  float* dw;
+  float* db;
+  gtr_dtype dtype;
+  int32_t act;
+  int64_t L;
+  int32_t B, C, groups;
+  int32_t accumulate;
+  void* workspace;
+  size_t workspace_bytes;
+} gtr_groupnorm_bwd_args;
+
+size_t gtr_groupnorm_bwd_workspace_size(const gtr_groupnorm_bwd_args* args);
+gtr_status gtr_groupnorm_bwd(const gtr_groupnorm_bwd_args* args, hipStream_t stream);
+
 /*
  * gtr_gla_fwd_noalloc - gtr_gla_fwd for callers that cannot allocate device
  * memory (code under HIP graph capture, serving loops, harnesses that forbid

@@ -19,6 +19,8 @@ Entry points (same names as the C ABI in ``include/gtr.h``):
   for training, with the gradients of input, weight and bias.
 * :func:`gtr_ffn_fwd`, :func:`gtr_ffn_bwd` - the gated feed-forward
   ``[act(x W_gate^T) * (x W_value^T)] W_out^T`` and its gradients.
+* :func:`gtr_groupnorm_fwd`, :func:`gtr_groupnorm_bwd` - group normalisation with
+  an activation over token grids, channels last, and its gradients.
 * :func:`gtr_recurrence_fwd`, :func:`gtr_recurrence_bwd` - the gated linear
   recurrence with a diagonal state, ``h_t = a_t h_{t-1} + b_t`` along the four
   scan orders, from single tokens to long sequences, and its gradients.
@@ -44,6 +46,7 @@ F32, F16, BF16 = 0, 1, 2
 SCANS = {"row": 0, "col": 1, "row_rev": 2, "col_rev": 3}
 PATHS = {"auto": 0, "fused": 1, "staged": 2, "inline": 3}
 ACTS = {"silu": 0, "gelu": 1}
+ACT_NONE = 2  # (group norm only)
 STATUS = {0: "GTR_OK", 1: "GTR_ERR_NULL", 2: "GTR_ERR_SHAPE", 3: "GTR_ERR_UNSUPPORTED",
           4: "GTR_ERR_ALIAS", 5: "GTR_ERR_WORKSPACE", 6: "GTR_ERR_HIP", 7: "GTR_ERR_SCRATCH"}
 
@@ -55,7 +58,9 @@ EXPORTS = ("gtr_scan_permute", "gtr_gla_workspace_size", "gtr_gla_workspace_init
            "gtr_spatial_swiglu", "gtr_gemm", "gtr_layernorm", "gtr_heads_split", "gtr_heads_merge", "gtr_add",
            "gtr_layernorm_fwd", "gtr_layernorm_bwd_workspace_size", "gtr_layernorm_bwd", "gtr_ffn_fwd_workspace_size",
            "gtr_ffn_fwd", "gtr_ffn_bwd_workspace_size", "gtr_ffn_bwd", "gtr_recurrence_fwd_workspace_size",
-           "gtr_recurrence_fwd", "gtr_recurrence_bwd_workspace_size", "gtr_recurrence_bwd")
+           "gtr_recurrence_fwd", "gtr_recurrence_bwd_workspace_size", "gtr_recurrence_bwd",
+           "gtr_groupnorm_fwd_workspace_size", "gtr_groupnorm_fwd", "gtr_groupnorm_bwd_workspace_size",
+           "gtr_groupnorm_bwd")
 
 
 class GtrError(RuntimeError):
@@ -171,6 +176,27 @@ class RecurrenceBwdArgs(ctypes.Structure):
     ]
 
 
+class GroupnormFwdArgs(ctypes.Structure):
+    """Mirror of ``gtr_groupnorm_fwd_args`` (include/gtr.h)."""
+    _fields_ = [
+        ("x", ctypes.c_void_p), ("w", ctypes.c_void_p), ("b", ctypes.c_void_p), ("y", ctypes.c_void_p),
+        ("mean", ctypes.c_void_p), ("rstd", ctypes.c_void_p), ("dtype", ctypes.c_int), ("act", ctypes.c_int32),
+        ("L", ctypes.c_int64), ("B", ctypes.c_int32), ("C", ctypes.c_int32), ("groups", ctypes.c_int32),
+        ("eps", ctypes.c_float), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class GroupnormBwdArgs(ctypes.Structure):
+    """Mirror of ``gtr_groupnorm_bwd_args`` (include/gtr.h)."""
+    _fields_ = [
+        ("dy", ctypes.c_void_p), ("x", ctypes.c_void_p), ("mean", ctypes.c_void_p), ("rstd", ctypes.c_void_p),
+        ("w", ctypes.c_void_p), ("b", ctypes.c_void_p), ("dres", ctypes.c_void_p), ("dx", ctypes.c_void_p),
+        ("dw", ctypes.c_void_p), ("db", ctypes.c_void_p), ("dtype", ctypes.c_int), ("act", ctypes.c_int32),
+        ("L", ctypes.c_int64), ("B", ctypes.c_int32), ("C", ctypes.c_int32), ("groups", ctypes.c_int32),
+        ("accumulate", ctypes.c_int32), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 _lib = None
 
 
@@ -221,7 +247,8 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.gtr_add.restype = ctypes.c_int
     for name, args in (("gtr_layernorm_fwd", LayernormFwdArgs), ("gtr_layernorm_bwd", LayernormBwdArgs),
                        ("gtr_ffn_fwd", FfnFwdArgs), ("gtr_ffn_bwd", FfnBwdArgs),
-                       ("gtr_recurrence_fwd", RecurrenceFwdArgs), ("gtr_recurrence_bwd", RecurrenceBwdArgs)):
+                       ("gtr_recurrence_fwd", RecurrenceFwdArgs), ("gtr_recurrence_bwd", RecurrenceBwdArgs),
+                       ("gtr_groupnorm_fwd", GroupnormFwdArgs), ("gtr_groupnorm_bwd", GroupnormBwdArgs)):
         getattr(lib, name).argtypes = [ctypes.POINTER(args), P]
         getattr(lib, name).restype = ctypes.c_int
         if args is not LayernormFwdArgs:
@@ -927,6 +954,134 @@ def _ffn_bwd(dy, x, w_gate, w_value, w_out, gate, value, act, want_dx, want_dw, 
     if st:
         raise GtrError("gtr_ffn_bwd", st)
     return dx, dwg, dwv, dwo
+
+
+# ---------------------------------------------------------------------------
+# normalisation over a token grid: gtr_groupnorm_fwd / gtr_groupnorm_bwd
+# ---------------------------------------------------------------------------
+def _groups_act(act: Optional[str]) -> int:
+    if act is None:
+        return ACT_NONE
+    if act not in ACTS:
+        raise ValueError(f"act must be None or one of {sorted(ACTS)}")
+    return ACTS[act]
+
+
+def _grid_rows(name: str, t: torch.Tensor) -> None:
+    _rows(name, t)
+    if t.dim() < 2:
+        raise ValueError(f"{name} must be [B, ..., C]")
+
+
+def gtr_groupnorm_fwd(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = None,
+                      bias: Optional[torch.Tensor] = None, *, act: Optional[str] = None, eps: float = 1e-5,
+                      out: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
+                      rstd: Optional[torch.Tensor] = None, workspace: Optional["Workspace"] = None, stream=None):
+    """Group normalisation with an activation: y = act((x - mean) rstd weight + bias).
+
+    x [B, ..., C] (float32, fp16 or bf16; the dimensions between are the tokens, channels last), the statistics over the
+    tokens and the C / groups consecutive channels of each group of each of the B images. weight, bias [C] float32.
+    ``act``: None, "silu" or "gelu". ``out`` may be x. Returns ``(y, mean, rstd)``, the statistics float32 [B, groups]."""
+    code = _groups_act(act)
+    if stream is None and x.is_cuda and x.get_device() == torch._C._cuda_getDevice():
+        return _groupnorm_fwd(x, groups, weight, bias, code, eps, out, mean, rstd, workspace)
+    _grid_rows("x", x)
+    return _on_stream(_groupnorm_fwd, stream, (x, weight, bias, out, mean, rstd),
+                      (x, groups, weight, bias, code, eps, out, mean, rstd, workspace))
+
+
+def _groupnorm_fwd(x, groups, weight, bias, act, eps, y, mu, rs, workspace):
+    shape, dev, dt, f32 = x.shape, x.device, x.dtype, torch.float32
+    code = _DT.get(dt)
+    if code is None or len(shape) < 2 or not x.is_contiguous():
+        _grid_rows("x", x)
+    B, C, index = shape[0], shape[-1], dev.index
+    if not 0 < groups <= C or C % groups:
+        raise ValueError(f"groups must divide the {C} channels")
+    stats = (B, groups)
+    if y is None:
+        y = torch.empty_like(x)
+    if mu is None:
+        mu = torch.empty(stats, dtype=f32, device=dev)
+    if rs is None:
+        rs = torch.empty(stats, dtype=f32, device=dev)
+    if not (_is(y, shape, dt, index) and _is(mu, stats, f32, index) and _is(rs, stats, f32, index) and
+            _vector(weight, C, index) and _vector(bias, C, index)):
+        _check("out", y, shape, (dt,), dev)
+        for name, t, want in (("weight", weight, (C,)), ("bias", bias, (C,)), ("mean", mu, stats), ("rstd", rs, stats)):
+            _check(name, t, want, (f32,), dev)
+    a = GroupnormFwdArgs(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), mu.data_ptr(), rs.data_ptr(), code, act,
+                         x.numel() // (B * C) if B else 0, _i32(B), _i32(C), groups, eps)
+    lib, ref = load(), ctypes.byref(a)
+    need = lib.gtr_groupnorm_fwd_workspace_size(ref)
+    if need:
+        buf = _scratch(need, dev, workspace)
+        a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel()
+    st = lib.gtr_groupnorm_fwd(ref, torch._C._cuda_getCurrentRawStream(index))
+    if st:
+        raise GtrError("gtr_groupnorm_fwd", st)
+    return y, mu, rs
+
+
+def gtr_groupnorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                      weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+                      act: Optional[str] = None, dres: Optional[torch.Tensor] = None, want_dx: bool = True,
+                      want_dw: bool = True, out: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
+                      db: Optional[torch.Tensor] = None, accumulate: bool = False,
+                      workspace: Optional["Workspace"] = None, stream=None):
+    """Gradients of :func:`gtr_groupnorm_fwd`: ``(dx, dw, db)``, from the statistics [B, groups] that it returned. dx is in
+    x's type, dw and db [C] float32, summed over all tokens. ``dres`` (x's shape and type, a residual path's gradient) is
+    added to dx. ``out`` (for dx) may be dy, x or dres. ``accumulate``: dw and db are added to what the given ``dw`` and
+    ``db`` hold. What is not wanted is None."""
+    code = _groups_act(act)
+    if accumulate and want_dw and (dw is None or db is None):
+        raise ValueError("accumulate needs dw and db")
+    args = (dy, x, mean, rstd, weight, bias, code, dres, want_dx, want_dw, out, dw, db, accumulate, workspace)
+    if stream is None and x.is_cuda and x.get_device() == torch._C._cuda_getDevice():
+        return _groupnorm_bwd(*args)
+    _grid_rows("x", x)
+    return _on_stream(_groupnorm_bwd, stream, (x, dy, mean, rstd, weight, bias, dres, out, dw, db), args)
+
+
+def _groupnorm_bwd(dy, x, mean, rstd, weight, bias, act, dres, want_dx, want_dw, dx, dw, db, accumulate, workspace):
+    shape, dev, dt, f32 = x.shape, x.device, x.dtype, torch.float32
+    code = _DT.get(dt)
+    if code is None or len(shape) < 2 or not x.is_contiguous():
+        _grid_rows("x", x)
+    B, C, index = shape[0], shape[-1], dev.index
+    groups = mean.shape[1] if mean.dim() == 2 else 0
+    if not 0 < groups <= C or C % groups:
+        raise ValueError(f"mean must be [B, groups], with groups that divide the {C} channels")
+    stats = (B, groups)
+    if not (_is(dy, shape, dt, index) and _is(dres, shape, dt, index) and _is(dx, shape, dt, index) and
+            _is(mean, stats, f32, index) and _is(rstd, stats, f32, index) and _vector(weight, C, index) and
+            _vector(bias, C, index) and _vector(dw, C, index) and _vector(db, C, index)):
+        for name, t in (("dy", dy), ("dres", dres), ("out", dx)):
+            _check(name, t, shape, (dt,), dev)
+        for name, t, want in (("mean", mean, stats), ("rstd", rstd, stats), ("weight", weight, (C,)), ("bias", bias, (C,)),
+                              ("dw", dw, (C,)), ("db", db, (C,))):
+            _check(name, t, want, (f32,), dev)
+    if not want_dx:
+        dx = None
+    elif dx is None:
+        dx = torch.empty_like(x)
+    if not want_dw:
+        dw = db = None
+    else:
+        dw = torch.empty(C, dtype=f32, device=dev) if dw is None else dw
+        db = torch.empty(C, dtype=f32, device=dev) if db is None else db
+    a = GroupnormBwdArgs(dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(weight), _ptr(bias), _ptr(dres),
+                         _ptr(dx), _ptr(dw), _ptr(db), code, act, x.numel() // (B * C) if B else 0, _i32(B), _i32(C), groups,
+                         bool(accumulate))
+    lib, ref = load(), ctypes.byref(a)
+    need = lib.gtr_groupnorm_bwd_workspace_size(ref)
+    if need:
+        buf = _scratch(need, dev, workspace)
+        a.workspace, a.workspace_bytes = buf.data_ptr(), buf.numel()
+    st = lib.gtr_groupnorm_bwd(ref, torch._C._cuda_getCurrentRawStream(index))
+    if st:
+        raise GtrError("gtr_groupnorm_bwd", st)
+    return dx, dw, db
 
 
 # ---------------------------------------------------------------------------

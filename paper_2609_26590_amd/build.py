@@ -19,7 +19,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgtr.so")
 
 SOURCES = ["gtr_host.cpp", "permute.hip", "gla_fwd.hip", "gla_lean.hip", "swiglu.hip", "block.hip", "norm.hip", "ffn.hip",
-           "recurrence.hip"]
+           "recurrence.hip", "groupnorm.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

@@ -33,6 +33,15 @@ static void ffn_prepare(FfnGemm& g, const FfnPlan& plan, int epi) {
   g.part_slice = off;
 }
 
+__global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g, FfnGemm h) {
+  const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  const int64_t ng = g.ksplit > 1 ? g.part_slice : 0, nh = h.ksplit > 1 ? h.part_slice : 0;
+  if (t < ng)
+    ffn_reduce(g, t);
+  else if (t - ng < nh)
+    ffn_reduce(h, t - ng);
+}
+
 static gtr_status ffn_add_slices(const FfnGemm& g, const FfnGemm& h, hipStream_t stream) {
   const int64_t n = (g.ksplit > 1 ? g.part_slice : 0) + (h.ksplit > 1 ? h.part_slice : 0);
   if (!n) return GTR_OK;

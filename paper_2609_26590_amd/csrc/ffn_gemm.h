@@ -635,14 +635,6 @@ __device__ __forceinline__ void ffn_reduce(const FfnGemm& g, int64_t t) {
   }
   store_n<8>(c, g.cdt, off, x);
 }
-__global__ void __launch_bounds__(256) ffn_reduce_kernel(FfnGemm g, FfnGemm h) {
-  const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-  const int64_t ng = g.ksplit > 1 ? g.part_slice : 0, nh = h.ksplit > 1 ? h.part_slice : 0;
-  if (t < ng)
-    ffn_reduce(g, t);
-  else if (t - ng < nh)
-    ffn_reduce(h, t - ng);
-}
 
 // ---------------------------------------------------------------------------
 // A few tokens (up to kFewTokens): the weights' bytes are the work, each read once,
