@@ -16,6 +16,10 @@
 #include "gtr_device.h"
 #include "gtr_internal.h"
 
+// Products and sums round as they are written: both ways through a wave's steps give the
+// same bits.
+#pragma clang fp contract(off)
+
 namespace gtr {
 
 // ---------------------------------------------------------------------------
@@ -45,21 +49,30 @@ struct RecVec {
       return __builtin_bit_cast(float, r.u[v]);
     else if constexpr (DT == GTR_F16)
       return (float)__builtin_bit_cast(_Float16, half(v));
+    else if constexpr (V == 1)
+      return bf16_bits_to_f32(r.u[0]);
     else
-      return bf16_bits_to_f32(half(v));
+      return __builtin_bit_cast(float, v & 1 ? r.u[v / 2] & 0xffff0000u : r.u[v / 2] << 16);
   }
   __device__ __forceinline__ void set(const float (&x)[V]) {
+    if constexpr (DT == GTR_F32) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if constexpr (DT == GTR_F32) {
-        r.u[v] = __builtin_bit_cast(unsigned, x[v]);
-      } else {
-        unsigned short b;
+      for (int v = 0; v < V; ++v) r.u[v] = __builtin_bit_cast(unsigned, x[v]);
+    } else if constexpr (V == 1) {
+      if constexpr (DT == GTR_F16)
+        r.u[0] = __builtin_bit_cast(unsigned short, (_Float16)x[0]);
+      else
+        r.u[0] = __builtin_bit_cast(unsigned short, (__bf16)x[0]);
+    } else {
+      typedef _Float16 hh __attribute__((ext_vector_type(2)));
+      typedef __bf16 bb __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int v = 0; v < V; v += 2) {  // pairs, which convert in one instruction
+        const f2 p = {x[v], x[v + 1]};
         if constexpr (DT == GTR_F16)
-          b = __builtin_bit_cast(unsigned short, (_Float16)x[v]);
+          r.u[v / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector(p, hh));
         else
-          b = __builtin_bit_cast(unsigned short, (__bf16)x[v]);
-        r.u[v / 2] = v & 1 ? r.u[v / 2] | (unsigned)b << 16 : b;
+          r.u[v / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector(p, bb));
       }
     }
   }
@@ -73,7 +86,7 @@ struct RecVec {
 
 // The rows that a scan visits one after the other, from step s on. Uniform over a wave.
 struct RecWalk {
-  int64_t row;         // spatial index of the present step
+  int64_t row;         // spatial index of the first step
   int64_t step, wrap;  // to the next one, within a grid column and behind its end
   int left, run;       // steps to that end; steps of a whole column less one
   __device__ __forceinline__ RecWalk(int64_t s, int64_t L, int H, int W, int dir) {
@@ -93,47 +106,58 @@ struct RecWalk {
       run = H - 1;
     }
   }
-  __device__ __forceinline__ void next() {
+  // whether the next step is behind a column's end
+  __device__ __forceinline__ bool next() {
     const bool end = left == 0;
-    row += end ? wrap : step;
     left = end ? run : left - 1;
+    return end;
   }
+};
+// One operand's rows along a walk, `ld` bytes apart: a uniform address, to which a lane
+// adds its column (the form of address that needs no vector arithmetic).
+struct RecRow {
+  char* p;
+  int64_t step, wrap;
+  __device__ __forceinline__ RecRow(const void* base, int64_t first, int64_t ld, const RecWalk& w)
+      : p(static_cast<char*>(const_cast<void*>(base)) + (first + w.row) * ld), step(w.step * ld), wrap(w.wrap * ld) {}
+  __device__ __forceinline__ void next(bool end) { p += end ? wrap : step; }
 };
 
 // ---------------------------------------------------------------------------
 // gates
 // ---------------------------------------------------------------------------
-// log(1 + u) for 0 <= u <= 1 as log(w) u / (w - 1), w = 1 + u as rounded: the quotient
-// takes back the rounding of w, so that small u keep their relative accuracy.
-__device__ __forceinline__ float log1p_unit(float u) {
-  const float w = 1.f + u, m = w - 1.f;
-  const float r = __builtin_amdgcn_logf(w) * 0.693147180559945309f * u * __builtin_amdgcn_rcpf(m);
-  return m == 0.f ? u : r;
-}
-// 1 - exp(la), of which a = exp(la): as the exponential's series about 0 up to 1/2
-// (what is left out is under 2^-26 of it), else as it stands.
-__device__ __forceinline__ float one_minus_exp(float la, float a) {
-  float s = 1.f / 40320.f;
-  s = fmaf(s, la, 1.f / 5040.f);
-  s = fmaf(s, la, 1.f / 720.f);
-  s = fmaf(s, la, 1.f / 120.f);
-  s = fmaf(s, la, 1.f / 24.f);
-  s = fmaf(s, la, 1.f / 6.f);
-  s = fmaf(s, la, 0.5f);
-  s = fmaf(s, la, 1.f);
-  return fabsf(la) < 0.5f ? -la * s : 1.f - a;
-}
-// a, 1 - a where KEEP, and d la / d g where SLOPE.
+// In powers of two: a = 2^y with y = g log2(e), or of a logit (min(g, 0) log2(e) - l) / tau
+// with l = log2(1 + u), u = exp(-|g|): the machine's exponential and logarithm as they
+// are, three of them per logit. w = 1 + u loses the low bits of a small u, of which
+// 1 - a would keep the relative error; l takes them back as r / w log2(e), r = u - (w - 1)
+// exactly, where w is so close to 1 that it does not divide (r is 2^-24 at most, and l
+// at least 0.58 where w is 1.5).
+// 1 - 2^y is the exponential's series about 0 up to |y ln 2| = 1/4 (what is left out is
+// under 2^-24 of it), else as it stands: 10 roundings of a at most.
+// a, 1 - a where KEEP, and d log a / d g where SLOPE.
 template <bool LOGITS, bool KEEP, bool SLOPE>
 __device__ __forceinline__ void rec_gate(float g, float inv_tau, float& a, float& keep, float& slope) {
-  float la = g;
+  constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+  float y;
   if constexpr (LOGITS) {
-    const float u = __builtin_amdgcn_exp2f(-fabsf(g) * 1.44269504088896341f);
-    la = (fminf(g, 0.f) - log1p_unit(u)) * inv_tau;
-    if constexpr (SLOPE) slope = (g < 0.f ? 1.f : u) * __builtin_amdgcn_rcpf(1.f + u) * inv_tau;
+    const float u = __builtin_amdgcn_exp2f(-fabsf(g) * kLog2e), w = 1.f + u;
+    const float l = fmaf(u - (w - 1.f), kLog2e, __builtin_amdgcn_logf(w));
+    y = fmaf(fminf(g, 0.f), kLog2e, -l) * inv_tau;
+    if constexpr (SLOPE) slope = (g < 0.f ? 1.f : u) * __builtin_amdgcn_rcpf(w) * inv_tau;
+  } else {
+    y = g * kLog2e;
   }
-  a = __builtin_amdgcn_exp2f(la * 1.44269504088896341f);
-  if constexpr (KEEP) keep = one_minus_exp(la, a);
+  a = __builtin_amdgcn_exp2f(y);
+  if constexpr (KEEP) {
+    constexpr float l2 = kLn2 * kLn2, l3 = l2 * kLn2, l4 = l2 * l2;
+    float s = l4 * l2 / 720.f;
+    s = fmaf(s, y, l4 * kLn2 / 120.f);
+    s = fmaf(s, y, l4 / 24.f);
+    s = fmaf(s, y, l3 / 6.f);
+    s = fmaf(s, y, l2 / 2.f);
+    s = fmaf(s, y, kLn2);
+    keep = fabsf(y) < 0.25f * kLog2e ? -y * s : 1.f - a;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -152,19 +176,27 @@ __device__ __forceinline__ void rec_gate(float g, float inv_tau, float& a, float
 //
 // So a sequence of n tiles has a chain of n / group hand-overs, and the composition is the
 // same whatever the order in which work-groups run: results do not depend on it. Tiles are
-// numbered by a counter as their work-groups start, the first steps of all sequences first:
-// what a tile waits for has started before it, and a map is handed on before anything is
-// waited for, so every wait ends on any number of compute units. (Waits are bounded all the
-// same: one that runs out makes the states NaN from there on.)
+// numbered by a counter as their work-groups start, the first steps of all of its sequences
+// first: what a tile waits for has started before it, and a map is handed on before
+// anything is waited for, so every wait ends, whatever else the device is running. (By
+// work-group index instead, two calls on two streams could fill each other's chiplets with
+// work-groups that wait for ones not started. Waits are bounded all the same: one that
+// runs out makes the states NaN from there on.) A counter hands out 80 numbers per
+// microsecond. Where that counts, in short calls, there are up to 32, each for sequences of
+// its own (8 x 1600 x 384 fp16 18.6 us, with one 20.9); in long ones a single counter keeps
+// blocks of channels that lie next to each other next to each other in time too, which the
+// memory wants (32768 x 4096 bf16 188 us, with 32 counters 232).
 struct RecTiles {
   unsigned long long* maps;    // [sequences][tiles][64 V]
   unsigned long long* states;  // [sequences][groups][64 V]
-  unsigned* counter;           // the next tile; null where a sequence is one tile
+  unsigned* counters;          // the next tile of each `share` sequences; null where a sequence is one tile
   int tiles, group, groups, blocks;
+  unsigned share, lanes;       // sequences per counter, counters
   unsigned spin;
 };
 
 constexpr int kRecWaves = 16;
+constexpr unsigned kRecCounters = 32, kRecCounterStep = 32;  // at most; words from one to the next (128 bytes)
 
 __device__ __forceinline__ unsigned long long rec_word(float P, float E) {
   unsigned lo = ~__builtin_bit_cast(unsigned, P);
@@ -201,21 +233,27 @@ __device__ __forceinline__ void rec_wait(unsigned long long (&w)[N][V], const un
 struct RecWhere {
   int tile, seq, b, block;  // uniform
 };
-// Which tile this work-group takes.
-__device__ __forceinline__ RecWhere rec_where(const RecTiles& t, unsigned sequences) {
-  unsigned id = blockIdx.x;
-  if (t.counter) {
+// Which tile this work-group takes; false if none. Work-groups of index i mod `lanes`
+// share counter i, which numbers the tiles of its own sequences.
+__device__ __forceinline__ bool rec_where(const RecTiles& t, unsigned sequences, RecWhere& w) {
+  unsigned tile, seq;
+  if (t.counters) {
     __shared__ unsigned mine;
-    if (threadIdx.x == 0) mine = atomicAdd(t.counter, 1u);
+    const unsigned lane = blockIdx.x % t.lanes;
+    if (threadIdx.x == 0) mine = atomicAdd(t.counters + kRecCounterStep * lane, 1u);
     __syncthreads();
-    id = (unsigned)__builtin_amdgcn_readfirstlane((int)mine);
+    const unsigned id = (unsigned)__builtin_amdgcn_readfirstlane((int)mine);
+    tile = id / t.share;
+    seq = lane * t.share + (id - tile * t.share);
+  } else {
+    tile = blockIdx.x / sequences;
+    seq = blockIdx.x - tile * sequences;
   }
-  RecWhere w;
-  w.tile = (int)(id / sequences);
-  w.seq = (int)(id % sequences);
+  w.tile = (int)tile;
+  w.seq = (int)seq;
   w.b = w.seq / t.blocks;
-  w.block = w.seq % t.blocks;
-  return w;
+  w.block = w.seq - w.b * t.blocks;
+  return seq < sequences;
 }
 
 // The state s before this wave's steps, of which (P, E) is the map. The first wave of a
@@ -359,11 +397,20 @@ __device__ __forceinline__ void rec_store(const RecVec<DT, V>& r, char* p, int s
   }
 }
 
+// Rows' addresses are formed one after the other: the compiler would form all of them
+// ahead and spill scalar registers for it.
+__device__ __forceinline__ void rec_fence() { __builtin_amdgcn_sched_barrier(0); }
+
+// Both kernels ask for all of a wave's rows at once and keep its gates in registers across
+// the look-back. A whole wave (all T steps, no channels that two lanes have) has a way of
+// its own without masks and tests per row (of the vector instructions per value about a
+// fifth).
 template <int DT, int GT, int V, int T, bool LOGITS, bool COMPLEMENT>
 __global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_fwd_kernel(RecFwd p) {
   constexpr int ES = RecVec<DT, V>::ES, GS = RecVec<GT, V>::ES;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const RecWhere at = rec_where(p.t, p.sequences);
+  RecWhere at;
+  if (!rec_where(p.t, p.sequences, at)) return;
   const RecCols<V> k(at.block, lane, p.d);
   const int64_t s0 = ((int64_t)at.tile * waves + wave) * T;
   const int n = (int)min((int64_t)T, p.L - s0);  // this wave's steps (none: 0 or less)
@@ -371,51 +418,99 @@ __global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_fwd_kernel(
   float s[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) s[v] = first && p.h0 ? p.h0[(int64_t)at.b * p.d + k.c + v] : 0.f;
-  const char* x = p.x + at.b * p.L * p.x_ld + (int64_t)k.c * ES;
-  const char* g = p.g + at.b * p.L * p.g_ld + (int64_t)k.c * GS;
-  RecVec<DT, V> rx[T];
-  RecVec<GT, V> rg[T];
+  const int64_t row0 = at.b * p.L;
+  const unsigned cx = (unsigned)k.c * ES, cg = (unsigned)k.c * GS;
+  const bool whole = T > 1 && n == T && p.d % V == 0;
   float a[T][V], b[T][V], P[V], E[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     P[v] = first ? 0.f : 1.f;
     E[v] = s[v];
   }
-  if (n > 0) {
+  auto gate = [&](const RecVec<DT, V>& rx, const RecVec<GT, V>& rg, float (&at)[V], float (&bt)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float keep = 0.f, slope;
+      rec_gate<LOGITS, COMPLEMENT, false>(rg.get(v), p.inv_tau, at[v], keep, slope);
+      bt[v] = COMPLEMENT ? keep * rx.get(v) : rx.get(v);
+    }
+  };
+  if (whole) {
     RecWalk w(s0, p.L, p.H, p.W, p.dir);
+    RecRow x(p.x, row0, p.x_ld, w), g(p.g, row0, p.g_ld, w);
+    RecVec<DT, V> rx[T];
+    RecVec<GT, V> rg[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      rx[t].load(x + w.row * p.x_ld);
-      rg[t].load(g + w.row * p.g_ld);
-      if (t + 1 < n) w.next();  // (steps past the end read the last row again)
+      rx[t].load(x.p + cx);
+      rg[t].load(g.p + cg);
+      const bool end = w.next();
+      x.next(end);
+      g.next(end);
+      rec_fence();
     }
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+    for (int t = 0; t < T; ++t) {
+      gate(rx[t], rg[t], a[t], b[t]);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float keep = 0.f, slope;
-        rec_gate<LOGITS, COMPLEMENT, false>(rg[t].get(v), p.inv_tau, a[t][v], keep, slope);
-        b[t][v] = COMPLEMENT ? keep * rx[t].get(v) : rx[t].get(v);
-        if (T > 1 && t >= n) {
-          a[t][v] = 1.f;
-          b[t][v] = 0.f;
-        }
         E[v] = fmaf(a[t][v], E[v], b[t][v]);
         P[v] *= a[t][v];
       }
+    }
+  } else if (n > 0) {
+    RecWalk w(s0, p.L, p.H, p.W, p.dir);
+    RecRow x(p.x, row0, p.x_ld, w), g(p.g, row0, p.g_ld, w);
+    RecVec<DT, V> rx[T];
+    RecVec<GT, V> rg[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      rx[t].load(x.p + cx);
+      rg[t].load(g.p + cg);
+      if (t + 1 < n) {  // (steps past the end read the last row again)
+        const bool end = w.next();
+        x.next(end);
+        g.next(end);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      gate(rx[t], rg[t], a[t], b[t]);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        a[t][v] = t < n ? a[t][v] : 1.f;
+        b[t][v] = t < n ? b[t][v] : 0.f;
+        E[v] = fmaf(a[t][v], E[v], b[t][v]);
+        P[v] *= a[t][v];
+      }
+    }
   }
   if constexpr (T > 1) rec_carry<V>(p.t, at, wave, lane, P, E, s);
-  if (n <= 0) return;
-  char* h = p.h + (at.b * p.L * p.d + k.c) * ES;
+  if (n <= 0 || k.skip == V) return;
   RecWalk w(s0, p.L, p.H, p.W, p.dir);
+  RecRow h(p.h, row0, (int64_t)p.d * ES, w);
+  if (whole) {
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    RecVec<DT, V> r;
+    for (int t = 0; t < T; ++t) {
+      RecVec<DT, V> r;
 #pragma unroll
-    for (int v = 0; v < V; ++v) s[v] = fmaf(a[t][v], s[v], b[t][v]);
-    r.set(s);
-    if (t < n) rec_store(r, h + w.row * p.d * ES, k.skip);
-    w.next();
+      for (int v = 0; v < V; ++v) s[v] = fmaf(a[t][v], s[v], b[t][v]);
+      r.set(s);
+      r.store(h.p + cx);
+      h.next(w.next());
+      rec_fence();
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      // (past the end a = 1 and b = 0: the state stays)
+      RecVec<DT, V> r;
+#pragma unroll
+      for (int v = 0; v < V; ++v) s[v] = fmaf(a[t][v], s[v], b[t][v]);
+      r.set(s);
+      if (t < n) rec_store(r, h.p + cx, k.skip);
+      h.next(w.next());
+    }
   }
   if (p.h_final && s0 + n == p.L) {
 #pragma unroll
@@ -442,7 +537,8 @@ template <int DT, int GT, int V, int T, bool LOGITS, bool COMPLEMENT>
 __global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_bwd_kernel(RecBwd p) {
   constexpr int ES = RecVec<DT, V>::ES, GS = RecVec<GT, V>::ES;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const RecWhere at = rec_where(p.t, p.sequences);
+  RecWhere at;
+  if (!rec_where(p.t, p.sequences, at)) return;
   const RecCols<V> k(at.block, lane, p.d);
   const int64_t s0 = ((int64_t)at.tile * waves + wave) * T, state = (int64_t)at.b * p.d + k.c;
   const int n = (int)min((int64_t)T, p.L - s0);
@@ -450,71 +546,123 @@ __global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_bwd_kernel(
   float y[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) y[v] = first && p.dh_final ? p.dh_final[state + v] : 0.f;
-  const char* dh = p.dh + (at.b * p.L * p.d + k.c) * ES;
-  const char* h = p.h + (at.b * p.L * p.d + k.c) * ES;
-  const char* g = p.g + at.b * p.L * p.g_ld + (int64_t)k.c * GS;
-  const char* x = COMPLEMENT ? p.x + at.b * p.L * p.x_ld + (int64_t)k.c * ES : nullptr;
+  const int64_t row0 = at.b * p.L, dense = (int64_t)p.d * ES;
+  const unsigned cx = (unsigned)k.c * ES, cg = (unsigned)k.c * GS;
+  const bool whole = T > 1 && n == T && p.d % V == 0 && p.dx && p.dg;
+  const bool to_start = s0 + n == p.L;  // this wave has the scan's first token, before which the state is h0
   RecVec<DT, V> rd[T], rh[T], rx[T];
-  RecVec<GT, V> rg[T];
   float a[T][V], keep[T][V], slope[T][V], P[V], E[V], h0[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     P[v] = first ? 0.f : 1.f;
     E[v] = y[v];
-    h0[v] = 0.f;
+    h0[v] = to_start && p.h0 ? p.h0[state + v] : 0.f;
   }
-  if (n > 0) {
-    const bool to_start = s0 + n == p.L;  // this wave has the scan's first token, before which the state is h0
+  if (whole) {
     RecWalk w(s0, p.L, p.H, p.W, p.dir);
+    RecRow dh(p.dh, row0, dense, w), g(p.g, row0, p.g_ld, w), x(p.x, row0, p.x_ld, w), h(p.h, row0, dense, w);
+    RecVec<GT, V> rg[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      rd[t].load(dh + w.row * p.d * ES);
-      rg[t].load(g + w.row * p.g_ld);
-      if constexpr (COMPLEMENT) rx[t].load(x + w.row * p.x_ld);
-      if (t + 1 < n || (t + 1 == n && !to_start)) w.next();
-      rh[t].load(h + w.row * p.d * ES);  // (of the scan's first token: not used)
-    }
-    if (to_start && p.h0) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) h0[v] = p.h0[state + v];
+      rd[t].load(dh.p + cx);
+      rg[t].load(g.p + cg);
+      if constexpr (COMPLEMENT) rx[t].load(x.p + cx);
+      const bool end = w.next();
+      if (t + 1 < T || !to_start) h.next(end);
+      rh[t].load(h.p + cx);  // the row before; of the scan's first token its own, which is not used
+      dh.next(end);
+      g.next(end);
+      x.next(end);
     }
 #pragma unroll
     for (int t = 0; t < T; ++t)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         rec_gate<LOGITS, COMPLEMENT, true>(rg[t].get(v), p.inv_tau, a[t][v], keep[t][v], slope[t][v]);
-        const bool mine = T == 1 || t < n;
-        E[v] = mine ? a[t][v] * (rd[t].get(v) + E[v]) : E[v];
-        P[v] = mine ? a[t][v] * P[v] : P[v];
+        E[v] = a[t][v] * (rd[t].get(v) + E[v]);
+        P[v] *= a[t][v];
+      }
+  } else if (n > 0) {
+    RecWalk w(s0, p.L, p.H, p.W, p.dir);
+    RecRow dh(p.dh, row0, dense, w), g(p.g, row0, p.g_ld, w), x(p.x, row0, p.x_ld, w), h(p.h, row0, dense, w);
+    RecVec<GT, V> rg[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      rd[t].load(dh.p + cx);
+      rg[t].load(g.p + cg);
+      if constexpr (COMPLEMENT) rx[t].load(x.p + cx);
+      const bool inside = t + 1 < n;  // (steps past the end read the last row again)
+      if (inside || (t + 1 == n && !to_start)) {
+        const bool end = w.next();
+        h.next(end);
+        if (inside) {
+          dh.next(end);
+          g.next(end);
+          x.next(end);
+        }
+      }
+      rh[t].load(h.p + cx);
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        rec_gate<LOGITS, COMPLEMENT, true>(rg[t].get(v), p.inv_tau, a[t][v], keep[t][v], slope[t][v]);
+        E[v] = t < n ? a[t][v] * (rd[t].get(v) + E[v]) : E[v];
+        P[v] = t < n ? P[v] * a[t][v] : P[v];
       }
   }
   if constexpr (T > 1) rec_carry<V>(p.t, at, wave, lane, P, E, y);
-  if (n <= 0) return;
-  char* dx = p.dx ? p.dx + at.b * p.L * p.dx_ld + (int64_t)k.c * ES : nullptr;
-  char* dg = p.dg ? p.dg + at.b * p.L * p.dg_ld + (int64_t)k.c * GS : nullptr;
-  const bool to_start = s0 + n == p.L;
+  if (n <= 0 || k.skip == V) return;
   RecWalk w(s0, p.L, p.H, p.W, p.dir);
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    if (T > 1 && t >= n) break;
-    RecVec<DT, V> rdx;
-    RecVec<GT, V> rdg;
-    float ox[V], og[V];
+  RecRow dx(p.dx, row0, p.dx_ld, w), dg(p.dg, row0, p.dg_ld, w);
+  // one step's gradients
+  auto out = [&](const RecVec<DT, V>& rd, const RecVec<DT, V>& rx, const float (&before)[V], const float (&at)[V],
+                 const float (&kt)[V], const float (&st)[V], RecVec<DT, V>& ox, RecVec<GT, V>& og) {
+    float fx[V], fg[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const float D = rd[t].get(v) + y[v];
-      y[v] = a[t][v] * D;
-      ox[v] = COMPLEMENT ? keep[t][v] * D : D;
-      float before = to_start && t == n - 1 ? h0[v] : rh[t].get(v);
-      if constexpr (COMPLEMENT) before -= rx[t].get(v);
-      og[v] = y[v] * before;
-      if constexpr (LOGITS) og[v] *= slope[t][v];
+      const float D = rd.get(v) + y[v];
+      y[v] = at[v] * D;
+      fx[v] = COMPLEMENT ? kt[v] * D : D;
+      fg[v] = y[v] * (COMPLEMENT ? before[v] - rx.get(v) : before[v]);
+      if constexpr (LOGITS) fg[v] *= st[v];
     }
-    rdx.set(ox);
-    rdg.set(og);
-    if (dx) rec_store(rdx, dx + w.row * p.dx_ld, k.skip);
-    if (dg) rec_store(rdg, dg + w.row * p.dg_ld, k.skip);
-    w.next();
+    ox.set(fx);
+    og.set(fg);
+  };
+  if (whole) {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      RecVec<DT, V> ox;
+      RecVec<GT, V> og;
+      float before[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) before[v] = t + 1 == T && to_start ? h0[v] : rh[t].get(v);
+      out(rd[t], rx[t], before, a[t], keep[t], slope[t], ox, og);
+      ox.store(dx.p + cx);
+      og.store(dg.p + cg);
+      const bool end = w.next();
+      dx.next(end);
+      dg.next(end);
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      if (t < n) {
+        RecVec<DT, V> ox;
+        RecVec<GT, V> og;
+        float before[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) before[v] = t + 1 == n && to_start ? h0[v] : rh[t].get(v);
+        out(rd[t], rx[t], before, a[t], keep[t], slope[t], ox, og);
+        if (p.dx) rec_store(ox, dx.p + cx, k.skip);
+        if (p.dg) rec_store(og, dg.p + cg, k.skip);
+        const bool end = w.next();
+        dx.next(end);
+        dg.next(end);
+      }
+    }
   }
   if (p.dh0 && to_start) {
 #pragma unroll
@@ -535,8 +683,17 @@ __global__ void __launch_bounds__(256) rec_clear_kernel(u32x4* p, int64_t n) {
 // ---------------------------------------------------------------------------
 namespace gtr {
 
-constexpr int kRecFwdSteps = 16, kRecBwdSteps = 8;  // per wave
+// Steps of a wave and waves of a tile: what a work-group holds in registers and moves
+// while it has them decides how busy it keeps the memory (two work-groups per CU). Us of
+// 16, 8 and 4 waves, forward with 16 steps: 32768 x 4096 bf16 182, 177, 232; 16384 x 4096
+// float32 178, 160, 178; 8 x 1600 x 384 fp16 17.5, 17.2, 18.5 (with 8 steps: 248, 257, 412;
+// 176, 175, 233; 21, 22, 29); backward with 8 steps: 4 x 16384 x 2048 bf16 355, 327, 441;
+// 1600 x 192 fp16 13.8, 13.8, 14.6. A sequence that 16 waves take is one tile.
+constexpr int kRecFwdSteps = 16, kRecBwdSteps = 8;
+constexpr int kRecTileWaves = 8;
 constexpr unsigned kRecSpin = 1u << 22;             // polls of a wait, of a microsecond or less each
+
+static int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct RecPlan {
   int V, T, waves;
@@ -552,23 +709,26 @@ static gtr_status rec_plan(int32_t B, int32_t H, int32_t W, int32_t d, int steps
   r->V = d == 1 ? 1 : 2;
   r->T = L == 1 ? 1 : steps;
   const int64_t waves = (L + r->T - 1) / r->T;
-  r->waves = (int)(waves < kRecWaves ? waves : kRecWaves);
+  r->waves = (int)(waves <= kRecWaves ? waves : kRecTileWaves);
   const int64_t tiles = (waves + r->waves - 1) / r->waves;
   r->t = RecTiles{};
   r->t.tiles = (int)tiles;
   r->t.blocks = (d + 64 * r->V - 1) / (64 * r->V);
-  r->t.group = 4;
-  while ((int64_t)r->t.group * r->t.group < tiles && r->t.group < 64) r->t.group *= 2;
+  r->sequences = (int64_t)B * r->t.blocks;
+  // a hand-over between groups takes about 2 us, in which the sequences' tiles of a group
+  // are read (about 20 ns each): enough of them that the chain does not set the pace
+  r->t.group = r->sequences >= 16 ? 8 : r->sequences >= 8 ? 16 : r->sequences >= 4 ? 32 : 64;
   r->t.groups = (int)((tiles + r->t.group - 1) / r->t.group);
   r->t.spin = kRecSpin;
-  r->sequences = (int64_t)B * r->t.blocks;
-  r->grid = r->sequences * tiles;  // (below 2^62)
+  r->t.share = (unsigned)(r->sequences * tiles <= 2048 ? up(r->sequences, kRecCounters) : r->sequences);
+  r->t.lanes = (unsigned)up(r->sequences, r->t.share);
+  r->grid = tiles > 1 ? (int64_t)r->t.share * r->t.lanes * tiles : r->sequences;  // (below 2^62)
   // a launch's threads stay below 2^32
   if (r->grid > (((int64_t)1 << 32) - 1) / (64 * r->waves)) return GTR_ERR_SHAPE;
   r->need = r->clear = 0;
   if (tiles > 1) {
     const size_t words = (size_t)r->sequences * (size_t)(tiles + r->t.groups) * 64 * r->V;
-    r->clear = r->need = 256 + words * 8;
+    r->clear = r->need = kRecCounters * kRecCounterStep * 4 + words * 8;
   }
   return GTR_OK;
 }
@@ -618,8 +778,8 @@ static gtr_status rec_workspace(const RecPlan& r, const void* ws, size_t bytes) 
 static void rec_words(RecPlan* r, void* ws, uint32_t spin, hipStream_t stream) {
   if (spin) r->t.spin = spin;
   if (!r->need) return;
-  r->t.counter = static_cast<unsigned*>(ws);
-  r->t.maps = reinterpret_cast<unsigned long long*>(static_cast<char*>(ws) + 256);
+  r->t.counters = static_cast<unsigned*>(ws);
+  r->t.maps = reinterpret_cast<unsigned long long*>(static_cast<char*>(ws) + kRecCounters * kRecCounterStep * 4);
   r->t.states = r->t.maps + r->sequences * r->t.tiles * 64 * r->V;
   const int64_t n = (int64_t)(r->clear / 16), blocks = (n + 255) / 256;
   hipLaunchKernelGGL(rec_clear_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, stream,

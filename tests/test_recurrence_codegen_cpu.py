@@ -6,7 +6,7 @@ import pytest
 
 from test_training_codegen_cpu import Buffers, check_kernel, emu, kernel_named, listing
 
-WAVES, STEPS = 16, (16, 8)  # most waves of a work-group, steps of a wave forward and backward
+WAVES, TILE_WAVES, STEPS = 16, 8, (16, 8)  # of a sequence in one tile, of a tile; steps of a wave forward and backward
 
 
 def _brev(w, i):
@@ -14,23 +14,32 @@ def _brev(w, i):
     w.s32set(i.ops[0], int(f"{v & 0xffffffff:032b}"[::-1], 2), emu.M32 if o else 0, d)
 
 
-emu.HANDLERS["s_brev_b32"] = _brev
+def _sign_extend(w, i):  # the lower 32 bits of a pair
+    assert i.ops[2] == "0x200000", i.raw
+    at = int(i.ops[1][2:].split(":")[0])
+    v, o, d = w.s32(f"s{at}", i)
+    w.s64set(i.ops[0], v | (0xffffffff00000000 if v >> 31 else 0), (1 << 64) - 1 if o else 0, d)
+    emu.set_scc(w, v != 0, bool(o), d)
+
+
+emu.HANDLERS.update({"s_brev_b32": _brev, "s_bfe_i64": _sign_extend})
 for _c in ("ngt", "nlt", "gt", "lt"):  # (of loaded values: every outcome)
     for _e in ("e32", "sdwa"):
         emu.HANDLERS.setdefault(f"v_cmp_{_c}_f16_{_e}", emu.vcmp(lambda a, b: a < a, "u32"))
 
 
-def tiles_of(L, T, waves_most):
+def tiles_of(L, T):
     T = 1 if L == 1 else T
     waves = -(-L // T)
-    return T, min(waves, waves_most), -(-waves // min(waves, waves_most))
+    most = waves if waves <= WAVES else TILE_WAVES
+    return T, most, -(-waves // most)
 
 
 def tiles(new, seqs, n, V, group, blocks):
     groups = -(-n // group)
     maps, states = (new(k, seqs * m * 64 * V * 8, "rw") if n > 1 else 0 for k, m in (("maps", n), ("states", groups)))
-    # no counter: a work-group's tile is its index, which the emulator knows
-    return struct.pack("<QQQiiiiI4x", maps, states, 0, n, group, groups, blocks, 1)
+    # no counters: a work-group's tile is its index, which the emulator knows
+    return struct.pack("<QQQiiiiIII4x", maps, states, 0, n, group, groups, blocks, seqs, 1, 1)
 
 
 # one token; a wave's steps, broken; several waves; several tiles, groups of them, a broken last one; a grid by columns
@@ -47,7 +56,7 @@ def test_addresses(B, H, W, d, dt, gt, logits, complement, scan):
     blocks = -(-d // (64 * V))
     seqs = B * blocks
     for forward, steps in ((True, STEPS[0]), (False, STEPS[1])):
-        T, waves, n = tiles_of(L, steps, WAVES)
+        T, waves, n = tiles_of(L, steps)
         new = Buffers()
         t = tiles(new, seqs, n, V, 4, blocks)
         span = ((B * L - 1) * ld + d)
