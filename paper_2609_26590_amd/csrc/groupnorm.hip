@@ -7,10 +7,14 @@
 //             dx = rstd (t - mean(t) - xh mean(t xh)) (+ dres)
 //             dw = sum over images and tokens of du xh,  db = that of du
 //
-// What bounds both is memory: each value read once and written once, where an image's
-// block of groups fits the registers of one work-group (gn_*_slab_kernel), else read
-// twice by two launches (gn_*_sums_kernel, gn_*_rows_kernel).
+// What bounds both is memory and, for small images, the chain of loads, sums and stores.
+// Where an image's block of groups fits the registers of one work-group, it is read once,
+// in one launch (gn_*_image_kernel), else twice by two launches (gn_*_sums_kernel,
+// gn_*_rows_kernel).
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
 
 #include "ffn_gemm.h"
 #include "gtr.h"
@@ -21,16 +25,23 @@
 namespace gtr {
 
 // The channels in blocks: kg whole groups each, or where a group is wider than a block
-// allows, `pieces` of pw channels (the last may be narrower). The tokens in tiles of R.
+// allows, `pieces` of pw channels (the last may be narrower). nl lanes, a power of two up to
+// 64, hold a block's row, and a work-group rp rows at a time, a row group. Tile t of an image
+// has the row groups t, t + tiles, ..: all tiles go through the memory side by side.
 struct GnShape {
   int64_t L;
   int B, C, G, Cg;
   int kg, pieces, pw, blocks;
-  int tiles, R;
-  int team;  // threads that add a group's channels: a power of two, kg teams at most the work-group's threads
+  int nl, shift;  // shift: log2 nl
+  int tiles;
+  int team, tshift;  // threads that add a group's channels: a power of two, kg teams at most the work-group's threads
+  float inv_width, inv_pieces;  // of a group's channels in a block
 };
+// n / d for 0 <= n < 2^14 and whole d: (n + 1/2) / d is 1 / (2 d) from a whole number or more,
+// its rounding errors under 2^-8 / d.
+__device__ __forceinline__ int gn_div(int n, float inv) { return (int)(((float)n + 0.5f) * inv); }
 struct GnBlock {
-  int g0, ng, c0, cb, piece;
+  int g0, ng, c0, cb, piece, width;  // width: of a group, or of the piece
   __device__ __forceinline__ GnBlock(const GnShape& s, int block) {
     if (s.pieces == 1) {
       g0 = block * s.kg;
@@ -38,12 +49,13 @@ struct GnBlock {
       piece = 0;
       c0 = g0 * s.Cg;
       cb = ng * s.Cg;
+      width = s.Cg;
     } else {
-      g0 = block / s.pieces;
+      g0 = block / s.pieces;  // (uniform)
       ng = 1;
       piece = block - g0 * s.pieces;
       c0 = g0 * s.Cg + piece * s.pw;
-      cb = min(s.pw, s.Cg - piece * s.pw);
+      cb = width = min(s.pw, s.Cg - piece * s.pw);
     }
   }
 };
@@ -55,47 +67,54 @@ struct GnAt {
   int image, tile, block;
   __device__ __forceinline__ GnAt(const GnShape& s, unsigned id, bool back) {
     if (back) id = (unsigned)s.B * s.tiles * s.blocks - 1 - id;
-    const unsigned t = id / (unsigned)s.blocks;
+    const unsigned t = s.blocks == 1 ? id : id / (unsigned)s.blocks;
     block = (int)(id - t * (unsigned)s.blocks);
-    image = (int)(t / (unsigned)s.tiles);
+    image = s.B == 1 ? 0 : (int)(t / (unsigned)s.tiles);
     tile = (int)(t - (unsigned)image * (unsigned)s.tiles);
   }
 };
 
-__device__ __forceinline__ float gn_act(float u, int act) {
-  if (act == GTR_ACT_NONE) return u;
-  float slope;
-  return ffn_act(u, act, slope);
-}
-__device__ __forceinline__ float gn_slope(float u, int act) {
-  if (act == GTR_ACT_NONE) return 1.f;
-  float slope;
-  ffn_act(u, act, slope);
-  return slope;
+// f with the activation as a constant: one test per loop, not three per value.
+template <int ACT>
+struct GnAct {
+  static __device__ __forceinline__ float value(float u) {
+    if constexpr (ACT == GTR_ACT_NONE) return u;
+    float slope;
+    return ffn_act(u, ACT, slope);
+  }
+  static __device__ __forceinline__ float slope(float u) {
+    if constexpr (ACT == GTR_ACT_NONE) return 1.f;
+    float s;
+    ffn_act(u, ACT, s);
+    return s;
+  }
+};
+template <class F>
+__device__ __forceinline__ void gn_by_act(int act, const F& f) {
+  if (act == GTR_ACT_SILU)
+    f(GnAct<GTR_ACT_SILU>());
+  else if (act == GTR_ACT_GELU)
+    f(GnAct<GTR_ACT_GELU>());
+  else
+    f(GnAct<GTR_ACT_NONE>());
 }
 
-// A work-group's threads on a block: nl lanes hold a row's vectors, rp rows at a time.
-// Threads past rp nl are off.
+// A thread's place on a block: its vector of the row, and which of the rows that the
+// work-group takes at a time. Lanes past the block's width have nothing.
 template <int DT, bool TINY>
 struct GnLane {
   static constexpr int VE = Ln<DT>::VE;
-  int nl, rp, r;
-  bool on;
   LnCols<DT, TINY> k;
-  __device__ __forceinline__ GnLane(int cb)
-      : nl((cb + VE - 1) / VE),
-        rp((int)blockDim.x / nl),
-        r((int)threadIdx.x / nl),
-        on(r < rp),
-        k((int)threadIdx.x - r * nl, cb) {}
+  int r, rp;
+  __device__ __forceinline__ GnLane(const GnShape& s, int cb)
+      : k((int)threadIdx.x & (s.nl - 1), cb), r((int)threadIdx.x >> s.shift), rp((int)blockDim.x >> s.shift) {}
   // the groups (of the block's) of this lane's channels
-  __device__ __forceinline__ void groups(int Cg, int (&g)[VE]) const {
-    const int q = k.c / Cg;
-    int rem = k.c - q * Cg, i = q;
+  __device__ __forceinline__ void groups(const GnShape& s, const GnBlock& b, int (&g)[VE]) const {
+    int i = s.pieces == 1 ? gn_div(k.c, s.inv_width) : 0, rem = k.c - i * b.width;
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
-      g[e] = i;
-      if (++rem == Cg) {
+      g[e] = min(i, b.ng - 1);
+      if (++rem == b.width) {
         rem = 0;
         ++i;
       }
@@ -103,51 +122,104 @@ struct GnLane {
   }
 };
 
-// Sums over a work-group, all in a fixed order. `v`: a value per channel of this thread's,
-// zeros in threads that are off; cols: at least blockDim VE floats. What is returned lies in
-// cols[0 .. cb): the columns' sums. (Starts and ends with a barrier.)
-template <int DT, bool TINY>
-__device__ __forceinline__ void gn_columns(const GnLane<DT, TINY>& ln, int cb, const float (&v)[Ln<DT>::VE], float* cols) {
-  constexpr int VE = Ln<DT>::VE;
-  const int n = blockDim.x, t = threadIdx.x;
-  __syncthreads();
-  if (ln.on)
-#pragma unroll
-    for (int e = 0; e < VE; ++e)
-      if (ln.k.has(e)) cols[ln.r * cb + ln.k.c + e] = v[e];
-  __syncthreads();
-  if (cb >= n) {
-    for (int c = t; c < cb; c += n) {
-      float a = 0.f;
-      for (int r = 0; r < ln.rp; ++r) a += cols[r * cb + c];
-      cols[c] = a;  // (only this thread reads column c)
-    }
-  } else {
-    // slices of the rows, then the slices: each thread adds about VE values
-    const int slices = n / cb, s = t / cb, c = t - s * cb;
-    float a = 0.f;
-    if (s < slices)
-      for (int r = s; r < ln.rp; r += slices) a += cols[r * cb + c];
-    __syncthreads();
-    if (s < slices) cols[s * cb + c] = a;
-    __syncthreads();
-    if (t < cb) {
-      a = cols[t];
-      for (int i = 1; i < slices; ++i) a += cols[i * cb + t];
-      cols[t] = a;
-    }
+// An image's row groups over its tiles: each tile has `base`, the first `more` one besides,
+// and the last group lacks `lack` rows.
+struct GnTiles {
+  int base, more, lack, last;
+  __device__ __forceinline__ GnTiles(const GnShape& s, int rp) {
+    const int L = (int)s.L, groups = (L >> __builtin_ctz(rp)) + ((L & (rp - 1)) != 0);
+    base = s.tiles == 1 ? groups : groups / s.tiles;
+    more = groups - base * s.tiles;
+    lack = (int)((int64_t)groups * rp - s.L);
+    last = more ? more - 1 : s.tiles - 1;  // the tile that has it
   }
-  __syncthreads();
+  __device__ __forceinline__ int groups(int tile) const { return base + (tile < more); }
+  __device__ __forceinline__ int rows(int tile, int rp) const { return groups(tile) * rp - (tile == last ? lack : 0); }
+  // of which a thread whose row of each group is r has
+  __device__ __forceinline__ int rows_of(int tile, int r, int rp) const {
+    return groups(tile) - (tile == last && r >= rp - lack);
+  }
+};
+
+// Sums of N values per lane over the lanes of a wave that hold the same vector of a row, in
+// every one of them, in registers: rows of 16 lanes rotate, halves and quarters swap.
+template <int ROT>
+__device__ __forceinline__ float gn_rot(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x120 + ROT, 0xf, 0xf, false));
 }
-// The groups' sums of cols[0 .. cb) into sums[0 .. ng) (ends with a barrier).
-__device__ __forceinline__ void gn_teams(const GnShape& s, const GnBlock& b, const float* cols, float* sums) {
-  const int g = threadIdx.x / s.team, i = threadIdx.x - g * s.team;
-  const int width = s.pieces == 1 ? s.Cg : b.cb;
+__device__ __forceinline__ float gn_halves(float x) {
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const unsigned lo = r[0], hi = r[1];
+  return __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+}
+__device__ __forceinline__ float gn_quarters(float x) {
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const unsigned lo = r[0], hi = r[1];
+  return __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+}
+template <int N>
+__device__ __forceinline__ void gn_wave(float (&v)[N], int nl) {
+  if (nl <= 32)
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = gn_halves(v[e]);
+  if (nl <= 16)
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = gn_quarters(v[e]);
+  if (nl <= 8)
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] += gn_rot<8>(v[e]);
+  if (nl <= 4)
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] += gn_rot<4>(v[e]);
+  if (nl <= 2)
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] += gn_rot<2>(v[e]);
+  if (nl <= 1)
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] += gn_rot<1>(v[e]);
+}
+
+// The waves' sums of each channel lie in cols[wave][element][lane]: by element first, so
+// that neither writes nor reads meet in a bank of LDS.
+template <int DT>
+__device__ __forceinline__ void gn_put(const GnShape& s, float (&v)[Ln<DT>::VE], float* cols) {
+  constexpr int VE = Ln<DT>::VE;
+  gn_wave(v, s.nl);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (lane < s.nl)
+#pragma unroll
+    for (int e = 0; e < VE; ++e) cols[(wave * VE + e) * s.nl + lane] = v[e];
+}
+// The work-group's sum of channel c of the block.
+template <int DT, bool TINY>
+__device__ __forceinline__ float gn_column(const GnShape& s, int cb, int c, const float* cols) {
+  constexpr int VE = Ln<DT>::VE;
+  const int l = c / VE, e = c - (TINY ? l * VE : min(l * VE, cb - VE)), waves = blockDim.x >> 6;
+  float a = 0.f;
+  for (int w = 0; w < waves; ++w) a += cols[(w * VE + e) * s.nl + l];
+  return a;
+}
+// Sums over a team's threads, which a wave has whole, in every one of them.
+__device__ __forceinline__ float gn_team_sum(float a, int team) {
+  for (int o = 1; o < team; o <<= 1) a += __shfl_xor(a, o, kWave);
+  return a;
+}
+// The groups' sums over a work-group of a value per channel (v is used up; values of
+// channels that the lane has not, or shares, are not looked at), in a fixed order, divided by
+// n, into sums[0 .. ng). Two barriers, the last at the end; cols: 64 VE floats per wave.
+template <int DT, bool TINY>
+__device__ __forceinline__ void gn_group_sums(const GnShape& s, const GnBlock& b, float (&v)[Ln<DT>::VE], float n,
+                                              float* cols, float* sums) {
+  gn_put<DT>(s, v, cols);
+  __syncthreads();
+  const int g = threadIdx.x >> s.tshift, i = threadIdx.x & (s.team - 1);
   float a = 0.f;
   if (g < b.ng)
-    for (int c = i; c < width; c += s.team) a += cols[g * width + c];
-  for (int o = 1; o < s.team; o <<= 1) a += __shfl_xor(a, o, kWave);
-  if (g < b.ng && i == 0) sums[g] = a;
+    for (int c = i; c < b.width; c += s.team) a += gn_column<DT, TINY>(s, b.cb, g * b.width + c, cols);
+  a = gn_team_sum(a, s.team);
+  if (g < b.ng && i == 0) sums[g] = a / n;
   __syncthreads();
 }
 
@@ -155,21 +227,47 @@ __device__ __forceinline__ void gn_teams(const GnShape& s, const GnBlock& b, con
 struct GnStat {
   float n, mean, m2;
   __device__ __forceinline__ void join(float n2, float mean2, float m22) {
-    const float all = n + n2, d = mean2 - mean, f = all > 0.f ? n2 / all : 0.f;
+    const float all = n + n2, d = mean2 - mean, f = n > 0.f ? n2 * __builtin_amdgcn_rcpf(all) : 1.f;
     mean = fmaf(d, f, mean);
     m2 += fmaf(d * d, n * f, m22);
     n = all;
   }
+  // with the lane's across bit o: both in the same order, the lower lane's first
+  __device__ __forceinline__ void join_across(int o) {
+    const float n2 = __shfl_xor(n, o, kWave), mn = __shfl_xor(mean, o, kWave), q = __shfl_xor(m2, o, kWave);
+    const bool low = (threadIdx.x & o) == 0;
+    GnStat a = {low ? n : n2, low ? mean : mn, low ? m2 : q};
+    a.join(low ? n2 : n, low ? mn : mean, low ? q : m2);
+    *this = a;
+  }
 };
 
-// Vectors that are unpacked again from here on: without it the compiler keeps their
-// elements, in twice the registers or more.
+// A vector in four registers next to each other, and unpacked again from here on: without
+// that the compiler keeps its elements, in twice the registers or more.
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x4 gn_load(const char* p) {
+  return __builtin_bit_cast(u32x4, *reinterpret_cast<const Vec16*>(p));
+}
+__device__ __forceinline__ Vec16 gn_vec(u32x4 v) { return __builtin_bit_cast(Vec16, v); }
 template <int N>
-__device__ __forceinline__ void gn_packed(Vec16 (&v)[N]) {
+__device__ __forceinline__ void gn_packed(u32x4 (&v)[N]) {
 #pragma unroll
-  for (int i = 0; i < N; ++i)
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
+}
+
+// One vector after the other: unpacked side by side they would not fit the registers.
+__device__ __forceinline__ void gn_next() { __builtin_amdgcn_sched_barrier(0); }
+
+// To a lane's vector of a row, at its address.
+template <int DT>
+__device__ __forceinline__ void gn_store(const LnCols<DT, false>& k, char* at, const float (&x)[Ln<DT>::VE]) {
+  if (k.skip == 0) {
+    *reinterpret_cast<Vec16*>(at) = Ln<DT>::pack(x);
+  } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(v[i].u[e]));
+    for (int e = 0; e < Ln<DT>::VE; ++e)
+      if (k.has(e)) Ln<DT>::put(at + e * Ln<DT>::ES, x[e]);
+  }
 }
 
 struct GnFwd {
@@ -183,7 +281,83 @@ struct GnFwd {
   int act;
 };
 
-constexpr int kGnThreads = 256, kGnSlab = 1024;
+constexpr int kGnThreads = 256, kGnImage = 1024;
+
+// An image's block whole: its rows in the registers of one work-group, NV vectors per
+// thread, so that x is read once and the squares are taken about the mean.
+template <int DT, int NV>
+__global__ void __launch_bounds__(kGnImage) gn_fwd_image_kernel(GnFwd p) {
+  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES;
+  __shared__ float cols[kGnImage * VE], sums[2][kGnImage];
+  const GnShape& s = p.s;
+  const GnAt wg(s, blockIdx.x, false);
+  const GnBlock blk(s, wg.block);
+  const GnLane<DT, false> ln(s, blk.cb);
+  const int64_t ld = (int64_t)s.C * ES, at = (int64_t)wg.image * s.L * ld + (int64_t)blk.c0 * ES;
+  const int L = (int)s.L;
+  u32x4 x[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) x[i] = gn_load(p.x + at + (int64_t)min(ln.r + i * ln.rp, L - 1) * ld + ln.k.c * ES);
+  float v[VE], w[VE], b[VE], mean[VE];
+  int gi[VE];
+  ln.groups(s, blk, gi);
+  ln.k.load_f32(p.w ? p.w + blk.c0 : nullptr, 1.f, w);
+  ln.k.load_f32(p.b ? p.b + blk.c0 : nullptr, 0.f, b);
+  const float all = (float)L * (float)s.Cg;
+#pragma unroll
+  for (int e = 0; e < VE; ++e) v[e] = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float a[VE];
+    Ln<DT>::unpack(gn_vec(x[i]), a);
+    const bool in = ln.r + i * ln.rp < L;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) v[e] += in ? a[e] : 0.f;
+    gn_next();
+  }
+  gn_packed(x);
+  gn_group_sums<DT, false>(s, blk, v, all, cols, sums[0]);
+#pragma unroll
+  for (int e = 0; e < VE; ++e) {
+    mean[e] = sums[0][gi[e]];
+    v[e] = 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float a[VE];
+    Ln<DT>::unpack(gn_vec(x[i]), a);
+    const bool in = ln.r + i * ln.rp < L;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const float d = in ? a[e] - mean[e] : 0.f;
+      v[e] = fmaf(d, d, v[e]);
+    }
+    gn_next();
+  }
+  gn_packed(x);
+  gn_group_sums<DT, false>(s, blk, v, all, cols, sums[1]);
+  if ((int)threadIdx.x < blk.ng) {
+    const int64_t g = (int64_t)wg.image * s.G + blk.g0 + threadIdx.x;
+    if (p.mean) p.mean[g] = sums[0][threadIdx.x];
+    if (p.rstd) p.rstd[g] = 1.f / sqrtf(sums[1][threadIdx.x] + p.eps);
+  }
+  if (ln.k.skip == VE) return;
+#pragma unroll
+  for (int e = 0; e < VE; ++e) w[e] *= 1.f / sqrtf(sums[1][gi[e]] + p.eps);
+  gn_by_act(p.act, [&](auto act) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (ln.r + i * ln.rp < L) {
+        float a[VE];
+        Ln<DT>::unpack(gn_vec(x[i]), a);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) a[e] = act.value(fmaf(a[e] - mean[e], w[e], b[e]));
+        ln.k.store(p.y + at + (int64_t)(ln.r + i * ln.rp) * ld, a);
+      }
+      gn_next();
+    }
+  });
+}
 
 // Each tile's statistics. A lane takes its channels' sums about the first value it sees of
 // each (n values about one of them: their sum of squares loses at most n 2^-24 of itself),
@@ -191,62 +365,60 @@ constexpr int kGnThreads = 256, kGnSlab = 1024;
 template <int DT, bool TINY>
 __global__ void __launch_bounds__(kGnThreads) gn_fwd_sums_kernel(GnFwd p) {
   constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES, U = 4;
-  __shared__ float cols[kGnThreads * VE], sums[kGnThreads];
-  const GnAt wg(p.s, blockIdx.x, false);
-  const GnBlock blk(p.s, wg.block);
-  const GnLane<DT, TINY> ln(blk.cb);
-  const int64_t first = (int64_t)wg.tile * p.s.R, end = min(first + p.s.R, p.s.L), ld = (int64_t)p.s.C * ES;
-  const int rows = (int)(end - first);
-  const char* x = p.x + ((int64_t)wg.image * p.s.L + first) * ld + (int64_t)blk.c0 * ES;
+  __shared__ float cols[kGnThreads * VE], sums[2][kGnThreads];
+  const GnShape& s = p.s;
+  const GnAt wg(s, blockIdx.x, false);
+  const GnBlock blk(s, wg.block);
+  const GnLane<DT, TINY> ln(s, blk.cb);
+  const GnTiles tiles(s, ln.rp);
+  const int64_t ld = (int64_t)s.C * ES, step = (int64_t)ln.rp * s.tiles * ld;
+  const int n = tiles.rows_of(wg.tile, ln.r, ln.rp);
+  const char* x = p.x + ((int64_t)wg.image * s.L + (int64_t)ln.rp * wg.tile + ln.r) * ld + (int64_t)blk.c0 * ES;
   float pivot[VE], s1[VE], s2[VE];
-  int n = 0;
 #pragma unroll
   for (int e = 0; e < VE; ++e) pivot[e] = s1[e] = s2[e] = 0.f;
-  if (ln.on && ln.r < rows) {
-    n = (rows - ln.r + ln.rp - 1) / ln.rp;
+  if (n > 0) {
     for (int i = 0; i < n; i += U) {
       Vec16 v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = ln.k.load(x + (int64_t)(ln.r + min(i + u, n - 1) * ln.rp) * ld);
+      for (int u = 0; u < U; ++u) v[u] = ln.k.load(x + min(i + u, n - 1) * step);
       if (i == 0) ln.k.unpack(v[0], pivot);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (i + u >= n) break;
-        float a[VE];
-        ln.k.unpack(v[u], a);
+        if (i + u < n) {
+          float a[VE];
+          ln.k.unpack(v[u], a);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-          a[e] -= pivot[e];
-          s1[e] += a[e];
-          s2[e] = fmaf(a[e], a[e], s2[e]);
+          for (int e = 0; e < VE; ++e) {
+            a[e] -= pivot[e];
+            s1[e] += a[e];
+            s2[e] = fmaf(a[e], a[e], s2[e]);
+          }
         }
       }
     }
   }
-  const float cnt = (float)n, inv = n ? 1.f / cnt : 0.f, all = (float)rows * (float)(p.s.pieces == 1 ? p.s.Cg : blk.cb);
+  const float cnt = (float)n, inv = n ? 1.f / cnt : 0.f, all = (float)tiles.rows(wg.tile, ln.rp) * (float)blk.width;
   float v[VE], mean[VE];
 #pragma unroll
   for (int e = 0; e < VE; ++e) {
     mean[e] = fmaf(s1[e], inv, pivot[e]);
-    s2[e] = fmaxf(fmaf(-s1[e] * inv, s1[e], s2[e]), 0.f);
+    s2[e] = fmaf(-s1[e] * inv, s1[e], s2[e]);
+    s2[e] = s2[e] < 0.f ? 0.f : s2[e];  // (a NaN stays)
     v[e] = fmaf(cnt, pivot[e], s1[e]);
   }
-  gn_columns(ln, blk.cb, v, cols);
-  gn_teams(p.s, blk, cols, sums);
+  gn_group_sums<DT, TINY>(s, blk, v, all, cols, sums[0]);
   int gi[VE];
-  ln.groups(p.s.pieces == 1 ? p.s.Cg : blk.cb, gi);
+  ln.groups(s, blk, gi);
 #pragma unroll
   for (int e = 0; e < VE; ++e) {
-    const float d = mean[e] - sums[min(gi[e], blk.ng - 1)] / all;
+    const float d = mean[e] - sums[0][gi[e]];
     v[e] = fmaf(cnt * d, d, s2[e]);
   }
-  float m = 0.f;
-  if ((int)threadIdx.x < blk.ng) m = sums[threadIdx.x] / all;
-  gn_columns(ln, blk.cb, v, cols);
-  gn_teams(p.s, blk, cols, sums);
+  gn_group_sums<DT, TINY>(s, blk, v, 1.f, cols, sums[1]);
   if ((int)threadIdx.x < blk.ng)
-    p.part[(((int64_t)wg.image * p.s.tiles + wg.tile) * p.s.pieces + blk.piece) * p.s.G + blk.g0 + threadIdx.x] =
-        float2{m, sums[threadIdx.x]};
+    p.part[(((int64_t)wg.image * s.tiles + wg.tile) * s.pieces + blk.piece) * s.G + blk.g0 + threadIdx.x] =
+        float2{sums[0][threadIdx.x], sums[1][threadIdx.x]};
 }
 
 // The groups' statistics of an image from its tiles', and a tile's rows.
@@ -257,29 +429,32 @@ __global__ void __launch_bounds__(kGnThreads) gn_fwd_rows_kernel(GnFwd p) {
   const GnShape& s = p.s;
   const GnAt wg(s, blockIdx.x, true);
   const GnBlock blk(s, wg.block);
-  const GnLane<DT, TINY> ln(blk.cb);
+  const GnLane<DT, TINY> ln(s, blk.cb);
+  const GnTiles tiles(s, ln.rp);
+  const int64_t ld = (int64_t)s.C * ES, step = (int64_t)ln.rp * s.tiles * ld;
+  const int n = tiles.rows_of(wg.tile, ln.r, ln.rp);
+  const int64_t at = ((int64_t)wg.image * s.L + (int64_t)ln.rp * wg.tile + ln.r) * ld + (int64_t)blk.c0 * ES;
+  // the first rows are on their way while the statistics are put together
+  Vec16 v[U];
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = ln.k.load(p.x + at + min(i + u, n - 1) * step);
+  };
+  if (n > 0) fetch(0);
   {
-    const int g = threadIdx.x / s.team, i = threadIdx.x - g * s.team, entries = s.tiles * s.pieces;
+    const int g = threadIdx.x >> s.tshift, i = threadIdx.x & (s.team - 1), entries = s.tiles * s.pieces;
     GnStat st = {0.f, 0.f, 0.f};
     if (g < blk.ng) {
       const float2* q = p.part + (int64_t)wg.image * entries * s.G + blk.g0 + g;
 #pragma unroll 4
       for (int j = i; j < entries; j += s.team) {
         const float2 v = q[(int64_t)j * s.G];
-        const int tile = s.pieces == 1 ? j : j / s.pieces, piece = s.pieces == 1 ? 0 : j - tile * s.pieces;
-        const int rows = (int)min((int64_t)s.R, s.L - (int64_t)tile * s.R);
+        const int tile = s.pieces == 1 ? j : gn_div(j, s.inv_pieces), piece = s.pieces == 1 ? 0 : j - tile * s.pieces;
         const int width = s.pieces == 1 ? s.Cg : min(s.pw, s.Cg - piece * s.pw);
-        st.join((float)rows * (float)width, v.x, v.y);
+        st.join((float)tiles.rows(tile, ln.rp) * (float)width, v.x, v.y);
       }
     }
-    for (int o = 1; o < s.team; o <<= 1) {
-      // (both partners join in the same order, the lower one's first)
-      const float n = __shfl_xor(st.n, o, kWave), m = __shfl_xor(st.mean, o, kWave), q = __shfl_xor(st.m2, o, kWave);
-      const bool low = (threadIdx.x & o) == 0;
-      GnStat a = {low ? st.n : n, low ? st.mean : m, low ? st.m2 : q};
-      a.join(low ? n : st.n, low ? m : st.mean, low ? q : st.m2);
-      st = a;
-    }
+    for (int o = 1; o < s.team; o <<= 1) st.join_across(o);
     if (g < blk.ng && i == 0) {
       const float rs = 1.f / sqrtf(st.m2 / st.n + p.eps);
       smean[g] = st.mean;
@@ -291,109 +466,32 @@ __global__ void __launch_bounds__(kGnThreads) gn_fwd_rows_kernel(GnFwd p) {
     }
     __syncthreads();
   }
-  const int64_t first = (int64_t)wg.tile * s.R, end = min(first + s.R, s.L), ld = (int64_t)s.C * ES;
-  const int rows = (int)(end - first);
-  if (!ln.on || ln.r >= rows) return;
-  const int64_t at = ((int64_t)wg.image * s.L + first) * ld + (int64_t)blk.c0 * ES;
+  if (ln.k.skip == VE || n <= 0) return;
   int gi[VE];
-  ln.groups(s.pieces == 1 ? s.Cg : blk.cb, gi);
-  float mean[VE], rs[VE], w[VE], b[VE];
+  ln.groups(s, blk, gi);
+  float mean[VE], w[VE], b[VE];
   ln.k.load_f32(p.w ? p.w + blk.c0 : nullptr, 1.f, w);
   ln.k.load_f32(p.b ? p.b + blk.c0 : nullptr, 0.f, b);
 #pragma unroll
   for (int e = 0; e < VE; ++e) {
-    const int g = min(gi[e], blk.ng - 1);
-    mean[e] = smean[g];
-    rs[e] = srstd[g];
+    mean[e] = smean[gi[e]];
+    w[e] *= srstd[gi[e]];
   }
-  const int n = (rows - ln.r + ln.rp - 1) / ln.rp;
-  for (int i = 0; i < n; i += U) {
-    Vec16 v[U];
+  gn_by_act(p.act, [&](auto act) {
+    for (int i = 0; i < n; i += U) {
+      if (i) fetch(i);
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = ln.k.load(p.x + at + (int64_t)(ln.r + min(i + u, n - 1) * ln.rp) * ld);
+      for (int u = 0; u < U; ++u) {
+        if (i + u < n) {
+          float a[VE];
+          ln.k.unpack(v[u], a);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i + u >= n) break;
-      float a[VE];
-      ln.k.unpack(v[u], a);
-#pragma unroll
-      for (int e = 0; e < VE; ++e) a[e] = gn_act(fmaf((a[e] - mean[e]) * rs[e], w[e], b[e]), p.act);
-      ln.k.store(p.y + at + (int64_t)(ln.r + (i + u) * ln.rp) * ld, a);
+          for (int e = 0; e < VE; ++e) a[e] = act.value(fmaf(a[e] - mean[e], w[e], b[e]));
+          ln.k.store(p.y + at + (i + u) * step, a);
+        }
+      }
     }
-  }
-}
-
-// An image's block whole: its rows in the registers of one work-group, NV vectors per
-// thread, so that x is read once and the squares are taken about the mean.
-template <int DT, int NV>
-__global__ void __launch_bounds__(kGnSlab) gn_fwd_slab_kernel(GnFwd p) {
-  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES;
-  __shared__ float cols[kGnSlab * VE], sums[kGnSlab];
-  const GnShape& s = p.s;
-  const GnAt wg(s, blockIdx.x, false);
-  const GnBlock blk(s, wg.block);
-  const GnLane<DT, false> ln(blk.cb);
-  const int64_t ld = (int64_t)s.C * ES, at = (int64_t)wg.image * s.L * ld + (int64_t)blk.c0 * ES;
-  const int L = (int)s.L;
-  Vec16 x[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) x[i] = ln.k.load(p.x + at + (int64_t)min(ln.r + i * ln.rp, L - 1) * ld);
-  float v[VE], w[VE], b[VE], mean[VE], rs[VE];
-  int gi[VE];
-  ln.groups(s.Cg, gi);
-  ln.k.load_f32(p.w ? p.w + blk.c0 : nullptr, 1.f, w);
-  ln.k.load_f32(p.b ? p.b + blk.c0 : nullptr, 0.f, b);
-  const float all = (float)L * (float)s.Cg;
-#pragma unroll
-  for (int e = 0; e < VE; ++e) v[e] = 0.f;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    float a[VE];
-    ln.k.unpack(x[i], a);
-    const bool in = ln.on && ln.r + i * ln.rp < L;
-#pragma unroll
-    for (int e = 0; e < VE; ++e) v[e] += in ? a[e] : 0.f;
-  }
-  gn_columns(ln, blk.cb, v, cols);
-  gn_teams(s, blk, cols, sums);
-#pragma unroll
-  for (int e = 0; e < VE; ++e) {
-    mean[e] = sums[min(gi[e], blk.ng - 1)] / all;
-    v[e] = 0.f;
-  }
-  gn_packed(x);
-  const float m = (int)threadIdx.x < blk.ng ? sums[threadIdx.x] / all : 0.f;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    float a[VE];
-    ln.k.unpack(x[i], a);
-    const bool in = ln.on && ln.r + i * ln.rp < L;
-#pragma unroll
-    for (int e = 0; e < VE; ++e) {
-      const float d = in ? a[e] - mean[e] : 0.f;
-      v[e] = fmaf(d, d, v[e]);
-    }
-  }
-  gn_columns(ln, blk.cb, v, cols);
-  gn_teams(s, blk, cols, sums);
-#pragma unroll
-  for (int e = 0; e < VE; ++e) rs[e] = 1.f / sqrtf(sums[min(gi[e], blk.ng - 1)] / all + p.eps);
-  if ((int)threadIdx.x < blk.ng) {
-    const int64_t g = (int64_t)wg.image * s.G + blk.g0 + threadIdx.x;
-    if (p.mean) p.mean[g] = m;
-    if (p.rstd) p.rstd[g] = 1.f / sqrtf(sums[threadIdx.x] / all + p.eps);
-  }
-  if (!ln.on) return;
-  gn_packed(x);
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    if (ln.r + i * ln.rp >= L) break;
-    float a[VE];
-    ln.k.unpack(x[i], a);
-#pragma unroll
-    for (int e = 0; e < VE; ++e) a[e] = gn_act(fmaf((a[e] - mean[e]) * rs[e], w[e], b[e]), p.act);
-    ln.k.store(p.y + at + (int64_t)(ln.r + i * ln.rp) * ld, a);
-  }
+  });
 }
 
 struct GnBwd {
@@ -406,6 +504,7 @@ struct GnBwd {
   float* wpart;  // [B tiles][2][C]: sums of du xh and du by column, or null
   float *dw, *db;
   int accumulate, act;
+  int64_t sums;  // partial sums of a column
 };
 
 // A lane's constants of an image: its channels' statistics and affine weights.
@@ -415,43 +514,132 @@ struct GnConst {
   float mean[VE], rs[VE], w[VE], b[VE];
   __device__ __forceinline__ GnConst(const GnBwd& p, const GnBlock& blk, const GnLane<DT, TINY>& ln, int image) {
     int gi[VE];
-    ln.groups(p.s.pieces == 1 ? p.s.Cg : blk.cb, gi);
+    ln.groups(p.s, blk, gi);
     ln.k.load_f32(p.w ? p.w + blk.c0 : nullptr, 1.f, w);
     ln.k.load_f32(p.b ? p.b + blk.c0 : nullptr, 0.f, b);
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
-      const int64_t g = (int64_t)image * p.s.G + blk.g0 + min(gi[e], blk.ng - 1);
+      const int64_t g = (int64_t)image * p.s.G + blk.g0 + gi[e];
       mean[e] = p.mean[g];
       rs[e] = p.rstd[g];
     }
   }
   // xh, and du in place of dy
-  __device__ __forceinline__ void apply(float (&x)[VE], float (&dy)[VE], int act) const {
+  template <class A>
+  __device__ __forceinline__ void apply(float (&x)[VE], float (&dy)[VE], A) const {
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
       x[e] = (x[e] - mean[e]) * rs[e];
-      dy[e] *= gn_slope(fmaf(x[e], w[e], b[e]), act);
+      dy[e] *= A::slope(fmaf(x[e], w[e], b[e]));
     }
   }
 };
 
-// The sums of a tile's (or a whole image's, in one work-group) columns to memory, and
-// the groups' sums of t and t xh into LDS.
+// A work-group's sums of its columns (v, used up) to memory, and the groups' sums of those
+// times the affine weights into sums (ends with a barrier).
 template <int DT, bool TINY>
-__device__ __forceinline__ void gn_bwd_sums(const GnBwd& p, const GnBlock& blk, const GnLane<DT, TINY>& ln,
-                                            const float (&sx)[Ln<DT>::VE], const float (&sd)[Ln<DT>::VE], float* out_w,
-                                            float* out_b, int add, float* cols, float* s1, float* s2) {
-  for (int k = 0; k < 2; ++k) {
-    gn_columns(ln, blk.cb, k ? sd : sx, cols);
-    float* out = k ? out_b : out_w;
+__device__ __forceinline__ void gn_bwd_column_sums(const GnBwd& p, const GnBlock& blk, float (&v)[Ln<DT>::VE], float* out,
+                                                   int add, float* cols, float* sums) {
+  const GnShape& s = p.s;
+  gn_put<DT>(s, v, cols);
+  __syncthreads();
+  if (out)
     for (int c = threadIdx.x; c < blk.cb; c += blockDim.x) {
-      const float a = cols[c];
-      if (out) out[blk.c0 + c] = add ? out[blk.c0 + c] + a : a;
-      cols[c] = p.w ? a * p.w[blk.c0 + c] : a;
+      const float a = gn_column<DT, TINY>(s, blk.cb, c, cols);
+      out[blk.c0 + c] = add ? out[blk.c0 + c] + a : a;
     }
-    __syncthreads();
-    gn_teams(p.s, blk, cols, k ? s1 : s2);
+  const int g = threadIdx.x >> s.tshift, i = threadIdx.x & (s.team - 1);
+  float a = 0.f;
+  if (g < blk.ng)
+    for (int c = i; c < blk.width; c += s.team)
+      a = fmaf(gn_column<DT, TINY>(s, blk.cb, g * blk.width + c, cols), p.w ? p.w[blk.c0 + g * blk.width + c] : 1.f, a);
+  a = gn_team_sum(a, s.team);
+  if (g < blk.ng && i == 0) sums[g] = a;
+  __syncthreads();
+}
+// Both of a backward pass: sx of du xh, sd of du; the groups' sums of t into s1, of t xh into s2.
+template <int DT, bool TINY>
+__device__ __forceinline__ void gn_bwd_sums(const GnBwd& p, const GnBlock& blk, float (&sx)[Ln<DT>::VE],
+                                            float (&sd)[Ln<DT>::VE], float* out_w, float* out_b, int add, float* cols,
+                                            float* s1, float* s2) {
+  gn_bwd_column_sums<DT, TINY>(p, blk, sx, out_w, add, cols, s2);
+  gn_bwd_column_sums<DT, TINY>(p, blk, sd, out_b, add, cols, s1);
+}
+
+// An image's block whole, as the forward pass's. With one image dw and db are its sums.
+template <int DT, int NV>
+__global__ void __launch_bounds__(kGnImage) gn_bwd_image_kernel(GnBwd p) {
+  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES;
+  __shared__ float cols[kGnImage * VE], s1[kGnImage], s2[kGnImage];
+  const GnShape& s = p.s;
+  const GnAt wg(s, blockIdx.x, false);
+  const GnBlock blk(s, wg.block);
+  const GnLane<DT, false> ln(s, blk.cb);
+  const int64_t ld = (int64_t)s.C * ES, at = (int64_t)wg.image * s.L * ld + (int64_t)blk.c0 * ES;
+  const int L = (int)s.L;
+  u32x4 vx[NV], vy[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int64_t o = at + (int64_t)min(ln.r + i * ln.rp, L - 1) * ld + ln.k.c * ES;
+    vx[i] = gn_load(p.x + o);
+    vy[i] = gn_load(p.dy + o);
   }
+  const GnConst<DT, false> c(p, blk, ln, wg.image);
+  float sx[VE], sd[VE];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) sx[e] = sd[e] = 0.f;
+  gn_by_act(p.act, [&](auto act) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float x[VE], dy[VE];
+      Ln<DT>::unpack(gn_vec(vx[i]), x);
+      Ln<DT>::unpack(gn_vec(vy[i]), dy);
+      c.apply(x, dy, act);
+      const bool in = ln.r + i * ln.rp < L;
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        sx[e] = in ? fmaf(dy[e], x[e], sx[e]) : sx[e];
+        sd[e] += in ? dy[e] : 0.f;
+      }
+      gn_next();
+    }
+  });
+  gn_packed(vx);
+  gn_packed(vy);
+  float* out = p.wpart ? p.wpart + (int64_t)wg.image * 2 * s.C : nullptr;
+  gn_bwd_sums<DT, false>(p, blk, sx, sd, out ? out : p.dw, out ? out + s.C : p.db, out ? 0 : p.accumulate, cols, s1, s2);
+  if (!p.dx || ln.k.skip == VE) return;
+  int gi[VE];
+  ln.groups(s, blk, gi);
+  const float inv = 1.f / ((float)L * (float)s.Cg);
+  float m1[VE], m2[VE];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) {
+    m1[e] = s1[gi[e]] * inv;
+    m2[e] = s2[gi[e]] * inv;
+  }
+  gn_by_act(p.act, [&](auto act) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (ln.r + i * ln.rp < L) {
+        const int64_t o = at + (int64_t)(ln.r + i * ln.rp) * ld;
+        float x[VE], dy[VE];
+        Ln<DT>::unpack(gn_vec(vx[i]), x);
+        Ln<DT>::unpack(gn_vec(vy[i]), dy);
+        c.apply(x, dy, act);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) dy[e] = c.rs[e] * (fmaf(dy[e], c.w[e], -m1[e]) - x[e] * m2[e]);
+        if (p.dres) {
+          float z[VE];
+          Ln<DT>::unpack(ln.k.load(p.dres + o), z);
+#pragma unroll
+          for (int e = 0; e < VE; ++e) dy[e] += z[e];
+        }
+        ln.k.store(p.dx + o, dy);
+      }
+      gn_next();
+    }
+  });
 }
 
 template <int DT, bool TINY>
@@ -461,42 +649,45 @@ __global__ void __launch_bounds__(kGnThreads) gn_bwd_sums_kernel(GnBwd p) {
   const GnShape& s = p.s;
   const GnAt wg(s, blockIdx.x, false);
   const GnBlock blk(s, wg.block);
-  const GnLane<DT, TINY> ln(blk.cb);
-  const int64_t first = (int64_t)wg.tile * s.R, end = min(first + s.R, s.L), ld = (int64_t)s.C * ES;
-  const int rows = (int)(end - first);
-  const int64_t at = ((int64_t)wg.image * s.L + first) * ld + (int64_t)blk.c0 * ES;
+  const GnLane<DT, TINY> ln(s, blk.cb);
+  const GnTiles tiles(s, ln.rp);
+  const int64_t ld = (int64_t)s.C * ES, step = (int64_t)ln.rp * s.tiles * ld;
+  const int n = tiles.rows_of(wg.tile, ln.r, ln.rp);
+  const int64_t at = ((int64_t)wg.image * s.L + (int64_t)ln.rp * wg.tile + ln.r) * ld + (int64_t)blk.c0 * ES;
   float sx[VE], sd[VE];
 #pragma unroll
   for (int e = 0; e < VE; ++e) sx[e] = sd[e] = 0.f;
-  if (ln.on && ln.r < rows) {
+  if (n > 0) {
     const GnConst<DT, TINY> c(p, blk, ln, wg.image);
-    const int n = (rows - ln.r + ln.rp - 1) / ln.rp;
-    for (int i = 0; i < n; i += U) {
-      Vec16 vx[U], vy[U];
+    gn_by_act(p.act, [&](auto act) {
+      for (int i = 0; i < n; i += U) {
+        Vec16 vx[U], vy[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t o = at + (int64_t)(ln.r + min(i + u, n - 1) * ln.rp) * ld;
-        vx[u] = ln.k.load(p.x + o);
-        vy[u] = ln.k.load(p.dy + o);
-      }
+        for (int u = 0; u < U; ++u) {
+          const int64_t o = at + min(i + u, n - 1) * step;
+          vx[u] = ln.k.load(p.x + o);
+          vy[u] = ln.k.load(p.dy + o);
+        }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (i + u >= n) break;
-        float x[VE], dy[VE];
-        Ln<DT>::unpack(vx[u], x);
-        ln.k.unpack(vy[u], dy);
-        c.apply(x, dy, p.act);
+        for (int u = 0; u < U; ++u) {
+          if (i + u < n) {
+            float x[VE], dy[VE];
+            Ln<DT>::unpack(vx[u], x);
+            Ln<DT>::unpack(vy[u], dy);
+            c.apply(x, dy, act);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-          sx[e] = fmaf(dy[e], x[e], sx[e]);
-          sd[e] += dy[e];
+            for (int e = 0; e < VE; ++e) {
+              sx[e] = fmaf(dy[e], x[e], sx[e]);
+              sd[e] += dy[e];
+            }
+          }
         }
       }
-    }
+    });
   }
   const int64_t tile = (int64_t)wg.image * s.tiles + wg.tile;
   float* out = p.wpart ? p.wpart + tile * 2 * s.C : nullptr;
-  gn_bwd_sums(p, blk, ln, sx, sd, out, out ? out + s.C : nullptr, 0, cols, s1, s2);
+  gn_bwd_sums<DT, TINY>(p, blk, sx, sd, out, out ? out + s.C : nullptr, 0, cols, s1, s2);
   if (p.part && (int)threadIdx.x < blk.ng)
     p.part[(tile * s.pieces + blk.piece) * s.G + blk.g0 + threadIdx.x] = float2{s1[threadIdx.x], s2[threadIdx.x]};
 }
@@ -522,7 +713,7 @@ __device__ __forceinline__ void gn_reduce(const GnBwd& p, int64_t n, int at) {
     if (out) out[o] = p.accumulate ? out[o] + a : a;
   }
 }
-__global__ void __launch_bounds__(kGnThreads) gn_reduce_kernel(GnBwd p, int64_t n) { gn_reduce(p, n, blockIdx.x); }
+__global__ void __launch_bounds__(kGnThreads) gn_reduce_kernel(GnBwd p) { gn_reduce(p, p.sums, blockIdx.x); }
 
 template <int DT, bool TINY>
 __global__ void __launch_bounds__(kGnThreads) gn_bwd_rows_kernel(GnBwd p) {
@@ -530,13 +721,29 @@ __global__ void __launch_bounds__(kGnThreads) gn_bwd_rows_kernel(GnBwd p) {
   __shared__ float s1[kGnThreads], s2[kGnThreads];
   const GnShape& s = p.s;
   const unsigned tiles = (unsigned)s.B * s.tiles * s.blocks;
-  if (blockIdx.x >= tiles) return gn_reduce(p, (int64_t)s.B * s.tiles, (int)(blockIdx.x - tiles));  // (behind the rows)
+  if (blockIdx.x >= tiles) return gn_reduce(p, p.sums, (int)(blockIdx.x - tiles));  // (behind the rows)
   const GnAt wg(s, blockIdx.x, true);
   const GnBlock blk(s, wg.block);
-  const GnLane<DT, TINY> ln(blk.cb);
+  const GnLane<DT, TINY> ln(s, blk.cb);
+  const GnTiles at_tiles(s, ln.rp);
+  const int64_t ld = (int64_t)s.C * ES, step = (int64_t)ln.rp * s.tiles * ld;
+  const int n = at_tiles.rows_of(wg.tile, ln.r, ln.rp);
+  const int64_t at = ((int64_t)wg.image * s.L + (int64_t)ln.rp * wg.tile + ln.r) * ld + (int64_t)blk.c0 * ES;
+  // the first rows are on their way while the sums are put together
+  Vec16 vx[U], vy[U], vr[U];
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t o = at + min(i + u, n - 1) * step;
+      vx[u] = ln.k.load(p.x + o);
+      vy[u] = ln.k.load(p.dy + o);
+      if (p.dres) vr[u] = ln.k.load(p.dres + o);
+    }
+  };
+  if (n > 0) fetch(0);
   const float all = (float)(int)s.L * (float)s.Cg;
   {
-    const int g = threadIdx.x / s.team, i = threadIdx.x - g * s.team, entries = s.tiles * s.pieces;
+    const int g = threadIdx.x >> s.tshift, i = threadIdx.x & (s.team - 1), entries = s.tiles * s.pieces;
     float a = 0.f, b = 0.f;
     if (g < blk.ng) {
       const float2* q = p.part + (int64_t)wg.image * entries * s.G + blk.g0 + g;
@@ -547,128 +754,47 @@ __global__ void __launch_bounds__(kGnThreads) gn_bwd_rows_kernel(GnBwd p) {
         b += v.y;
       }
     }
-    for (int o = 1; o < s.team; o <<= 1) {
-      a += __shfl_xor(a, o, kWave);
-      b += __shfl_xor(b, o, kWave);
-    }
+    a = gn_team_sum(a, s.team);
+    b = gn_team_sum(b, s.team);
     if (g < blk.ng && i == 0) {
       s1[g] = a / all;
       s2[g] = b / all;
     }
     __syncthreads();
   }
-  const int64_t first = (int64_t)wg.tile * s.R, end = min(first + s.R, s.L), ld = (int64_t)s.C * ES;
-  const int rows = (int)(end - first);
-  if (!ln.on || ln.r >= rows) return;
-  const int64_t at = ((int64_t)wg.image * s.L + first) * ld + (int64_t)blk.c0 * ES;
+  if (ln.k.skip == VE || n <= 0) return;
   const GnConst<DT, TINY> c(p, blk, ln, wg.image);
   int gi[VE];
-  ln.groups(s.pieces == 1 ? s.Cg : blk.cb, gi);
+  ln.groups(s, blk, gi);
   float m1[VE], m2[VE];
 #pragma unroll
   for (int e = 0; e < VE; ++e) {
-    const int g = min(gi[e], blk.ng - 1);
-    m1[e] = s1[g];
-    m2[e] = s2[g];
+    m1[e] = s1[gi[e]];
+    m2[e] = s2[gi[e]];
   }
-  const int n = (rows - ln.r + ln.rp - 1) / ln.rp;
-  for (int i = 0; i < n; i += U) {
-    Vec16 vx[U], vy[U], vr[U];
+  gn_by_act(p.act, [&](auto act) {
+    for (int i = 0; i < n; i += U) {
+      if (i) fetch(i);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t o = at + (int64_t)(ln.r + min(i + u, n - 1) * ln.rp) * ld;
-      vx[u] = ln.k.load(p.x + o);
-      vy[u] = ln.k.load(p.dy + o);
-      if (p.dres) vr[u] = ln.k.load(p.dres + o);
-    }
+      for (int u = 0; u < U; ++u) {
+        if (i + u < n) {
+          float x[VE], dy[VE];
+          Ln<DT>::unpack(vx[u], x);
+          Ln<DT>::unpack(vy[u], dy);
+          c.apply(x, dy, act);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i + u >= n) break;
-      float x[VE], dy[VE];
-      Ln<DT>::unpack(vx[u], x);
-      ln.k.unpack(vy[u], dy);
-      c.apply(x, dy, p.act);
+          for (int e = 0; e < VE; ++e) dy[e] = c.rs[e] * (fmaf(dy[e], c.w[e], -m1[e]) - x[e] * m2[e]);
+          if (p.dres) {
+            float z[VE];
+            Ln<DT>::unpack(vr[u], z);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) dy[e] = c.rs[e] * (fmaf(dy[e], c.w[e], -m1[e]) - x[e] * m2[e]);
-      if (p.dres) {
-        float z[VE];
-        Ln<DT>::unpack(vr[u], z);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) dy[e] += z[e];
+            for (int e = 0; e < VE; ++e) dy[e] += z[e];
+          }
+          ln.k.store(p.dx + at + (i + u) * step, dy);
+        }
       }
-      ln.k.store(p.dx + at + (int64_t)(ln.r + (i + u) * ln.rp) * ld, dy);
     }
-  }
-}
-
-// An image's block whole, as the forward pass's. With one image dw and db are its sums.
-template <int DT, int NV>
-__global__ void __launch_bounds__(kGnSlab) gn_bwd_slab_kernel(GnBwd p) {
-  constexpr int VE = Ln<DT>::VE, ES = Ln<DT>::ES;
-  __shared__ float cols[kGnSlab * VE], s1[kGnSlab], s2[kGnSlab];
-  const GnShape& s = p.s;
-  const GnAt wg(s, blockIdx.x, false);
-  const GnBlock blk(s, wg.block);
-  const GnLane<DT, false> ln(blk.cb);
-  const int64_t ld = (int64_t)s.C * ES, at = (int64_t)wg.image * s.L * ld + (int64_t)blk.c0 * ES;
-  const int L = (int)s.L;
-  Vec16 vx[NV], vy[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int64_t o = at + (int64_t)min(ln.r + i * ln.rp, L - 1) * ld;
-    vx[i] = ln.k.load(p.x + o);
-    vy[i] = ln.k.load(p.dy + o);
-  }
-  const GnConst<DT, false> c(p, blk, ln, wg.image);
-  float sx[VE], sd[VE];
-#pragma unroll
-  for (int e = 0; e < VE; ++e) sx[e] = sd[e] = 0.f;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    float x[VE], dy[VE];
-    Ln<DT>::unpack(vx[i], x);
-    ln.k.unpack(vy[i], dy);
-    c.apply(x, dy, p.act);
-    const bool in = ln.on && ln.r + i * ln.rp < L;
-#pragma unroll
-    for (int e = 0; e < VE; ++e) {
-      sx[e] += in ? dy[e] * x[e] : 0.f;
-      sd[e] += in ? dy[e] : 0.f;
-    }
-  }
-  float* out = p.wpart ? p.wpart + (int64_t)wg.image * 2 * s.C : nullptr;
-  gn_bwd_sums(p, blk, ln, sx, sd, out ? out : p.dw, out ? out + s.C : p.db, out ? 0 : p.accumulate, cols, s1, s2);
-  if (!ln.on || !p.dx) return;
-  gn_packed(vx);
-  gn_packed(vy);
-  int gi[VE];
-  ln.groups(s.Cg, gi);
-  const float all = (float)L * (float)s.Cg;
-  float m1[VE], m2[VE];
-#pragma unroll
-  for (int e = 0; e < VE; ++e) {
-    const int g = min(gi[e], blk.ng - 1);
-    m1[e] = s1[g] / all;
-    m2[e] = s2[g] / all;
-  }
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    if (ln.r + i * ln.rp >= L) break;
-    const int64_t o = at + (int64_t)(ln.r + i * ln.rp) * ld;
-    float x[VE], dy[VE];
-    Ln<DT>::unpack(vx[i], x);
-    ln.k.unpack(vy[i], dy);
-    c.apply(x, dy, p.act);
-#pragma unroll
-    for (int e = 0; e < VE; ++e) dy[e] = c.rs[e] * (fmaf(dy[e], c.w[e], -m1[e]) - x[e] * m2[e]);
-    if (p.dres) {
-      float z[VE];
-      Ln<DT>::unpack(ln.k.load(p.dres + o), z);
-#pragma unroll
-      for (int e = 0; e < VE; ++e) dy[e] += z[e];
-    }
-    ln.k.store(p.dx + o, dy);
-  }
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -684,6 +810,11 @@ struct GnPlan {
 };
 
 static int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+static int pow2_from(int64_t n) {
+  int p = 1;
+  while (p < n) p *= 2;
+  return p;
+}
 
 // kg groups per block, the last block at least a vector wide.
 static void gn_blocks(GnShape* s, int64_t kg, int VE) {
@@ -695,31 +826,45 @@ static void gn_blocks(GnShape* s, int64_t kg, int VE) {
   s->pw = s->Cg;
   s->blocks = (int)up(s->G, kg);
 }
-static void gn_team(GnShape* s, int threads) {
+static void gn_lanes(GnShape* s, int threads, int VE) {
   const int width = s->pieces == 1 ? s->Cg : s->pw;
+  s->nl = pow2_from(up((int64_t)s->kg * width, VE));
+  s->shift = 0;
+  while (1 << s->shift < s->nl) ++s->shift;
   s->team = 1;
-  while (s->team < 64 && s->team < width && s->team * 2 * s->kg <= threads) s->team *= 2;
+  s->tshift = 0;
+  while (s->team < 64 && s->team < width && s->team * 2 * s->kg <= threads) {
+    s->team *= 2;
+    ++s->tshift;
+  }
+  s->inv_width = 1.f / (float)width;
+  s->inv_pieces = 1.f / (float)s->pieces;
 }
 
-// An image's block as one work-group's: blocks of at least `bytes` per row.
-static bool gn_slab(GnPlan* p, int bytes, int most, int dt) {
+// An image's block in the registers of one work-group, with blocks of 32 bytes per row or
+// more: where the whole batch is small, and a thread has few vectors (4 forward; backward 2,
+// with 4 the registers do not hold them), one launch is sooner than two. Us of launches one
+// after the other, forward and backward, in one / in two: 1 x 64 x 256 fp16 5.7 / 9.4, 5.9 /
+// 11.7; 1 x 256 x 192 8.4 / 9.6, 9.2 / 12.1; 8 x 256 x 384 9.0 / 10.7, 11.7 / 13.4; 1 x 784 x
+// 256 9.3 / 11.0, 11.1 / 12.8; 8 x 784 x 256 10.4 / 11.5, 15.2 / 13.7; 1 x 1600 x 512 11.5 /
+// 11.6, 25.3 / 14.5; 32 x 256 x 384 15.8 / 13.1, 26.2 / 18.5; 256 x 256 x 384 83 / 38, 156 / 66.
+static bool gn_image(GnPlan* p, bool bwd, int dt) {
+  constexpr int bytes = 32;
+  const int most = bwd ? 2 : 4;
+  if ((int64_t)p->s.B * p->s.L > ((int64_t)1 << (bwd ? 20 : 21)) / p->s.C) return false;
   const int VE = dt == GTR_F32 ? 4 : 8, ES = dt == GTR_F32 ? 4 : 2;
   GnShape* s = &p->s;
   gn_blocks(s, up(bytes, (int64_t)s->Cg * ES), VE);
-  const int64_t nl = up((int64_t)s->kg * s->Cg, VE);
-  if (nl > kGnSlab || s->L > (int64_t)kGnSlab * most) return false;
-  int64_t threads = up(s->L * nl, 64) * 64;
-  if (threads < up(s->kg, 64) * 64) threads = up(s->kg, 64) * 64;
-  p->threads = (int)(threads < kGnSlab ? threads : kGnSlab);
-  if (s->kg > p->threads) return false;
-  const int64_t nv = up(s->L, p->threads / nl);
-  if (nv > most) return false;
-  p->NV = nv <= 1 ? 1 : nv <= 2 ? 2 : nv <= 4 ? 4 : nv <= 8 ? 8 : 16;
+  if (s->kg > 64 || (int64_t)s->kg * s->Cg > 64 * VE) return false;
+  gn_lanes(s, kGnImage, VE);
+  const int64_t nl = s->nl;
+  if (s->L > kGnImage / nl * most) return false;
+  p->threads = (int)(s->L * nl >= kGnImage ? kGnImage : up(s->L * nl, 64) * 64);
+  gn_lanes(s, p->threads, VE);
+  p->NV = pow2_from(up(s->L, p->threads / nl));
   s->tiles = 1;
-  s->R = 0;
-  gn_team(s, p->threads);
   p->grid = (int64_t)s->B * s->blocks;
-  return p->grid * p->threads < (int64_t)1 << 32;
+  return p->NV <= most && p->grid * p->threads < (int64_t)1 << 32;
 }
 
 static gtr_status gn_plan(int32_t B, int64_t L, int32_t C, int32_t G, int dt, bool bwd, GnPlan* p) {
@@ -735,98 +880,82 @@ static gtr_status gn_plan(int32_t B, int64_t L, int32_t C, int32_t G, int dt, bo
   s->G = G;
   s->Cg = C / G;
   p->tiny = C < VE;
-  if (!p->tiny)
-    for (int bytes : {128, 64})
-      if (gn_slab(p, bytes, bwd ? 4 : 8, dt)) return GTR_OK;
+  if (!p->tiny && gn_image(p, bwd, dt)) return GTR_OK;
   p->NV = 0;
   p->threads = kGnThreads;
   const int CB = 64 * VE;
   if (s->Cg <= CB) {
     const int kg = CB / s->Cg;
     gn_blocks(s, kg < kGnThreads ? kg : kGnThreads, VE);
+    if ((int64_t)s->kg * s->Cg > CB) gn_blocks(s, kg > 1 ? kg - 1 : 1, VE);
   } else {
     s->kg = 1;
     s->pieces = (int)up(s->Cg, CB);
     s->pw = (int)up(s->Cg, s->pieces);
     s->blocks = s->G * s->pieces;
   }
-  gn_team(s, kGnThreads);
-  const int64_t cb = s->pieces == 1 ? (int64_t)s->kg * s->Cg : s->pw, rp = kGnThreads / up(cb, VE);
-  int64_t tiles = up(2048, (int64_t)B * s->blocks);
-  if (tiles > up(L, rp * 4)) tiles = up(L, rp * 4);
-  if (tiles > 256) tiles = 256;
-  s->R = (int)(up(up(L, tiles), rp) * rp);
-  s->tiles = (int)up(L, s->R);
+  gn_lanes(s, kGnThreads, VE);
+  const int64_t rp = kGnThreads / s->nl;
+  // Up to 8 work-groups per CU and 8 rows per thread or more, for the most part (8 x 1600 x 384
+  // fp16 forward 17.1 us, with 4 rows 21.7; 16 x 16384 x 512 bf16 in 512, 1024, 2048 work-groups
+  // 191, 189, 176, backward of 16 x 4096 x 1024 180, 177, 162).
+  const int64_t chains = (int64_t)B * s->blocks;
+  int64_t tiles = std::min(up(2048, chains), up(L, rp * 8));
+  if (tiles * chains < 256) tiles = std::min(up(256, chains), up(L, rp * 4));
+  s->tiles = (int)std::min<int64_t>(tiles, 256);
   p->grid = (int64_t)B * s->tiles * s->blocks;
   return (p->grid + up(2 * (int64_t)C, 32)) * kGnThreads < (int64_t)1 << 32 ? GTR_OK : GTR_ERR_SHAPE;
 }
 
+// Bytes of workspace: the tiles' sums, and the columns' partial sums.
 static size_t gn_stats_bytes(const GnPlan& p) {
   return p.NV ? 0 : (size_t)up((int64_t)p.s.B * p.s.tiles * p.s.pieces * p.s.G * 8, 256) * 256;
 }
-static size_t gn_weights_bytes(const GnPlan& p) {  // of the columns' partial sums
+static size_t gn_weights_bytes(const GnPlan& p) {
   return p.NV && p.s.B == 1 ? 0 : (size_t)up((int64_t)p.s.B * p.s.tiles * 2 * p.s.C * 4, 256) * 256;
 }
 
-template <int DT>
-static void gn_go(const GnPlan& p, const GnFwd& f, hipStream_t st) {
-  const dim3 g((unsigned)p.grid), t(p.threads);
-  switch (p.NV) {
-    case 0:
-      if (p.tiny) {
-        hipLaunchKernelGGL((gn_fwd_sums_kernel<DT, true>), g, t, 0, st, f);
-        hipLaunchKernelGGL((gn_fwd_rows_kernel<DT, true>), g, t, 0, st, f);
-      } else {
-        hipLaunchKernelGGL((gn_fwd_sums_kernel<DT, false>), g, t, 0, st, f);
-        hipLaunchKernelGGL((gn_fwd_rows_kernel<DT, false>), g, t, 0, st, f);
-      }
-      break;
-    case 1: hipLaunchKernelGGL((gn_fwd_slab_kernel<DT, 1>), g, t, 0, st, f); break;
-    case 2: hipLaunchKernelGGL((gn_fwd_slab_kernel<DT, 2>), g, t, 0, st, f); break;
-    case 4: hipLaunchKernelGGL((gn_fwd_slab_kernel<DT, 4>), g, t, 0, st, f); break;
-    case 8: hipLaunchKernelGGL((gn_fwd_slab_kernel<DT, 8>), g, t, 0, st, f); break;
-    default: hipLaunchKernelGGL((gn_fwd_slab_kernel<DT, 16>), g, t, 0, st, f); break;
-  }
+template <int DT, int NV>
+static void gn_go_image(const GnPlan& p, const GnFwd& f, hipStream_t st) {
+  hipLaunchKernelGGL((gn_fwd_image_kernel<DT, NV>), dim3((unsigned)p.grid), dim3(p.threads), 0, st, f);
 }
-template <int DT>
-static void gn_go(const GnPlan& p, const GnBwd& f, hipStream_t st) {
-  const dim3 g((unsigned)p.grid), t(p.threads);
-  const unsigned sums = f.wpart ? (unsigned)up(2 * (int64_t)p.s.C, 32) : 0;
-  if (p.NV == 0) {
-    const dim3 gr(g.x + sums);
-    if (p.tiny)
-      hipLaunchKernelGGL((gn_bwd_sums_kernel<DT, true>), g, t, 0, st, f);
-    else
-      hipLaunchKernelGGL((gn_bwd_sums_kernel<DT, false>), g, t, 0, st, f);
-    if (f.dx) {
-      if (p.tiny)
-        hipLaunchKernelGGL((gn_bwd_rows_kernel<DT, true>), gr, t, 0, st, f);
-      else
-        hipLaunchKernelGGL((gn_bwd_rows_kernel<DT, false>), gr, t, 0, st, f);
-      return;
-    }
-  } else if (p.NV == 1) {
-    hipLaunchKernelGGL((gn_bwd_slab_kernel<DT, 1>), g, t, 0, st, f);
-  } else if (p.NV == 2) {
-    hipLaunchKernelGGL((gn_bwd_slab_kernel<DT, 2>), g, t, 0, st, f);
-  } else if (p.NV == 4) {
-    hipLaunchKernelGGL((gn_bwd_slab_kernel<DT, 4>), g, t, 0, st, f);
-  } else {
-    hipLaunchKernelGGL((gn_bwd_slab_kernel<DT, 8>), g, t, 0, st, f);
+template <int DT, int NV>
+static void gn_go_image(const GnPlan& p, const GnBwd& f, hipStream_t st) {
+  hipLaunchKernelGGL((gn_bwd_image_kernel<DT, NV>), dim3((unsigned)p.grid), dim3(p.threads), 0, st, f);
+}
+template <int DT, bool TINY>
+static void gn_go_tiles(const GnPlan& p, const GnFwd& f, hipStream_t st) {
+  const dim3 g((unsigned)p.grid), t(kGnThreads);
+  hipLaunchKernelGGL((gn_fwd_sums_kernel<DT, TINY>), g, t, 0, st, f);
+  hipLaunchKernelGGL((gn_fwd_rows_kernel<DT, TINY>), g, t, 0, st, f);
+}
+static unsigned gn_sums_grid(const GnBwd& f) { return f.wpart ? (unsigned)up(2 * (int64_t)f.s.C, 32) : 0; }
+template <int DT, bool TINY>
+static void gn_go_tiles(const GnPlan& p, const GnBwd& f, hipStream_t st) {
+  const dim3 g((unsigned)p.grid), t(kGnThreads);
+  hipLaunchKernelGGL((gn_bwd_sums_kernel<DT, TINY>), g, t, 0, st, f);
+  if (f.dx) hipLaunchKernelGGL((gn_bwd_rows_kernel<DT, TINY>), dim3(g.x + gn_sums_grid(f)), t, 0, st, f);
+}
+template <int DT, class F>
+static void gn_go(const GnPlan& p, const F& f, hipStream_t st) {
+  switch (p.NV) {
+    case 0: return p.tiny ? gn_go_tiles<DT, true>(p, f, st) : gn_go_tiles<DT, false>(p, f, st);
+    case 1: return gn_go_image<DT, 1>(p, f, st);
+    case 2: return gn_go_image<DT, 2>(p, f, st);
+    default:
+      if constexpr (std::is_same<F, GnFwd>::value) gn_go_image<DT, 4>(p, f, st);
   }
-  if (sums)
-    hipLaunchKernelGGL(gn_reduce_kernel, dim3(sums), dim3(kGnThreads), 0, st, f, (int64_t)p.s.B * p.s.tiles);
 }
 template <class F>
-static gtr_status gn_launch(int dt, const GnPlan& p, const F& f, hipStream_t st) {
+static void gn_launch(int dt, const GnPlan& p, const F& f, hipStream_t st) {
   if (dt == GTR_F32)
     gn_go<GTR_F32>(p, f, st);
   else if (dt == GTR_F16)
     gn_go<GTR_F16>(p, f, st);
   else
     gn_go<GTR_BF16>(p, f, st);
-  return hipGetLastError() == hipSuccess ? GTR_OK : GTR_ERR_HIP;
 }
+static gtr_status gn_launched() { return hipGetLastError() == hipSuccess ? GTR_OK : GTR_ERR_HIP; }
 
 static bool gn_misaligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
 static bool gn_act_ok(int act) { return act == GTR_ACT_SILU || act == GTR_ACT_GELU || act == GTR_ACT_NONE; }
@@ -875,7 +1004,8 @@ extern "C" gtr_status gtr_groupnorm_fwd(const gtr_groupnorm_fwd_args* a, hipStre
   }
   const GnFwd f = {p.s, static_cast<const char*>(a->x), a->w, a->b, static_cast<char*>(a->y), a->mean, a->rstd,
                    static_cast<float2*>(a->workspace), a->eps, a->act};
-  return gn_launch(a->dtype, p, f, stream);
+  gn_launch(a->dtype, p, f, stream);
+  return gn_launched();
 }
 
 extern "C" size_t gtr_groupnorm_bwd_workspace_size(const gtr_groupnorm_bwd_args* a) {
@@ -910,6 +1040,11 @@ extern "C" gtr_status gtr_groupnorm_bwd(const gtr_groupnorm_bwd_args* a, hipStre
   char* ws = static_cast<char*>(a->workspace);
   const GnBwd f = {p.s, static_cast<const char*>(a->dy), static_cast<const char*>(a->x), a->mean, a->rstd, a->w, a->b,
                    static_cast<const char*>(a->dres), static_cast<char*>(a->dx), stat ? reinterpret_cast<float2*>(ws) : nullptr,
-                   sums ? reinterpret_cast<float*>(ws + stat) : nullptr, a->dw, a->db, a->accumulate, a->act};
-  return gn_launch(a->dtype, p, f, stream);
+                   sums ? reinterpret_cast<float*>(ws + stat) : nullptr, a->dw, a->db, a->accumulate, a->act,
+                   (int64_t)p.s.B * p.s.tiles};
+  gn_launch(a->dtype, p, f, stream);
+  // the columns' sums, where they are not the rows' launch's
+  if (f.wpart && (p.NV || !f.dx))
+    hipLaunchKernelGGL(gn_reduce_kernel, dim3(gn_sums_grid(f)), dim3(kGnThreads), 0, stream, f);
+  return gn_launched();
 }

@@ -1488,7 +1488,9 @@ def dpp_src(w, i, tok):
         idx = (LANES // 8) * 8 + 7 - LANES % 8
     elif 'row_mirror' in i.mods:
         idx = (LANES // 16) * 16 + 15 - LANES % 16
-    elif 'row_bcast' in i.mods or 'wave_shr' in i.mods or 'row_ror' in i.mods:
+    elif 'row_ror' in i.mods:
+        idx = (LANES // 16) * 16 + (LANES - int(i.mods['row_ror'], 0)) % 16
+    elif 'row_bcast' in i.mods or 'wave_shr' in i.mods:
         raise NotImplementedError(f"dpp {i.mods}")
     valid = valid & act[idx]
     v = src.v[idx].copy()

@@ -4,10 +4,20 @@ import struct
 
 import pytest
 
+import test_training_codegen_cpu as training
 from test_recurrence_codegen_cpu import check_waves
-from test_training_codegen_cpu import Buffers, kernel_named, listing
+from test_training_codegen_cpu import Buffers, emu, kernel_named, listing
+
+emu.HANDLERS["v_permlane32_swap_b32_e32"] = training._swap
 
 up = lambda a, b: -(-a // b)
+
+
+def pow2(n):
+    p = 1
+    while p < n:
+        p *= 2
+    return p
 
 
 def blocks(G, Cg, kg, VE):
@@ -17,41 +27,44 @@ def blocks(G, Cg, kg, VE):
     return kg, 1, Cg, up(G, kg)
 
 
-def team(width, kg, threads):
-    t = 1
-    while t < 64 and t < width and t * 2 * kg <= threads:
-        t *= 2
-    return t
+def lanes(p, threads, VE):
+    width = p["pw"]
+    p["nl"] = pow2(up(p["kg"] * width, VE))
+    p["team"] = 1
+    while p["team"] < 64 and p["team"] < width and p["team"] * 2 * p["kg"] <= threads:
+        p["team"] *= 2
+    return threads // p["nl"]
 
 
 def tiles_plan(B, L, C, G, dt, tiles):
     """Two launches: as groupnorm.hip lays out its blocks, with the tiles given."""
     VE, Cg, CB = (4 if dt == 0 else 8), C // G, 64 * (4 if dt == 0 else 8)
+    p = {}
     if Cg <= CB:
-        kg, pieces, pw, nb = blocks(G, Cg, min(256, CB // Cg), VE)
+        p["kg"], p["pieces"], p["pw"], p["blocks"] = blocks(G, Cg, min(256, CB // Cg), VE)
     else:
-        kg, pieces = 1, up(Cg, CB)
-        pw, nb = up(Cg, pieces), G * pieces
-    rp = 256 // up(kg * Cg if pieces == 1 else pw, VE)
-    R = up(up(L, tiles), rp) * rp
-    return dict(kg=kg, pieces=pieces, pw=pw, blocks=nb, tiles=up(L, R), R=R, team=team(Cg if pieces == 1 else pw, kg, 256),
-                threads=256, NV=0)
+        p["kg"], p["pieces"] = 1, up(Cg, CB)
+        p["pw"], p["blocks"] = up(Cg, p["pieces"]), G * p["pieces"]
+    lanes(p, 256, VE)
+    p["tiles"] = tiles
+    return p
 
 
-def slab_plan(B, L, C, G, dt, row_bytes, most):
-    VE, ES, Cg = (4, 4, C // G) if dt == 0 else (8, 2, C // G)
-    kg, pieces, pw, nb = blocks(G, Cg, up(row_bytes, Cg * ES), VE)
-    nl = up(kg * Cg, VE)
-    threads = min(1024, max(up(L * nl, 64), up(kg, 64)) * 64)
-    nv = up(L, threads // nl)
-    assert nv <= most
-    return dict(kg=kg, pieces=pieces, pw=pw, blocks=nb, tiles=1, R=0, team=team(Cg, kg, threads), threads=threads,
-                NV=next(v for v in (1, 2, 4, 8, 16) if v >= nv))
+def image_plan(L, C, G, dt, row_bytes):
+    """An image's block in the registers of a work-group."""
+    VE, ES, Cg, p = (4 if dt == 0 else 8), (4 if dt == 0 else 2), C // G, {}
+    p["kg"], p["pieces"], p["pw"], p["blocks"] = blocks(G, Cg, up(row_bytes, Cg * ES), VE)
+    lanes(p, 1024, VE)
+    p["threads"] = 1024 if L * p["nl"] >= 1024 else up(L * p["nl"], 64) * 64
+    p["NV"] = pow2(up(L, lanes(p, p["threads"], VE)))
+    p["tiles"] = 1
+    return p
 
 
 def shape(B, L, C, G, p):
-    return struct.pack("<qiiiiiiiiiii4x", L, B, C, G, C // G, p["kg"], p["pieces"], p["pw"], p["blocks"], p["tiles"], p["R"],
-                       p["team"])
+    return struct.pack("<qiiiiiiiiiiiiiff4x", L, B, C, G, C // G, p["kg"], p["pieces"], p["pw"], p["blocks"], p["nl"],
+                       p["nl"].bit_length() - 1, p["tiles"], p["team"], p["team"].bit_length() - 1, 1 / p["pw"],
+                       1 / p["pieces"])
 
 
 def run(text, name, kern, new, grid, threads):
@@ -83,32 +96,34 @@ def test_tiles(B, L, C, G, dt, tiles, act):
     dy, dres, dx = new("dy", n, "r"), new("dres", n, "r"), new("dx", n, "w")
     wpart = new("wpart", B * p["tiles"] * 2 * C * 4, "rw")
     dw, db = new("dw", C * 4, "rw"), new("db", C * 4, "rw")
-    kern = shape(B, L, C, G, p) + struct.pack("<QQQQQQQQQQQQii", dy, x, mean, rstd, w, b, dres, dx, part, wpart, dw, db, 1, act)
+    kern = shape(B, L, C, G, p) + struct.pack("<QQQQQQQQQQQQiiq", dy, x, mean, rstd, w, b, dres, dx, part, wpart, dw, db, 1,
+                                              act, B * p["tiles"])
     run(text, kernel_named(text, f"gn_bwd_sums_kernelILi{dt}ELb{tiny}E"), kern, new, grid, 256)
     run(text, kernel_named(text, f"gn_bwd_rows_kernelILi{dt}ELb{tiny}E"), kern, new, grid + up(2 * C, 32), 256)
-    run(text, kernel_named(text, "gn_reduce_kernel"), kern + struct.pack("<q", B * p["tiles"]), new, up(2 * C, 32), 256)
+    run(text, kernel_named(text, "gn_reduce_kernel"), kern, new, up(2 * C, 32), 256)
 
 
-# one token; all of a wave's, a work-group's threads; one to all vectors per thread; broken vectors and groups
-SLABS = [(2, 1, 64, 4, 1, 64, 8), (1, 49, 100, 5, 2, 64, 8), (2, 300, 33, 33, 0, 64, 8), (1, 1600, 40, 5, 1, 64, 16),
-         (1, 700, 192, 32, 1, 128, 8)]
+# images, tokens, channels, groups, type, bytes per row: one token; part of a wave's, all of a work-group's threads; one
+# to all vectors per thread; broken vectors and groups
+IMAGES = [(2, 1, 64, 4, 1, 32), (1, 49, 100, 5, 2, 32), (2, 300, 33, 33, 0, 32), (1, 700, 40, 5, 1, 32),
+          (1, 1950, 192, 12, 1, 32), (2, 333, 72, 9, 0, 128)]
 
 
-@pytest.mark.parametrize("B,L,C,G,dt,row_bytes,most", SLABS)
-def test_slabs(B, L, C, G, dt, row_bytes, most):
+@pytest.mark.parametrize("B,L,C,G,dt,row_bytes", IMAGES)
+def test_images(B, L, C, G, dt, row_bytes):
     text, es = listing("groupnorm.hip"), (4 if dt == 0 else 2)
-    p = slab_plan(B, L, C, G, dt, row_bytes, most)
+    p = image_plan(L, C, G, dt, row_bytes)
     grid, n = B * p["blocks"], B * L * C * es
     new = Buffers()
     x, w, b, y = new("x", n, "r"), new("w", C * 4, "r"), new("b", C * 4, "r"), new("y", n, "w")
     mean, rstd = new("mean", B * G * 4, "rw"), new("rstd", B * G * 4, "rw")
     kern = shape(B, L, C, G, p) + struct.pack("<QQQQQQQfi", x, w, b, y, mean, rstd, 0, 1e-5, 0)
-    run(text, kernel_named(text, f"gn_fwd_slab_kernelILi{dt}ELi{p['NV']}E"), kern, new, grid, p["threads"])
-    if p["NV"] > 8:
+    run(text, kernel_named(text, f"gn_fwd_image_kernelILi{dt}ELi{p['NV']}E"), kern, new, grid, p["threads"])
+    if p["NV"] > 2:
         return
     dy, dres, dx = new("dy", n, "r"), new("dres", n, "r"), new("dx", n, "w")
     wpart = new("wpart", B * 2 * C * 4, "rw")
     dw, db = new("dw", C * 4, "rw"), new("db", C * 4, "rw")
-    kern = shape(B, L, C, G, p) + struct.pack("<QQQQQQQQQQQQii", dy, x, mean, rstd, w, b, dres, dx, 0, wpart if B > 1 else 0,
-                                              dw, db, 1, 1)
-    run(text, kernel_named(text, f"gn_bwd_slab_kernelILi{dt}ELi{p['NV']}E"), kern, new, grid, p["threads"])
+    kern = shape(B, L, C, G, p) + struct.pack("<QQQQQQQQQQQQiiq", dy, x, mean, rstd, w, b, dres, dx, 0, wpart if B > 1 else 0,
+                                              dw, db, 1, 1, B)
+    run(text, kernel_named(text, f"gn_bwd_image_kernelILi{dt}ELi{p['NV']}E"), kern, new, grid, p["threads"])

@@ -1,9 +1,9 @@
 """gtr_groupnorm_fwd and gtr_groupnorm_bwd on the GPU against the formulas in 64 bits.
 
 Tolerances, per element, from the kernels' arithmetic (e = 2^-24, the rounding of a float32 operation; u, half a step of
-the output type). No sum goes through more than S = 330 + L / 256 additions one after the other (rows of a lane, at most
-16 or, in tiles, L / 256 and 4; 8 of a column's slices and 256 of a group's channels in the rest; at most 256 tiles),
-n = 16 + L / 256 of them a lane's own. D is the largest |x - mean| of a group, A its largest |x|:
+the output type). No sum goes through more than S = 330 + L / 256 additions one after the other (a lane's rows, at most
+n = 16 + L / 256 at these sizes; 16 waves, 8 channels of a team's thread and 6 steps across its threads; at most 256
+tiles). D is the largest |x - mean| of a group, A its largest |x|:
 * mean: S e (2 D + mean |x|) + 2 e A (sums about one of the values, which is at most 2 D from any);
 * var, relative: (S + 2 n^2) e (a lane's sum of squares about one of its n values is at most 2 (n + 1) times that about
   their mean) + 8 (e A + 2 n e D) rstd (the lanes' means against the group's) + (mean's error rstd)^2; rstd: half of it
