@@ -1104,6 +1104,12 @@ def _row_stride(name: str, t: torch.Tensor, shape, dtypes, dev: torch.device) ->
     raise ValueError(f"{name} has dtype {t.dtype}, expected one of {list(dtypes)}")
 
 
+def _gates(g: torch.Tensor, shape, dt: torch.dtype, index: int) -> bool:
+    """Whether g is contiguous gates for rows of this shape and type (what _row_stride explains where it is not)."""
+    return (g.shape == shape and (g.dtype is dt or g.dtype is torch.float32) and g.get_device() == index and
+            g.is_contiguous())
+
+
 def _rec_shape(name, t, H, W, scan, gate_tau) -> torch.Size:
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
@@ -1138,9 +1144,9 @@ def gtr_recurrence_fwd(x: torch.Tensor, g: torch.Tensor, *, H: int, W: int, scan
 
 def _recurrence_fwd(x, g, H, W, scan, gate_tau, complement, h0, want_final, h, last, workspace, spin):
     shape, dev, dt, f32 = x.shape, x.device, x.dtype, torch.float32
-    x_ld = _row_stride("x", x, shape, (dt,), dev)
-    g_ld = _row_stride("g", g, shape, (dt, f32), dev)
     state, index = (shape[0], shape[2]), dev.index
+    x_ld = 0 if x.is_contiguous() else _row_stride("x", x, shape, (dt,), dev)
+    g_ld = 0 if _gates(g, shape, dt, index) else _row_stride("g", g, shape, (dt, f32), dev)
     if h is None:
         h = torch.empty(shape, dtype=dt, device=dev)
     if last is None and want_final:
@@ -1195,8 +1201,8 @@ def _recurrence_bwd(dh, g, h, x, H, W, scan, gate_tau, complement, h0, dlast, wa
         for name, t, want, of in (("dh", dh, shape, dt), ("h", h, shape, dt), ("h0", h0, state, f32),
                                   ("dh_final", dlast, state, f32), ("dh0", dh0, state, f32)):
             _check(name, t, want, (of,), dev)
-    g_ld = _row_stride("g", g, shape, (dt, f32), dev)
-    x_ld = 0 if x is None else _row_stride("x", x, shape, (dt,), dev)
+    g_ld = 0 if _gates(g, shape, dt, index) else _row_stride("g", g, shape, (dt, f32), dev)
+    x_ld = 0 if _is(x, shape, dt, index) else _row_stride("x", x, shape, (dt,), dev)
     if not want_dx:
         dx = None
     elif dx is None:
@@ -1207,8 +1213,8 @@ def _recurrence_bwd(dh, g, h, x, H, W, scan, gate_tau, complement, h0, dlast, wa
         dg = torch.empty(shape, dtype=g.dtype, device=dev)
     if dh0 is None and want_dh0:
         dh0 = torch.empty(state, dtype=f32, device=dev)
-    dx_ld = 0 if dx is None else _row_stride("out", dx, shape, (dt,), dev)
-    dg_ld = 0 if dg is None else _row_stride("dg", dg, shape, (g.dtype,), dev)
+    dx_ld = 0 if _is(dx, shape, dt, index) else _row_stride("out", dx, shape, (dt,), dev)
+    dg_ld = 0 if _is(dg, shape, g.dtype, index) else _row_stride("dg", dg, shape, (g.dtype,), dev)
     a = RecurrenceBwdArgs(dh.data_ptr(), g.data_ptr(), h.data_ptr(), _ptr(x), _ptr(h0), _ptr(dlast), _ptr(dx), _ptr(dg),
                           _ptr(dh0), _DT[dt], _DT[g.dtype], GATE_LOG_DECAY if gate_tau is None else GATE_LOGITS,
                           0.0 if gate_tau is None else gate_tau, bool(complement), _i32(shape[0]), _i32(H), _i32(W),
