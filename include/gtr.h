@@ -568,7 +568,7 @@ gtr_status gtr_ffn_bwd(const gtr_ffn_bwd_args* args, hipStream_t stream);
  * gtr_recurrence_fwd: for every sequence and channel, visiting the tokens of the
  * H x W grid in the order of `scan`,
  *   h_t = a_t h_{t-1} + b_t,  b_t = x_t, or with complement (1 - a_t) x_t
- * a_t = exp(g_t) with g_kind GTR_GATE_LOG_DECAY (-inf forgets all that was before),
+ * a_t = exp(g_t) with g_kind GTR_GATE_LOG_DECAY (g_t <= 0; -inf forgets all before),
  * sigmoid(g_t)^(1 / gate_tau) with GTR_GATE_LOGITS (any g_t, infinities among them);
  * an a_t below 2^-126 is 0.
  * x, h  : [B, H*W, d] dtype (GTR_F32, GTR_F16 or GTR_BF16), tokens in SPATIAL order;
@@ -579,9 +579,11 @@ gtr_status gtr_ffn_bwd(const gtr_ffn_bwd_args* args, hipStream_t stream);
  * h0    : [B, d] float32, the state before the first token in scan order; NULL is 0
  * h_final : [B, d] float32, receives the state after the last one, or NULL; may be
  *         h0 itself, so one call of H = W = 1 is a server's step in place
- * Any d >= 1 and H*W < 2^31 (one token upwards; a 1-D sequence is H = 1), no
- * alignment beyond an element's; a launch's threads stay below 2^32, which passes
- * over B d H W of about 2^40 / 4. Gates and states are float32, h is rounded once.
+ * Any d from 1 to 2^29 and H*W < 2^31 (one token upwards; a 1-D sequence is H = 1),
+ * no alignment beyond an element's; a launch's threads stay below 2^32 (GTR_ERR_SHAPE
+ * beyond: some 10^11 values). Gates and states are float32, h is rounded once.
+ * A NaN, or an infinity in x, reaches its own channel's states from its token on and no
+ * others; an infinity may become a NaN on the way.
  * workspace : where gtr_recurrence_fwd_workspace_size(args) is not 0 (sequences of
  *         more tokens than a work-group takes): 256-byte aligned, at least that many
  *         bytes, no initialisation needed; calls that overlap in time must not share

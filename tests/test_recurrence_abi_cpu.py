@@ -94,3 +94,14 @@ def test_the_binding_refuses_host_tensors():
     for call in (lambda: gtr.gtr_recurrence_fwd(x, x, H=3, W=4), lambda: gtr.gtr_recurrence_bwd(x, x, x, H=3, W=4)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("size", [{"d": (1 << 29) + 1}, {"d": (1 << 31) - 1}, {"B": 1 << 30, "d": 1 << 20},
+                                  {"B": (1 << 31) - 1, "d": 1 << 29}, {"B": (1 << 31) - 1, "H": 1 << 20, "W": 2047},
+                                  {"B": 1 << 26, "d": 128}, {"B": (1 << 31) - 1, "H": 46340, "W": 46340, "d": 1 << 29}])
+def test_sizes_beyond_a_launch(lib, size):
+    """Numbers whose products pass 32 or 64 bits on the way."""
+    size = {"H": 1, "W": 1, **size}
+    for name, make in (("gtr_recurrence_fwd", fwd), ("gtr_recurrence_bwd", bwd)):
+        assert getattr(lib, name)(ctypes.byref(make(**size)), None) == SHAPE
+        assert getattr(lib, name + "_workspace_size")(ctypes.byref(make(**size))) == 0
