@@ -10,11 +10,11 @@
 //
 // Both are a scan of affine maps s -> P s + E, which compose; the backward one runs in
 // the reversed order. One launch (behind one that clears its words), every array once: what
-// bounds long calls is memory (4 x 16384 x 2048 bf16 backward 327 us, 4.9 TB/s; 32768 x 4096
-// bf16 forward 177, 4.5; a large copy reaches 5.0) with, in 16-bit types, the gates' arithmetic
-// not quite hidden behind it (a logit and 1 - a take 22 vector instructions and three
-// exponentials or logarithms; 32768 x 4096 bf16 with 1 - a 204 us, of log decays 181; 16384 x
-// 4096 float32 160); short ones the chain of number, rows, gates, hand-over and stores.
+// bounds long calls is memory (4 x 16384 x 2048 bf16 backward 327 us, 4.9 TB/s; 16384 x 4096
+// float32 forward 156, 5.2; a large copy reaches 5.0) and, in 16-bit types, the gates'
+// arithmetic with it, three exponentials or logarithms per logit (32768 x 4096 bf16 forward of
+// log decays 174 us, of logits 178, with 1 - a 209); short ones the chain of number, rows,
+// gates, hand-over and stores.
 #include <hip/hip_runtime.h>
 
 #include "gtr.h"
@@ -188,9 +188,9 @@ __device__ __forceinline__ void rec_gate(float g, float inv_tau, float& a, float
 // work-groups that wait for ones not started. Waits are bounded all the same: one that
 // runs out makes the states NaN from there on.) A counter hands out 80 numbers per
 // microsecond. Where that counts, in short calls, there are up to 32, each for sequences of
-// its own (8 x 1600 x 384 fp16 18.6 us, with one 20.9); in long ones a single counter keeps
+// its own (8 x 1600 x 384 fp16 16.9 us, with one 19.0); in long ones a single counter keeps
 // blocks of channels that lie next to each other next to each other in time too, which the
-// memory wants (32768 x 4096 bf16 188 us, with 32 counters 232).
+// memory wants (32768 x 4096 bf16 178 us, with 32 counters 221).
 struct RecTiles {
   unsigned long long* maps;    // [sequences][tiles][64 V]
   unsigned long long* states;  // [sequences][groups][64 V]
