@@ -10,7 +10,7 @@
 //
 // Both are a scan of affine maps s -> P s + E, which compose; the backward one runs in
 // the reversed order. One launch (behind one that clears its words), every array once: what
-// bounds long calls is memory (4 x 16384 x 2048 bf16 backward 327 us, 4.9 TB/s; 16384 x 4096
+// bounds long calls is memory (4 x 16384 x 2048 bf16 backward 321 us, 5.0 TB/s; 16384 x 4096
 // float32 forward 156, 5.2; a large copy reaches 5.0) and, in 16-bit types, the gates'
 // arithmetic with it, three exponentials or logarithms per logit (32768 x 4096 bf16 forward of
 // log decays 174 us, of logits 178, with 1 - a 209); short ones the chain of number, rows,
@@ -555,18 +555,30 @@ __global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_bwd_kernel(
   const unsigned cx = (unsigned)k.c * ES, cg = (unsigned)k.c * GS;
   const bool whole = T > 1 && n == T && p.d % V == 0 && p.dx && p.dg;
   const bool to_start = s0 + n == p.L;  // this wave has the scan's first token, before which the state is h0
-  RecVec<DT, V> rd[T], rh[T], rx[T];
-  float a[T][V], keep[T][V], slope[T][V], P[V], E[V], h0[V];
+  RecVec<DT, V> rd[T];
+  float a[T][V], keep[T][V], m[T][V], P[V], E[V], h0[V];  // m: dg over Y
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     P[v] = first ? 0.f : 1.f;
     E[v] = y[v];
     h0[v] = to_start && p.h0 ? p.h0[state + v] : 0.f;
   }
+  // a step's gate, and the state before it
+  auto gate = [&](int t, const RecVec<GT, V>& g, const RecVec<DT, V>& x, const RecVec<DT, V>& h, bool start) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float slope;
+      rec_gate<LOGITS, COMPLEMENT, true>(g.get(v), p.inv_tau, a[t][v], keep[t][v], slope);
+      m[t][v] = start ? h0[v] : h.get(v);
+      if constexpr (COMPLEMENT) m[t][v] -= x.get(v);
+      if constexpr (LOGITS) m[t][v] *= slope;
+    }
+  };
   if (whole) {
     RecWalk w(s0, p.L, p.H, p.W, p.dir);
     RecRow dh(p.dh, row0, dense, w), g(p.g, row0, p.g_ld, w), x(p.x, row0, p.x_ld, w), h(p.h, row0, dense, w);
     RecVec<GT, V> rg[T];
+    RecVec<DT, V> rh[T], rx[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       rd[t].load(dh.p + cx);
@@ -580,17 +592,19 @@ __global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_bwd_kernel(
       x.next(end);
     }
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+    for (int t = 0; t < T; ++t) {
+      gate(t, rg[t], rx[t], rh[t], t + 1 == T && to_start);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        rec_gate<LOGITS, COMPLEMENT, true>(rg[t].get(v), p.inv_tau, a[t][v], keep[t][v], slope[t][v]);
         E[v] = a[t][v] * (rd[t].get(v) + E[v]);
         P[v] *= a[t][v];
       }
+    }
   } else if (n > 0) {
     RecWalk w(s0, p.L, p.H, p.W, p.dir);
     RecRow dh(p.dh, row0, dense, w), g(p.g, row0, p.g_ld, w), x(p.x, row0, p.x_ld, w), h(p.h, row0, dense, w);
     RecVec<GT, V> rg[T];
+    RecVec<DT, V> rh[T], rx[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       rd[t].load(dh.p + cx);
@@ -609,29 +623,28 @@ __global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_bwd_kernel(
       rh[t].load(h.p + cx);
     }
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+    for (int t = 0; t < T; ++t) {
+      gate(t, rg[t], rx[t], rh[t], t + 1 == n && to_start);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        rec_gate<LOGITS, COMPLEMENT, true>(rg[t].get(v), p.inv_tau, a[t][v], keep[t][v], slope[t][v]);
         E[v] = t < n ? a[t][v] * (rd[t].get(v) + E[v]) : E[v];
         P[v] = t < n ? P[v] * a[t][v] : P[v];
       }
+    }
   }
   if constexpr (T > 1) rec_carry<V>(p.t, at, wave, lane, P, E, y);
   if (n <= 0 || k.skip == V) return;
   RecWalk w(s0, p.L, p.H, p.W, p.dir);
   RecRow dx(p.dx, row0, p.dx_ld, w), dg(p.dg, row0, p.dg_ld, w);
   // one step's gradients
-  auto out = [&](const RecVec<DT, V>& rd, const RecVec<DT, V>& rx, const float (&before)[V], const float (&at)[V],
-                 const float (&kt)[V], const float (&st)[V], RecVec<DT, V>& ox, RecVec<GT, V>& og) {
+  auto out = [&](int t, RecVec<DT, V>& ox, RecVec<GT, V>& og) {
     float fx[V], fg[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const float D = rd.get(v) + y[v];
-      y[v] = at[v] * D;
-      fx[v] = COMPLEMENT ? kt[v] * D : D;
-      fg[v] = y[v] * (COMPLEMENT ? before[v] - rx.get(v) : before[v]);
-      if constexpr (LOGITS) fg[v] *= st[v];
+      const float D = rd[t].get(v) + y[v];
+      y[v] = a[t][v] * D;
+      fx[v] = COMPLEMENT ? keep[t][v] * D : D;
+      fg[v] = y[v] * m[t][v];
     }
     ox.set(fx);
     og.set(fg);
@@ -641,10 +654,7 @@ __global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_bwd_kernel(
     for (int t = 0; t < T; ++t) {
       RecVec<DT, V> ox;
       RecVec<GT, V> og;
-      float before[V];
-#pragma unroll
-      for (int v = 0; v < V; ++v) before[v] = t + 1 == T && to_start ? h0[v] : rh[t].get(v);
-      out(rd[t], rx[t], before, a[t], keep[t], slope[t], ox, og);
+      out(t, ox, og);
       ox.store(dx.p + cx);
       og.store(dg.p + cg);
       const bool end = w.next();
@@ -657,10 +667,7 @@ __global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_bwd_kernel(
       if (t < n) {
         RecVec<DT, V> ox;
         RecVec<GT, V> og;
-        float before[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) before[v] = t + 1 == n && to_start ? h0[v] : rh[t].get(v);
-        out(rd[t], rx[t], before, a[t], keep[t], slope[t], ox, og);
+        out(t, ox, og);
         if (p.dx) rec_store(ox, dx.p + cx, k.skip);
         if (p.dg) rec_store(og, dg.p + cg, k.skip);
         const bool end = w.next();
@@ -692,7 +699,7 @@ namespace gtr {
 // while it has them decides how busy it keeps the memory (two work-groups per CU). Us of
 // 16, 8 and 4 waves, forward with 16 steps: 32768 x 4096 bf16 182, 177, 232; 16384 x 4096
 // float32 178, 160, 178; 8 x 1600 x 384 fp16 17.5, 17.2, 18.5 (with 8 steps: 248, 257, 412;
-// 176, 175, 233; 21, 22, 29); backward with 8 steps: 4 x 16384 x 2048 bf16 355, 327, 441;
+// 176, 175, 233; 21, 22, 29); backward with 8 steps: 4 x 16384 x 2048 bf16 355, 321, 441;
 // 1600 x 192 fp16 13.8, 13.8, 14.6. A sequence that 16 waves take is one tile.
 constexpr int kRecFwdSteps = 16, kRecBwdSteps = 8;
 constexpr int kRecTileWaves = 8;
