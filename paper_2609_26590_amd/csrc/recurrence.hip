@@ -702,6 +702,14 @@ namespace gtr {
 // 176, 175, 233; 21, 22, 29); backward with 8 steps: 4 x 16384 x 2048 bf16 355, 321, 441;
 // 1600 x 192 fp16 13.8, 13.8, 14.6. A sequence that 16 waves take is one tile.
 constexpr int kRecFwdSteps = 16, kRecBwdSteps = 8;
+// Backward steps of 16-bit types where sequences are several tiles and all together more than
+// the CUs: as many as the registers hold (float16 logits with 1 - a keep 7 of them in scratch
+// memory). Us with 8 / with these, float16 logits without and with 1 - a: 8 x 1600 x 384 23.7 /
+// 20.4, 25.3 / 22.0; 64 x 400 x 384 27.6 / 27.1, 30.9 / 29.6; 1 x 16384 x 1024 60.6 / 52.1, 65.6
+// / 61.3; 4 x 16384 x 2048 307 / 277, 332 / 327. Few tiles lose: 1 x 1600 x 384 11.1 / 12.1, 11.9
+// / 12.8, and sequences of one tile: 1000 x 64 x 384 44.3 / 58.7, 53.1 / 75.0. In float32 they do
+// not fit (4 x 16384 x 1024 log decays with 1 - a 298, with 12 steps 369).
+constexpr int kRecBwdMore = 12, kRecBwdMoreKeep = 10, kRecCus = 256;
 constexpr int kRecTileWaves = 8;
 constexpr unsigned kRecSpin = 1u << 22;             // polls of a wait, of a microsecond or less each
 
@@ -823,6 +831,12 @@ static void rec_sized(const RecLaunch<P>& a) {
 }
 template <int STEPS, int DT, int GT, class P>
 static void rec_kind(const RecLaunch<P>& a, bool logits, bool complement) {
+  if constexpr (STEPS == kRecBwdSteps && DT != GTR_F32) {
+    if (a.r.T == kRecBwdMore)
+      return logits ? rec_sized<kRecBwdMore, DT, GT, true, false>(a) : rec_sized<kRecBwdMore, DT, GT, false, false>(a);
+    if (a.r.T == kRecBwdMoreKeep)
+      return logits ? rec_sized<kRecBwdMoreKeep, DT, GT, true, true>(a) : rec_sized<kRecBwdMoreKeep, DT, GT, false, true>(a);
+  }
   if (logits)
     complement ? rec_sized<STEPS, DT, GT, true, true>(a) : rec_sized<STEPS, DT, GT, true, false>(a);
   else
@@ -846,7 +860,9 @@ static gtr_status rec_fwd_plan(const gtr_recurrence_fwd_args* a, RecPlan* r) {
 }
 static gtr_status rec_bwd_plan(const gtr_recurrence_bwd_args* a, RecPlan* r) {
   if (!a) return GTR_ERR_NULL;
-  const gtr_status st = rec_plan(a->B, a->H, a->W, a->d, kRecBwdSteps, r);
+  gtr_status st = rec_plan(a->B, a->H, a->W, a->d, kRecBwdSteps, r);
+  if (st == GTR_OK && r->t.tiles > 1 && a->dtype != GTR_F32 && r->sequences * r->t.tiles > kRecCus)
+    st = rec_plan(a->B, a->H, a->W, a->d, a->complement ? kRecBwdMoreKeep : kRecBwdMore, r);
   return st != GTR_OK ? st : rec_types(a->dtype, a->g_dtype, a->g_kind, a->gate_tau, a->scan);
 }
 

@@ -50,12 +50,25 @@ CASES = [(3, 1, 1, 130), (1, 1, 1, 1), (2, 1, 7, 65), (1, 4, 5, 129), (1, 1, 200
 @pytest.mark.parametrize("dt,gt,logits,complement,scan", [(1, 1, 1, 1, 0), (2, 0, 0, 1, 1), (0, 0, 1, 0, 2), (2, 2, 0, 0, 3)])
 @pytest.mark.parametrize("B,H,W,d", CASES)
 def test_addresses(B, H, W, d, dt, gt, logits, complement, scan):
+    addresses(B, H, W, d, dt, gt, logits, complement, scan, ((True, STEPS[0]), (False, STEPS[1])))
+
+
+# the backward steps of calls of many tiles in 16-bit types
+@pytest.mark.parametrize("dt,gt,logits,complement,scan,steps", [(1, 1, 1, 0, 0, 12), (2, 0, 0, 0, 1, 12), (1, 0, 1, 1, 2, 10),
+                                                                (2, 2, 0, 1, 3, 10)])
+@pytest.mark.parametrize("B,H,W,d", [(2, 1, 7, 65), (1, 4, 5, 129), (1, 1, 2000, 64), (2, 9, 300, 131),
+                                     (1, 1, 259, 1)])
+def test_addresses_of_more_steps(B, H, W, d, dt, gt, logits, complement, scan, steps):
+    addresses(B, H, W, d, dt, gt, logits, complement, scan, ((False, steps),))
+
+
+def addresses(B, H, W, d, dt, gt, logits, complement, scan, passes):
     text, L, V = listing("recurrence.hip"), H * W, 1 if d == 1 else 2
     es, gs = (4 if dt == 0 else 2), (4 if gt == 0 else 2)
     ld = d + 3  # x and g as parts of wider rows
     blocks = -(-d // (64 * V))
     seqs = B * blocks
-    for forward, steps in ((True, STEPS[0]), (False, STEPS[1])):
+    for forward, steps in passes:
         T, waves, n = tiles_of(L, steps)
         new = Buffers()
         t = tiles(new, seqs, n, V, 4, blocks)

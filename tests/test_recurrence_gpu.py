@@ -150,6 +150,33 @@ def test_both_passes(gtr, n, shape, dtype):
     both(gtr, *shape, dtype, SCANS[k % 4], k % 2 == 0, k % 3 != 0, k % 5 != 0)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("complement", [False, True])
+@pytest.mark.parametrize("n,shape", list(enumerate([(5, 19, 79, 333), (9, 40, 40, 256), (20, 1, 1000, 1), (1, 1, 33000, 70),
+                                                    (300, 1, 131, 64), (257, 3, 7, 24)])))
+def test_more_tiles_than_cus(gtr, n, shape, complement, dtype):
+    """Where a backward pass in 16 bits has other tiles."""
+    both(gtr, *shape, dtype, SCANS[(n + complement) % 4], (n + (dtype == torch.float16)) % 2 == 0, complement, n % 2 == 0,
+         n in (1, 4), seed=20 + n)
+
+
+def test_more_tiles_than_cus_in_parts(gtr):
+    """Broken steps, one gradient alone, and gradients in place have the same bits as whole steps."""
+    B, L, d = 6, 1111, 258
+    i = inputs(B, L, d, torch.bfloat16, True, 31)
+    for complement in (False, True):
+        kind = dict(H=1, W=L, gate_tau=TAU, complement=complement, h0=i["h0"], dh_final=i["dh_final"])
+        h = gtr.gtr_recurrence_fwd(i["x"], i["g"], H=1, W=L, gate_tau=TAU, complement=complement, h0=i["h0"])[0]
+        want = gtr.gtr_recurrence_bwd(i["dh"], i["g"], h, i["x"], want_dh0=True, **kind)
+        one = gtr.gtr_recurrence_bwd(i["dh"], i["g"], h, i["x"], want_dx=False, **kind)
+        assert torch.equal(one[1], want[1])
+        one = gtr.gtr_recurrence_bwd(i["dh"], i["g"], h, i["x"], want_dg=False, **kind)
+        assert torch.equal(one[0], want[0])
+        t = {k: v.clone() for k, v in i.items()}
+        got = gtr.gtr_recurrence_bwd(t["dh"], t["g"], h, t["x"], out=t["dh"], dg=t["g"], want_dh0=True, **kind)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("scan", SCANS)
 @pytest.mark.parametrize("logits,complement,g32", [(False, False, False), (False, True, True), (True, False, True),
                                                    (True, True, False)])
