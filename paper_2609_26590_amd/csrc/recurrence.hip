@@ -709,6 +709,11 @@ constexpr int kRecFwdSteps = 16, kRecBwdSteps = 8;
 // / 61.3; 4 x 16384 x 2048 307 / 277, 332 / 327. Few tiles lose: 1 x 1600 x 384 11.1 / 12.1, 11.9
 // / 12.8, and sequences of one tile: 1000 x 64 x 384 44.3 / 58.7, 53.1 / 75.0. In float32 they do
 // not fit (4 x 16384 x 1024 log decays with 1 - a 298, with 12 steps 369).
+// Short sequences, a few tokens of each of many: fewer steps, so that more waves share them.
+// Us forward with 16 / with 4, fp16 logits with 1 - a: 4000 x 2 x 384 61 / 22, 32 x 4 x 2048 6.3
+// / 3.5, 512 x 16 x 384 11.4 / 8.0, 512 x 32 x 384 15.3 / 12.5, 512 x 48 x 384 15.6 / 17.3;
+// backward with 8 / with 4: 45 / 33, 5.5 / 4.1, 12.7 / 10.3, and 512 x 24 x 384 14.0 / 15.9.
+constexpr int kRecFew = 4, kRecFwdFew = 32, kRecBwdFew = 16;  // steps; tokens up to which
 constexpr int kRecBwdMore = 12, kRecBwdMoreKeep = 10, kRecCus = 256;
 constexpr int kRecTileWaves = 8;
 constexpr unsigned kRecSpin = 1u << 22;             // polls of a wait, of a microsecond or less each
@@ -722,13 +727,14 @@ struct RecPlan {
   size_t need, clear;  // bytes of workspace, of which those that are cleared
 };
 
-static gtr_status rec_plan(int32_t B, int32_t H, int32_t W, int32_t d, int steps, RecPlan* r) {
+// few: the tokens up to which a wave takes kRecFew steps
+static gtr_status rec_plan(int32_t B, int32_t H, int32_t W, int32_t d, int steps, int few, RecPlan* r) {
   // a lane's byte within a row is a 32-bit number
   if (B <= 0 || H <= 0 || W <= 0 || d <= 0 || d > 1 << 29) return GTR_ERR_SHAPE;
   const int64_t L = (int64_t)H * W;
   if (L >= (int64_t)1 << 31) return GTR_ERR_SHAPE;
   r->V = d == 1 ? 1 : 2;
-  r->T = L == 1 ? 1 : steps;
+  r->T = L == 1 ? 1 : L <= few ? kRecFew : steps;
   const int64_t waves = (L + r->T - 1) / r->T;
   r->waves = (int)(waves <= kRecWaves ? waves : kRecTileWaves);
   const int64_t tiles = (waves + r->waves - 1) / r->waves;
@@ -826,8 +832,15 @@ static void rec_go(const RecLaunch<RecBwd>& a) {
 }
 template <int STEPS, int DT, int GT, bool LOGITS, bool COMPLEMENT, class P>
 static void rec_sized(const RecLaunch<P>& a) {
-  if (a.r.V == 1) return a.r.T == 1 ? rec_go<DT, GT, 1, 1, LOGITS, COMPLEMENT>(a) : rec_go<DT, GT, 1, STEPS, LOGITS, COMPLEMENT>(a);
-  a.r.T == 1 ? rec_go<DT, GT, 2, 1, LOGITS, COMPLEMENT>(a) : rec_go<DT, GT, 2, STEPS, LOGITS, COMPLEMENT>(a);
+  constexpr int FEW = kRecFew;
+  if (a.r.V == 1)
+    a.r.T == 1     ? rec_go<DT, GT, 1, 1, LOGITS, COMPLEMENT>(a)
+    : a.r.T == FEW ? rec_go<DT, GT, 1, FEW, LOGITS, COMPLEMENT>(a)
+                   : rec_go<DT, GT, 1, STEPS, LOGITS, COMPLEMENT>(a);
+  else
+    a.r.T == 1     ? rec_go<DT, GT, 2, 1, LOGITS, COMPLEMENT>(a)
+    : a.r.T == FEW ? rec_go<DT, GT, 2, FEW, LOGITS, COMPLEMENT>(a)
+                   : rec_go<DT, GT, 2, STEPS, LOGITS, COMPLEMENT>(a);
 }
 template <int STEPS, int DT, int GT, class P>
 static void rec_kind(const RecLaunch<P>& a, bool logits, bool complement) {
@@ -855,14 +868,14 @@ static gtr_status rec_launch(const RecLaunch<P>& a, int dt, int gt, bool logits,
 
 static gtr_status rec_fwd_plan(const gtr_recurrence_fwd_args* a, RecPlan* r) {
   if (!a) return GTR_ERR_NULL;
-  const gtr_status st = rec_plan(a->B, a->H, a->W, a->d, kRecFwdSteps, r);
+  const gtr_status st = rec_plan(a->B, a->H, a->W, a->d, kRecFwdSteps, kRecFwdFew, r);
   return st != GTR_OK ? st : rec_types(a->dtype, a->g_dtype, a->g_kind, a->gate_tau, a->scan);
 }
 static gtr_status rec_bwd_plan(const gtr_recurrence_bwd_args* a, RecPlan* r) {
   if (!a) return GTR_ERR_NULL;
-  gtr_status st = rec_plan(a->B, a->H, a->W, a->d, kRecBwdSteps, r);
+  gtr_status st = rec_plan(a->B, a->H, a->W, a->d, kRecBwdSteps, kRecBwdFew, r);
   if (st == GTR_OK && r->t.tiles > 1 && a->dtype != GTR_F32 && r->sequences * r->t.tiles > kRecCus)
-    st = rec_plan(a->B, a->H, a->W, a->d, a->complement ? kRecBwdMoreKeep : kRecBwdMore, r);
+    st = rec_plan(a->B, a->H, a->W, a->d, a->complement ? kRecBwdMoreKeep : kRecBwdMore, 0, r);
   return st != GTR_OK ? st : rec_types(a->dtype, a->g_dtype, a->g_kind, a->gate_tau, a->scan);
 }
 

@@ -62,6 +62,13 @@ def test_addresses_of_more_steps(B, H, W, d, dt, gt, logits, complement, scan, s
     addresses(B, H, W, d, dt, gt, logits, complement, scan, ((False, steps),))
 
 
+# short sequences
+@pytest.mark.parametrize("dt,gt,logits,complement,scan", [(1, 1, 1, 1, 0), (2, 0, 0, 1, 1), (0, 0, 1, 0, 2), (2, 2, 0, 0, 3)])
+@pytest.mark.parametrize("B,H,W,d", [(3, 1, 2, 130), (2, 1, 7, 65), (1, 8, 4, 129), (1, 5, 3, 1), (2, 4, 4, 64)])
+def test_addresses_of_few_steps(B, H, W, d, dt, gt, logits, complement, scan):
+    addresses(B, H, W, d, dt, gt, logits, complement, scan, ((True, 4), (False, 4)))
+
+
 def addresses(B, H, W, d, dt, gt, logits, complement, scan, passes):
     text, L, V = listing("recurrence.hip"), H * W, 1 if d == 1 else 2
     es, gs = (4 if dt == 0 else 2), (4 if gt == 0 else 2)

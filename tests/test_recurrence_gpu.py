@@ -160,6 +160,15 @@ def test_more_tiles_than_cus(gtr, n, shape, complement, dtype):
          n in (1, 4), seed=20 + n)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n,shape", list(enumerate([(3, 1, 2, 130), (40, 1, 5, 65), (5, 4, 4, 333), (300, 1, 17, 24), (7, 8, 4, 200),
+                                                    (2, 11, 3, 64), (9, 2, 8, 1), (6, 1, 32, 1)])))
+def test_short_sequences(gtr, n, shape, dtype):
+    """From two tokens on, about the lengths at which a wave takes other numbers of steps."""
+    for complement in (False, True):
+        both(gtr, *shape, dtype, SCANS[n % 4], (n + complement) % 2 == 0, complement, n % 2 == 0, seed=40 + n)
+
+
 def test_more_tiles_than_cus_in_parts(gtr):
     """Broken steps, one gradient alone, and gradients in place have the same bits as whole steps."""
     B, L, d = 6, 1111, 258
