@@ -10,10 +10,10 @@
 //
 // Both are a scan of affine maps s -> P s + E, which compose; the backward one runs in
 // the reversed order. One launch (behind one that clears its words), every array once: what
-// bounds long calls is memory (4 x 16384 x 2048 bf16 backward 321 us, 5.0 TB/s; 16384 x 4096
+// bounds long calls is memory (4 x 16384 x 2048 bf16 backward 317 us, 5.1 TB/s; 16384 x 4096
 // float32 forward 156, 5.2; a large copy reaches 5.0) and, in 16-bit types, the gates'
-// arithmetic with it, three exponentials or logarithms per logit (32768 x 4096 bf16 forward of
-// log decays 174 us, of logits 178, with 1 - a 209); short ones the chain of number, rows,
+// arithmetic with it, three exponentials or logarithms per logit (32768 x 4096 forward of bf16
+// logits 172 us, of fp16 ones with 1 - a 184); short ones the chain of number, rows,
 // gates, hand-over and stores.
 #include <hip/hip_runtime.h>
 
@@ -744,8 +744,13 @@ static gtr_status rec_plan(int32_t B, int32_t H, int32_t W, int32_t d, int steps
   r->sequences = (int64_t)B * r->t.blocks;
   if (r->sequences >= (int64_t)1 << 26) return GTR_ERR_SHAPE;  // (more threads than a launch has, see below)
   // a hand-over between groups takes about 2 us, in which the sequences' tiles of a group
-  // are read (about 20 ns each): enough of them that the chain does not set the pace
-  r->t.group = r->sequences >= 16 ? 8 : r->sequences >= 8 ? 16 : r->sequences >= 4 ? 32 : 64;
+  // are read (about 20 ns each): enough of them that the chain does not set the pace, and no
+  // more, for maps to be composed again cost more than the hand-over (us forward, backward in
+  // groups of 8 / 4, fp16 with 1 - a: 16 x 1600 x 384 23.7 / 22.8, 33.1 / 32.7; 16 x 8192 x 128
+  // 37.2 / 35.2, 56.7 / 53.4; 1 x 32768 x 4096 190 / 184, 329 / 323; of 16 sequences of 16384
+  // tokens the chain is the longer: 62 / 58, 110 / 113). With one sequence of 65536 x 128 groups
+  // of 64, 32, 16 take 31, 38, 51.
+  r->t.group = r->sequences >= 16 ? 4 : r->sequences >= 8 ? 16 : r->sequences >= 4 ? 32 : 64;
   r->t.groups = (int)((tiles + r->t.group - 1) / r->t.group);
   r->t.spin = kRecSpin;
   r->t.share = (unsigned)(r->sequences * tiles <= 2048 ? up(r->sequences, kRecCounters) : r->sequences);
