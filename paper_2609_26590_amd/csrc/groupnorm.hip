@@ -230,7 +230,7 @@ struct GnStat {
   __device__ __forceinline__ void join(float n2, float mean2, float m22) {
     const float all = n + n2, d = mean2 - mean, f = n > 0.f ? n2 * __builtin_amdgcn_rcpf(all) : 1.f;
     mean = fmaf(d, f, mean);
-    m2 += fmaf(d * d, n * f, m22);
+    m2 += fmaf(d * (n * f), d, m22);  // (d d is past float32 where a far mean meets no values, n or n2 = 0)
     n = all;
   }
   // with the lane's across bit o: both in the same order, the lower lane's first

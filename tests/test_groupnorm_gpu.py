@@ -206,6 +206,15 @@ def test_an_outlier_first(gtr, L):
     check_forward(gtr.gtr_groupnorm_fwd(i["x"], 4, i["w"], i["b"], act="silu"), i, 4, "silu")
 
 
+@pytest.mark.parametrize("L,C,G,dtype,spread", [(5000, 16, 4, torch.float32, 3e16), (64, 3, 1, torch.float32, 6e17),
+                                                (64, 4, 2, torch.bfloat16, 6e17)])
+def test_a_mean_whose_square_is_past_float32(gtr, L, C, G, dtype, spread):
+    """Means of 3e19, of which the square is no float32, and sums of squares about them that are (at most 2e37)."""
+    i = inputs(2, L, C, dtype, 17)
+    i["x"] = (3e19 + spread * i["x"].float()).to(dtype)
+    check_forward(gtr.gtr_groupnorm_fwd(i["x"], G, i["w"], i["b"]), i, G, None)
+
+
 @pytest.mark.parametrize("L", [21, 5001])
 def test_equal_values(gtr, L):
     """A group of equal values gives act(b) and no gradient through the statistics."""
