@@ -215,6 +215,28 @@ def test_a_mean_whose_square_is_past_float32(gtr, L, C, G, dtype, spread):
     check_forward(gtr.gtr_groupnorm_fwd(i["x"], G, i["w"], i["b"]), i, G, None)
 
 
+@pytest.mark.parametrize("dtype,rows", [(torch.float32, 2048), (torch.bfloat16, 1500), (torch.float32, 403)])
+def test_many_equal_values_behind_others(gtr, dtype, rows):
+    """The first row of each lane is 0 and its `rows` others c (an image below a border): mean c (1 - p) and variance
+    c^2 p (1 - p), p = 1 / (rows + 1). A lane's sums are taken about values that leave at most 4 times its n = rows + 1
+    values' sum of squares about their mean, of which the sum of the deviations, squared over n, takes off at most 3:
+    n + 2 roundings of each, so (4 + 2 * 3) (n + 2) e, and 60 e for the moves from value to value (10 at each of 6). The
+    lanes' means are the group's; sums over them go through S = 330 additions, S e more, and the mean is off by
+    (S + 8) e c: relative to the deviation that squared is the variance's. rstd: half of all that and 4 e."""
+    C, G, S = 64, 8, 330
+    lanes = 256 // (C // (4 if dtype == torch.float32 else 8)) * 256  # of one channel: a work-group's rows, 256 tiles
+    n = rows + 1
+    c = torch.linspace(0.7, 2.1, G, device="cuda").to(dtype)
+    x = c.repeat_interleave(C // G).expand(1, lanes * n, C).contiguous()
+    x[:, :lanes] = 0
+    _, mean, rstd = gtr.gtr_groupnorm_fwd(x, G, eps=0.0)
+    c, p = c.double(), 1.0 / n
+    std = c * (p * (1 - p)) ** 0.5
+    emean = (S + 8) * E * c
+    close(mean[0], c * (1 - p), emean, 0.0)
+    close(rstd[0], 1 / std, (0.5 * ((10 * (n + 2) + 60 + S) * E + (emean / std) ** 2) + 4 * E) / std, 0.0)
+
+
 @pytest.mark.parametrize("L", [21, 5001])
 def test_equal_values(gtr, L):
     """A group of equal values gives act(b) and no gradient through the statistics."""
