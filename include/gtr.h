@@ -589,8 +589,10 @@ gtr_status gtr_ffn_bwd(const gtr_ffn_bwd_args* args, hipStream_t stream);
  *         bytes, no initialisation needed; calls that overlap in time must not share
  *         one. It is left with any contents: never a gtr_gla_fwd workspace.
  * spin_limit : polls of a wait between a sequence's work-groups before it gives up
- *         and the states become NaN from there on (0: the library's default, seconds;
- *         no wait depends on work that has not started). A small one is for tests.
+ *         (0: the library's default, seconds; no wait depends on work that has not
+ *         started). The states of a work-group that gave up are NaN; all others are
+ *         right or NaN, later ones and the last included, so a finite h_final does not
+ *         tell that no wait ran out. A small one is for tests.
  */
 typedef struct {
   const void* x;

@@ -20,6 +20,7 @@
 #include "gtr.h"
 #include "gtr_device.h"
 #include "gtr_internal.h"
+#include "rec_words.h"
 
 // Products and sums round as they are written: both ways through a wave's steps give the
 // same bits.
@@ -172,9 +173,9 @@ __device__ __forceinline__ void rec_gate(float g, float inv_tau, float& a, float
 // wave composes its own steps (P, E), the waves' maps meet in LDS, and the state before
 // the tile comes from the tiles before it in one launch, by look-back:
 //
-//   - every tile hands on its map, in one 64-bit word per channel that is its own flag:
-//     zero until it is written (~P in the low half, which no P leaves zero). Words travel by
-//     device-scope atomic loads and stores, so no cache is written back or dropped for them;
+//   - every tile hands on its map, in one 64-bit word per channel that is its own flag
+//     (rec_words.h). Words travel by device-scope atomic loads and stores, so no cache is
+//     written back or dropped for them;
 //   - tiles are in groups. The last tile of a group hands on the state behind the group,
 //     for which it waits for that of the group before. A tile composes the maps of the tiles
 //     before it in its group, shared out over its waves, and applies them to that state.
@@ -185,9 +186,10 @@ __device__ __forceinline__ void rec_gate(float g, float inv_tau, float& a, float
 // first: what a tile waits for has started before it, and a map is handed on before
 // anything is waited for, so every wait ends, whatever else the device is running. (By
 // work-group index instead, two calls on two streams could fill each other's chiplets with
-// work-groups that wait for ones not started. Waits are bounded all the same: one that
-// runs out makes the states NaN from there on.) A counter hands out 80 numbers per
-// microsecond. Where that counts, in short calls, there are up to 32, each for sequences of
+// work-groups that wait for ones not started. Waits are bounded all the same: of one that
+// runs out its work-group's states are NaN, and the one that it hands on behind a group; its
+// own map was handed on before, so others of its group go on.) A counter hands out 80 numbers
+// per microsecond. Where that counts, in short calls, there are up to 32, each for sequences of
 // its own (8 x 1600 x 384 fp16 16.9 us, with one 19.0); in long ones a single counter keeps
 // blocks of channels that lie next to each other next to each other in time too, which the
 // memory wants (32768 x 4096 bf16 178 us, with 32 counters 221).
@@ -202,38 +204,6 @@ struct RecTiles {
 
 constexpr int kRecWaves = 16;
 constexpr unsigned kRecCounters = 32, kRecCounterStep = 32;  // at most; words from one to the next (128 bytes)
-
-__device__ __forceinline__ unsigned long long rec_word(float P, float E) {
-  unsigned lo = ~__builtin_bit_cast(unsigned, P);
-  lo = lo ? lo : ~0x7fc00000u;  // (a NaN with every bit set becomes another one)
-  return (unsigned long long)__builtin_bit_cast(unsigned, E) << 32 | lo;
-}
-__device__ __forceinline__ float rec_map(unsigned long long w) { return __builtin_bit_cast(float, ~(unsigned)w); }
-__device__ __forceinline__ float rec_add(unsigned long long w) { return __builtin_bit_cast(float, (unsigned)(w >> 32)); }
-
-// N lanes' words of this lane's V channels, once all lanes have all of theirs.
-template <int V, int N>
-__device__ __forceinline__ void rec_wait(unsigned long long (&w)[N][V], const unsigned long long* const (&at)[N],
-                                         unsigned spin) {
-  for (unsigned n = 0;; ++n) {
-    bool all = true;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        w[i][v] = __hip_atomic_load(at[i] + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        all &= (unsigned)w[i][v] != 0u;
-      }
-    if (__all(all)) return;
-    if (n >= spin) break;
-    __builtin_amdgcn_s_sleep(1);
-  }
-  const float nan = __builtin_bit_cast(float, 0x7fc00000u);
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int v = 0; v < V; ++v) w[i][v] = rec_word(nan, nan);
-}
 
 struct RecWhere {
   int tile, seq, b, block;  // uniform
