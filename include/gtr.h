@@ -580,8 +580,11 @@ gtr_status gtr_ffn_bwd(const gtr_ffn_bwd_args* args, hipStream_t stream);
  * h_final : [B, d] float32, receives the state after the last one, or NULL; may be
  *         h0 itself, so one call of H = W = 1 is a server's step in place
  * Any d from 1 to 2^29 and H*W < 2^31 (one token upwards; a 1-D sequence is H = 1),
- * no alignment beyond an element's; a launch's threads stay below 2^32 (GTR_ERR_SHAPE
- * beyond: some 10^11 values). Gates and states are float32, h is rounded once.
+ * no alignment beyond an element's. GTR_ERR_SHAPE where a launch would have 2^32
+ * threads or more: B ceil(d / 128) waves of 64 for one token, for each 4 tokens of up to
+ * 32 (backward 16), for each 8 to 16 of longer sequences (so at most 8.6e9 values of one
+ * token, 2e8 where d is 3, 1.4e11 in long sequences). Gates and states are float32, h is
+ * rounded once.
  * A NaN, or an infinity in x, reaches its own channel's states from its token on and no
  * others; an infinity may become a NaN on the way.
  * workspace : where gtr_recurrence_fwd_workspace_size(args) is not 0 (sequences of

@@ -105,3 +105,16 @@ def test_sizes_beyond_a_launch(lib, size):
     for name, make in (("gtr_recurrence_fwd", fwd), ("gtr_recurrence_bwd", bwd)):
         assert getattr(lib, name)(ctypes.byref(make(**size)), None) == SHAPE
         assert getattr(lib, name + "_workspace_size")(ctypes.byref(make(**size))) == 0
+
+
+@pytest.mark.parametrize("size,most", [({"d": 128}, (1 << 26) - 1), ({"d": 3}, (1 << 26) - 1), ({"d": 129}, (1 << 25) - 1),
+                                       ({"W": 4, "d": 1}, (1 << 26) - 1), ({"W": 16, "d": 256}, (1 << 23) - 1),
+                                       ({"W": 32768, "d": 128}, (1 << 15) - 1)])
+def test_the_largest_batch(lib, size, most):
+    """Up to 2^32 - 1 threads: waves of 64 for 1, 4 (here up to 16 tokens) or 16 (forward) tokens of 128 channels."""
+    size = {"H": 1, "W": 1, **size}
+    for name, make in (("gtr_recurrence_fwd", fwd), ("gtr_recurrence_bwd", bwd)):
+        if size["W"] > 32 and make is bwd:
+            continue
+        assert getattr(lib, name)(ctypes.byref(make(B=most, g=None, **size)), None) == NULL
+        assert getattr(lib, name)(ctypes.byref(make(B=most + 1, g=None, **size)), None) == SHAPE
