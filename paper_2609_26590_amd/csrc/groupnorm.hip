@@ -840,7 +840,8 @@ static int pow2_from(int64_t n) {
   return p;
 }
 
-// kg groups per block, the last block at least a vector wide.
+// kg groups per block, the last block at least a vector wide (the groups that this moves to
+// the others never make them wider than kg whole groups were allowed to be).
 static void gn_blocks(GnShape* s, int64_t kg, int VE) {
   int64_t nb = up(s->G, kg);
   kg = up(s->G, nb);
@@ -911,7 +912,6 @@ static gtr_status gn_plan(int32_t B, int64_t L, int32_t C, int32_t G, int dt, bo
   if (s->Cg <= CB) {
     const int kg = CB / s->Cg;
     gn_blocks(s, kg < kGnThreads ? kg : kGnThreads, VE);
-    if ((int64_t)s->kg * s->Cg > CB) gn_blocks(s, kg > 1 ? kg - 1 : 1, VE);
   } else {
     s->kg = 1;
     s->pieces = (int)up(s->Cg, CB);
