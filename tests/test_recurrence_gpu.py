@@ -194,6 +194,31 @@ def test_kinds(gtr, scan, logits, complement, g32):
     both(gtr, 1, 24, 19, 65, torch.bfloat16, scan, logits, complement, False, g32, 3)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n,shape", list(enumerate([(35, 1, 600, 70), (16, 20, 30, 330), (11, 40, 40, 384), (67, 1, 1100, 5),
+                                                    (13, 1, 300, 600)])))
+def test_several_sequences_per_counter(gtr, n, shape, dtype):
+    """35, 48, 33, 67 and 65 sequences of several tiles: counters that number the tiles of 2 or 3 of them each, the last
+    one with numbers that belong to none where these do not divide the sequences."""
+    for complement in (False, True):
+        both(gtr, *shape, dtype, SCANS[(n + complement) % 4], (n + complement) % 2 == 0, complement, n % 2 == 0, seed=60 + n)
+
+
+@pytest.mark.parametrize("tau", [1.0, 3.0, 0.7, 0.01, 1000.0])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_other_taus(gtr, tau, dtype):
+    """1 / tau rounded, and products by it that round: two of the 16 roundings of log a and of the 8 of its slope."""
+    B, H, W, d = 2, 24, 19, 70
+    i = inputs(B, H * W, d, dtype, True, 70)
+    for complement in (False, True):
+        kind = dict(H=H, W=W, scan="col", gate_tau=tau, complement=complement)
+        got = gtr.gtr_recurrence_fwd(i["x"], i["g"], h0=i["h0"], want_final=True, **kind)
+        check_forward(got, i, H, W, "col", tau, complement, i["h0"])
+        back = gtr.gtr_recurrence_bwd(i["dh"], i["g"], got[0], i["x"], h0=i["h0"], dh_final=i["dh_final"], want_dh0=True,
+                                      **kind)
+        check_backward(back, i, got[0], H, W, "col", tau, complement, i["h0"], i["dh_final"])
+
+
 def test_several_groups_of_tiles(gtr):
     """More tokens than two groups of tiles take, and a group and a tile that the end breaks."""
     both(gtr, 1, 1, 20011, 20, torch.float16, "row", True, True, True, seed=4)
