@@ -134,6 +134,18 @@ def test_both_passes(gtr, n, shape, dtype):
         check_backward(back, i, G, act, res is not None)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("B,L,C,G", [(4096, 4, 384, 32), (3000, 1, 40, 4), (700, 16, 96, 8)])
+def test_many_images_of_a_few_tokens(gtr, B, L, C, G, dtype):
+    """dw and db from an image's sums each: 8 threads per column add B / 8 of them, so that no sum goes through more than
+    B / 8 + 100 additions one after the other (fewer than the 630 of the bounds)."""
+    i = inputs(B, L, C, dtype, 18)
+    got = gtr.gtr_groupnorm_fwd(i["x"], G, i["w"], i["b"], act="silu", eps=EPS)
+    check_forward(got, i, G, "silu")
+    back = gtr.gtr_groupnorm_bwd(i["dy"], i["x"], got[1], got[2], i["w"], i["b"], act="silu", dres=i["dres"])
+    check_backward(back, i, G, "silu")
+
+
 @pytest.mark.parametrize("B,L,C,G", [(3, 100, 48, 6), (2, 5000, 72, 8)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_options(gtr, B, L, C, G, dtype):
