@@ -369,6 +369,44 @@ def test_more_than_2_31_elements(gtr):
     assert (dx[1, -3000:].float() - single[0, -3000:].float()).abs().max() <= 0.02
 
 
+def test_more_than_2_31_elements_bit_for_bit(gtr):
+    """The second of two images, 1.15e9 elements each, has the bits of a call of its own: both calls have 256 tiles per
+    image, the most there are. Its last group against 64 bits: a lane's n rows are summed about values that leave at most
+    4 times their sum of squares about their mean, of which their sum takes off 3, with n + 2 roundings of each (10 (n + 2)
+    e); its mean is off by 2 n e D + 3 e A (D the largest deviation from the group's mean, A the largest value), which
+    with a deviation makes twice as much, over the spread, of the variance; sums over lanes and tiles S = 330 e more."""
+    L, C, G, S = 1_150_000, 1000, 5, 330
+    n = L // 1024 + 2  # 4 rows of 64 lanes at a time, in 256 tiles
+    gen = torch.Generator(device="cuda").manual_seed(19)
+    x = torch.empty(2, L, C, dtype=torch.float16, device="cuda")
+    for k in range(2):
+        for at in range(0, L, 50_000):
+            x[k, at:at + 50_000] = torch.randn(50_000, C, generator=gen, device="cuda").half()
+    x[1, ::3] += 1
+    y, mean, rstd = gtr.gtr_groupnorm_fwd(x, G, act="silu")
+    own = x[1:].clone()
+    one = gtr.gtr_groupnorm_fwd(own, G, act="silu")
+    assert torch.equal(y[1], one[0][0]) and torch.equal(mean[1:], one[1]) and torch.equal(rstd[1:], one[2])
+    del one
+    dx = gtr.gtr_groupnorm_bwd(x, x, mean, rstd, act="silu", want_dw=False)[0]
+    single = gtr.gtr_groupnorm_bwd(own, own, mean[1:].clone(), rstd[1:].clone(), act="silu", want_dw=False)[0]
+    assert torch.equal(dx[1], single[0])
+    del dx, single, own
+    last = x[1, :, 800:].double()
+    m = last.mean()
+    dev = last - m
+    var = dev.square().mean()
+    D, A, std = float(dev.abs().max()), float(last.abs().max()), float(var.sqrt())
+    emean = S * E * (2 * D + A) + 2 * n * E * D + 3 * E * A
+    erstd = 0.5 * ((10 * (n + 2) + 60 + S) * E + 2 * (2 * n * E * D + 3 * E * A) / std + (emean / std) ** 2) + 4 * E
+    r = 1 / (var + EPS).sqrt()
+    assert (mean[1, 4].double() - m).abs() <= emean and (rstd[1, 4].double() * (var + EPS).sqrt() - 1).abs() <= erstd
+    u = dev[-3000:] * r
+    eu = r * (emean + 2 * E * A) + u.abs() * (erstd + 3 * E)
+    want = u * torch.sigmoid(u)
+    close(y[1, -3000:, 800:], want, 1.13 * eu + (u.abs() + 6) * E * want.abs(), U[torch.float16], TINY[torch.float16])
+
+
 def test_the_binding_refuses(gtr):
     i = inputs(2, 12, 40, torch.float16, 16)
     x, w = i["x"], i["w"]
