@@ -674,7 +674,8 @@ enum { GTR_ACT_NONE = 2 };
  * x, y : [B, L, C] dtype (GTR_F32, GTR_F16 or GTR_BF16); y may be x (in place)
  * w, b : [C] float32; NULL stands for ones / zeros
  * mean, rstd : [B, groups] float32, for gtr_groupnorm_bwd, or NULL
- * act  : GTR_ACT_NONE, GTR_ACT_SILU or GTR_ACT_GELU
+ * act  : GTR_ACT_NONE, GTR_ACT_SILU or GTR_ACT_GELU of u, in float32 for every type: SiLU
+ *        to (|u| + 6) 2^-24 of itself, GELU to 10^-6 + (1.25 u^2 + 4) 2^-24
  * C a multiple of groups and at most 16384, 1 <= L < 2^31, B L < 2^40; no alignment
  * beyond an element's. 0 <= eps < 1e30 (a group of equal values with eps 0 gives NaN).
  * workspace : where gtr_groupnorm_fwd_workspace_size(args) is not 0, 256-byte

@@ -10,7 +10,7 @@
 // What bounds both is memory and, for small images, the chain of loads, sums and stores.
 // Where an image's block of groups fits the registers of one work-group, it is read once,
 // in one launch (gn_*_image_kernel), else twice by two launches (gn_*_sums_kernel,
-// gn_*_rows_kernel): 16 x 16384 x 512 bf16 forward 175 us, 4.6 TB/s of what both read and
+// gn_*_rows_kernel): 16 x 16384 x 512 bf16 forward 172 us, 4.7 TB/s of what both read and
 // write, 16 x 4096 x 1024 backward with dres 162, 5.0; a large copy reaches 5.0.
 #include <hip/hip_runtime.h>
 
@@ -183,7 +183,11 @@ __device__ __forceinline__ void gn_wave(float (&v)[N], int nl) {
 }
 
 // The waves' sums of each channel lie in cols[wave][element][lane]: by element first, so
-// that neither writes nor reads meet in a bank of LDS.
+// that writes do not meet in a bank of LDS. gn_column's reads do where nl is large: neighbouring
+// threads take neighbouring channels, whose sums lie nl words apart (with nl 64 those of a
+// vector are in one bank). Counted over all CUs: 2.6e5 cycles in the sums of 8 x 1600 x 384
+// forward, 1.8e6 of 16 x 16384 x 512, 3.7e6 of 16 x 4096 x 1024 backward; none with the few
+// lanes per row of an image in one launch.
 template <int DT>
 __device__ __forceinline__ void gn_put(const GnShape& s, float (&v)[Ln<DT>::VE], float* cols) {
   constexpr int VE = Ln<DT>::VE;
@@ -922,7 +926,7 @@ static gtr_status gn_plan(int32_t B, int64_t L, int32_t C, int32_t G, int dt, bo
   const int64_t rp = kGnThreads / s->nl;
   // Up to 8 work-groups per CU and 8 rows per thread or more, for the most part (8 x 1600 x 384
   // fp16 forward 17.1 us, with 4 rows 21.7; 16 x 16384 x 512 bf16 in 512, 1024, 2048 work-groups
-  // 191, 189, 176, backward of 16 x 4096 x 1024 180, 177, 162).
+  // 186, 181, 160, backward of 16 x 4096 x 1024 151, 142, 134, of the same inputs each time).
   const int64_t chains = (int64_t)B * s->blocks;
   int64_t tiles = std::min(up(2048, chains), up(L, rp * 8));
   if (tiles * chains < 256) tiles = std::min(up(256, chains), up(L, rp * 4));

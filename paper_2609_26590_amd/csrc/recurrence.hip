@@ -190,9 +190,9 @@ __device__ __forceinline__ void rec_gate(float g, float inv_tau, float& a, float
 // runs out its work-group's states are NaN, and the one that it hands on behind a group; its
 // own map was handed on before, so others of its group go on.) A counter hands out 80 numbers
 // per microsecond. Where that counts, in short calls, there are up to 32, each for sequences of
-// its own (8 x 1600 x 384 fp16 16.9 us, with one 19.0); in long ones a single counter keeps
+// its own (8 x 1600 x 384 fp16 17.4 us, with one 19.4; 64 x 400 x 384 21.5, 25.5); in long ones a single counter keeps
 // blocks of channels that lie next to each other next to each other in time too, which the
-// memory wants (32768 x 4096 bf16 178 us, with 32 counters 221).
+// memory wants (32768 x 4096 bf16 172 us, with 32 counters 220; backward 4 x 16384 x 2048 322, 351).
 struct RecTiles {
   unsigned long long* maps;    // [sequences][tiles][64 V]
   unsigned long long* states;  // [sequences][groups][64 V]
@@ -378,8 +378,9 @@ __device__ __forceinline__ void rec_fence() { __builtin_amdgcn_sched_barrier(0);
 
 // Both kernels ask for all of a wave's rows at once and keep its gates in registers across
 // the look-back. A whole wave (all T steps, no channels that two lanes have) has a way of
-// its own without masks and tests per row (32768 x 4096 bf16 forward 188 -> 177 us, 4 x 16384
-// x 2048 bf16 backward 372 -> 327).
+// its own without masks and tests per row (32768 x 4096 bf16 forward 172 us, with the other way
+// alone 199; 4 x 16384 x 2048 bf16 backward 322, 373; 8 x 1600 x 384 fp16 17.4, 22.7). Odd
+// widths have the other way in all of their waves.
 template <int DT, int GT, int V, int T, bool LOGITS, bool COMPLEMENT>
 __global__ void __launch_bounds__(64 * (T == 1 ? 1 : kRecWaves)) rec_fwd_kernel(RecFwd p) {
   constexpr int ES = RecVec<DT, V>::ES, GS = RecVec<GT, V>::ES;
@@ -667,17 +668,20 @@ namespace gtr {
 
 // Steps of a wave and waves of a tile: what a work-group holds in registers and moves
 // while it has them decides how busy it keeps the memory (two work-groups per CU). Us of
-// 16, 8 and 4 waves, forward with 16 steps: 32768 x 4096 bf16 182, 177, 232; 16384 x 4096
-// float32 178, 160, 178; 8 x 1600 x 384 fp16 17.5, 17.2, 18.5 (with 8 steps: 248, 257, 412;
-// 176, 175, 233; 21, 22, 29); backward with 8 steps: 4 x 16384 x 2048 bf16 355, 321, 441;
-// 1600 x 192 fp16 13.8, 13.8, 14.6. A sequence that 16 waves take is one tile.
+// 16, 8 and 4 waves, forward with 16 steps: 32768 x 4096 bf16 178, 172, 231; 16384 x 4096
+// float32 175, 156, 172; 8 x 1600 x 384 fp16 19.5, 17.4, 20.2 (8 waves of 8 steps: 244, 170,
+// 19.6); backward: 4 x 16384 x 2048 bf16 336, 322, 368; 4 x 16384 x 1024 float32 321, 300, 330;
+// 1600 x 192 fp16 14.4, 11.7, 11.6. A sequence that 16 waves take is one tile.
 constexpr int kRecFwdSteps = 16, kRecBwdSteps = 8;
 // Backward steps of 16-bit types where sequences are several tiles and all together more than
 // the CUs: as many as the registers hold (float16 logits with 1 - a keep 7 of them in scratch
 // memory). Us with 8 / with these, float16 logits without and with 1 - a: 8 x 1600 x 384 23.7 /
 // 20.4, 25.3 / 22.0; 64 x 400 x 384 27.6 / 27.1, 30.9 / 29.6; 1 x 16384 x 1024 60.6 / 52.1, 65.6
 // / 61.3; 4 x 16384 x 2048 307 / 277, 332 / 327. Few tiles lose: 1 x 1600 x 384 11.1 / 12.1, 11.9
-// / 12.8, and sequences of one tile: 1000 x 64 x 384 44.3 / 58.7, 53.1 / 75.0. In float32 they do
+// / 12.8, and sequences of one tile: 1000 x 64 x 384 44.3 / 58.7, 53.1 / 75.0. (Of 129 to 192 tokens,
+// several tiles of 8 steps but one of these, they gain as well: 64 x 129 x 384 15.4 / 11.3, 17.3 /
+// 13.8; 64 x 160 x 384 15.4 / 12.3, 17.3 / 13.0; 300 x 129 x 384 46.3 / 37.4, 50.5 / 51.2; 300 x
+// 192 x 384 49.4 / 44.9.) In float32 they do
 // not fit (4 x 16384 x 1024 log decays with 1 - a 298, with 12 steps 369).
 // Short sequences, a few tokens of each of many: fewer steps, so that more waves share them.
 // Us forward with 16 / with 4, fp16 logits with 1 - a: 4000 x 2 x 384 61 / 22, 32 x 4 x 2048 6.3

@@ -13,8 +13,9 @@ x [B, H*W, d] (fp16 or bf16, spatial order, a multiple of 8 elements: gtr_add's)
 projection of the caller's); ``p`` holds gn_w and gn_b ([d] float32). The calls allocate
 what they return and may be recorded into a HIP graph. Gradients come from ``backward``
 alone: nothing is recorded for torch's automatic differentiation. The statistics are an
-image's, over all of its tokens, so a server that goes on token by token normalises its
-tokens itself and calls ``step``.
+image's, over all of its tokens: ``forward`` is no causal model's, and ``step`` does not go on
+where it stopped. A server that goes on token by token normalises its tokens itself and calls
+``step``.
 """
 from __future__ import annotations
 
